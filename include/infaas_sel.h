@@ -539,11 +539,169 @@ typedef struct {
 } infaas_sel_info;
 int infaas_sel_get_info(infaas_sel_t *h, infaas_sel_info *out);
 
+/*
+ * ---- Executor: what a worker does with the queries sent to it ---------------------------------
+ *
+ * Case I ends with a variant and a worker; the worker's hardware Executor (Section 3.2) then runs
+ * the variant on the queries that came to it.  For variants that answer in text, one step of one
+ * layer is: append the step's keys and values to a paged cache, attend over it, and, behind the
+ * last layer, draw the next token of every sequence.  Queries of one application come to one
+ * variant with the application's prompt in front of them: that shared part is in the cache once,
+ * and its keys are read once for all sequences of a group.
+ *
+ * An executor is a handle of its own (no variant table; a worker need not be the dispatcher).  The
+ * conventions above hold: calls that take a hip_stream only enqueue, a handle is not thread-safe,
+ * and work enqueued on one handle is ordered by the caller, because its calls share the handle's
+ * scratch memory.  Every argument is checked before anything is enqueued; a refused call returns
+ * INVALID_ARG, changes nothing, and infaas_sel_last_error() says what was refused.  What lies in
+ * DEVICE memory (lengths, positions, pages) is checked by the kernels: see the calls.
+ */
+typedef struct infaas_sel_exec infaas_sel_exec_t; /* opaque; owned by the library */
+
+enum { INFAAS_SEL_TYPE_FP32 = 0, INFAAS_SEL_TYPE_BF16 = 1, INFAAS_SEL_TYPE_FP16 = 2 };
+
+/* A handle for calls on `device`.  Touches no device: the first call that enqueues does.
+ * Errors: INVALID_ARG (null, negative device), OOM. */
+int infaas_sel_exec_create(int32_t device, infaas_sel_exec_t **out);
+
+/* Free the handle and its scratch memory.  NULL is a no-op. */
+void infaas_sel_exec_destroy(infaas_sel_exec_t *x);
+
+/*
+ * One layer's cache of keys and values: two pools of pages in the caller's DEVICE memory.  Key
+ * (or value) number i of KV head j on page p starts at element
+ *     p * page_stride + i * slot_stride + j * head_stride
+ * of its pool and is head_dim consecutive elements long, so both usual orders ([page][slot][head]
+ * and [page][head][slot]) and pools that are interleaved with others are covered.
+ */
+typedef struct {
+    void *d_k, *d_v;        /* pools, 16-byte aligned */
+    int32_t type;           /* INFAAS_SEL_TYPE_BF16 or _FP16 */
+    int32_t kv_heads;       /* >= 1 */
+    int32_t head_dim;       /* 64, 128 or 256 */
+    int32_t page_size;      /* keys to a page, a power of two from 1 to 65536 */
+    int64_t num_pages;      /* >= 1 */
+    int64_t page_stride;    /* strides in elements, multiples of 8 */
+    int64_t slot_stride;
+    int64_t head_stride;
+} infaas_sel_cache;
+
+/*
+ * A ragged batch: the tokens of one step, sequence by sequence, and where the sequences' keys are.
+ * Key j of sequence s is in slot j % page_size of page d_page_table[s][j / page_size].  A token
+ * sees the keys j <= its position of its own sequence, below the sequence's length.  Sequences
+ * that share a prefix are neighbours and form a group: the keys j < d_shared_len[g] of all of
+ * them are those of the group's FIRST sequence (read through its row of the page table).
+ *
+ * The arrays are DEVICE memory and may change from step to step (in a replayed graph, too) as long
+ * as infaas_sel_exec_plan runs behind the change.  What cannot be is skipped: a page outside
+ * 0..num_pages-1, or a key at or beyond max_len or the table's width, is not seen by any token
+ * (and not written by infaas_sel_exec_append); a token that its d_token_seq and d_seq_start do not
+ * both place in a sequence sees nothing.  A token that sees no key gets zeros.
+ */
+typedef struct {
+    int32_t num_tokens;             /* n >= 0 */
+    int32_t num_seqs;               /* S >= 0 */
+    int32_t num_groups;             /* 0: nothing is shared */
+    int32_t heads;                  /* query heads, a multiple of the cache's kv_heads, at most 128 to each */
+    int32_t max_len;                /* no length of d_seq_len is greater */
+    int32_t table_width;            /* pages per row of d_page_table */
+    const int32_t *d_token_seq;     /* [n]   sequence of every token */
+    const int32_t *d_token_pos;     /* [n]   position of every token in its sequence; negative: padding */
+    const int32_t *d_seq_start;     /* [S+1] first token of every sequence (only tokens of this step), then n */
+    const int32_t *d_seq_len;       /* [S]   keys of every sequence, this step's included */
+    const int32_t *d_page_table;    /* [S * table_width] */
+    const int32_t *d_group_start;   /* [num_groups+1] first sequence of every group, then S; null without groups */
+    const int32_t *d_shared_len;    /* [num_groups]   keys that the sequences of a group share; null without groups */
+    void *d_plan;                   /* the caller's DEVICE memory for the plan, 16-byte aligned */
+    int64_t plan_bytes;             /* its size, at least infaas_sel_exec_plan_bytes() */
+} infaas_sel_batch;
+
+/* Bytes that d_plan needs for a batch of these sizes (the pointers are not looked at); 0 when the sizes are refused. */
+int64_t infaas_sel_exec_plan_bytes(const infaas_sel_cache *cache, const infaas_sel_batch *batch);
+
+/*
+ * Grow the handle's scratch memory for infaas_sel_exec_attend on batches of up to this one's sizes.
+ * infaas_sel_exec_attend does the same by itself, but not while its stream is being captured.
+ * Errors: INVALID_ARG, HIP, OOM.
+ */
+int infaas_sel_exec_reserve(infaas_sel_exec_t *x, const infaas_sel_cache *cache, const infaas_sel_batch *batch);
+
+/*
+ * Divide a batch's attention into work items, on the device, into d_plan: once per step, for all
+ * layers (whose caches differ in their pools only).  Errors: INVALID_ARG, HIP.
+ */
+int infaas_sel_exec_plan(infaas_sel_exec_t *x, const infaas_sel_cache *cache, const infaas_sel_batch *batch,
+                         void *hip_stream);
+
+/*
+ * Append a step's keys and values to the cache, rotated by their positions on the way; rotates the
+ * queries as well.  DEVICE arrays [token][head][head_dim] of the cache's type, the last dimension
+ * consecutive, 16-byte aligned, strides in elements and multiples of 8:
+ *   d_q [n][heads], d_k, d_v [n][kv_heads], d_q_out [n][heads] (may be d_q; d_q and d_q_out may both be null)
+ *   d_freq [rot_dim / 2]  rotation frequencies in radians per position, DOUBLE
+ *   rot_dim       how many of a head's leading dimensions are rotated: 0 .. head_dim, a multiple of 16
+ *   interleaved   0: dimension i is paired with i + rot_dim/2; 1: dimension 2i with 2i + 1
+ * The pair (a, b) becomes (a cos t - b sin t, b cos t + a sin t), t = position * frequency.  Angles
+ * are reduced in 64 bits, the products are taken in 32 and rounded once.  Keys of padding, of
+ * sequences outside 0..S-1 and of positions without a page are not written; queries always are.
+ * Needs d_token_seq, d_token_pos and d_page_table of the batch, and no plan.
+ * Errors: INVALID_ARG, HIP.
+ */
+typedef struct {
+    const void *d_q, *d_k, *d_v;
+    void *d_q_out;
+    int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride,
+            out_token_stride, out_head_stride;
+    const double *d_freq;
+    int32_t rot_dim;
+    int32_t interleaved;
+} infaas_sel_append_args;
+int infaas_sel_exec_append(infaas_sel_exec_t *x, const infaas_sel_cache *cache, const infaas_sel_batch *batch,
+                           const infaas_sel_append_args *args, void *hip_stream);
+
+/*
+ * Attention of the batch's tokens over the cache:
+ *     out[t][h] = sum over the keys j that t sees of softmax_j(scale * q[t][h] . k[j][h']) v[j][h'],
+ * h' = h / (heads / kv_heads).  Scores, their running maximum and sum, and the weighted sums are
+ * kept in 32 bits; the weights are rounded to the cache's type for the product with the values.
+ * Query and output arrays as in infaas_sel_exec_append; `scale` is finite and positive.
+ * The batch has to be planned: under a plan of other sizes every element of d_out becomes NaN.
+ * Errors: INVALID_ARG, HIP, OOM.
+ */
+int infaas_sel_exec_attend(infaas_sel_exec_t *x, const infaas_sel_cache *cache, const infaas_sel_batch *batch,
+                           const void *d_q, int64_t q_token_stride, int64_t q_head_stride,
+                           void *d_out, int64_t out_token_stride, int64_t out_head_stride,
+                           float scale, void *hip_stream);
+
+/*
+ * Draw a token of every row of logits.  In row r the tokens are ordered by logit, the greatest
+ * first, equal ones by number; weight w_i = exp((x_i - max x) / temperature).  Kept are, in this order,
+ *     the first top_k,                                                    (0 or less: all)
+ *     of those, token i while the weights before it sum to less than top_p of theirs,  (1 or more: all)
+ *     of those, the tokens with w_i >= min_p,                             (0 or less: all)
+ * and always the first.  The answer is the lowest-numbered kept token whose weight, added to those of
+ * the kept tokens with lower numbers, exceeds draw times their sum.  A temperature of 0 or less (or
+ * NaN) takes the first.  Logits of -infinity and NaN are never drawn; a row of nothing else gives
+ * token -1 and probability 0.  Among logits of +infinity the weights are 1, of the others then 0.
+ * Weights are computed in 64 bits and summed as integers, in units of 2^-43 of the greatest, so
+ * that neither the order of the sums nor rounding moves a border: the draw is reproducible.
+ *   d_logits       [rows][vocab], type INFAAS_SEL_TYPE_*, rows row_stride elements apart
+ *   d_temperature, d_top_k, d_top_p, d_min_p  [rows] limits of every row; null: 1, all, all, all
+ *   d_draw         [rows] random numbers in [0, 1)
+ *   d_out_token    [rows];  d_out_prob [rows] its share of the kept weights (may be null)
+ * rows >= 0, vocab 1..1,048,576.  Errors: INVALID_ARG, HIP, OOM.
+ */
+int infaas_sel_exec_sample(infaas_sel_exec_t *x, int32_t rows, int32_t vocab, int32_t type, const void *d_logits,
+                           int64_t row_stride, const float *d_temperature, const int32_t *d_top_k,
+                           const float *d_top_p, const float *d_min_p, const float *d_draw,
+                           int32_t *d_out_token, float *d_out_prob, void *hip_stream);
+
 /* Static text for a status code. */
 const char *infaas_sel_strerror(int status);
 
 /* Text of the HIP call that failed most recently on the calling thread (which call, HIP's
- * message); empty if none has.  Valid until the next failure on that thread. */
+ * message), or of the argument an executor's call refused; empty if none has.  Valid until the next failure on that thread. */
 const char *infaas_sel_last_error(void);
 
 #ifdef __cplusplus

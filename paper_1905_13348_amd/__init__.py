@@ -14,3 +14,4 @@ from .binding import (  # noqa: F401
     library_path,
     load_library,
 )
+from .executor import Batch, Executor, PagedCache  # noqa: F401

@@ -58,6 +58,26 @@ class _Info(ctypes.Structure):
                 ("lookup_unanswered", ctypes.c_int64), ("index_groups", ctypes.c_int32), ("lookup_route", ctypes.c_int32)]
 
 
+class _Cache(ctypes.Structure):
+    _fields_ = [("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p), ("type", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class _Batch(ctypes.Structure):
+    _fields_ = [("num_tokens", ctypes.c_int32), ("num_seqs", ctypes.c_int32), ("num_groups", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("max_len", ctypes.c_int32), ("table_width", ctypes.c_int32),
+                ("d_token_seq", ctypes.c_void_p), ("d_token_pos", ctypes.c_void_p), ("d_seq_start", ctypes.c_void_p),
+                ("d_seq_len", ctypes.c_void_p), ("d_page_table", ctypes.c_void_p), ("d_group_start", ctypes.c_void_p),
+                ("d_shared_len", ctypes.c_void_p), ("d_plan", ctypes.c_void_p), ("plan_bytes", ctypes.c_int64)]
+
+
+class _AppendArgs(ctypes.Structure):
+    _fields_ = [("d_q", ctypes.c_void_p), ("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p), ("d_q_out", ctypes.c_void_p),
+                *[(f"{t}_{w}_stride", ctypes.c_int64) for t in ("q", "k", "v", "out") for w in ("token", "head")],
+                ("d_freq", ctypes.c_void_p), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
 _lib: Optional[ctypes.CDLL] = None
 
 # every symbol include/infaas_sel.h declares
@@ -69,7 +89,9 @@ EXPORTED = ("infaas_sel_create", "infaas_sel_load_variants", "infaas_sel_update_
             "infaas_sel_select_workers", "infaas_sel_select_workers_closest", "infaas_sel_load_scaling",
             "infaas_sel_scale", "infaas_sel_scale_down", "infaas_sel_destroy", "infaas_sel_reserve",
             "infaas_sel_read_load", "infaas_sel_set_timing", "infaas_sel_get_timings",
-            "infaas_sel_get_info", "infaas_sel_strerror", "infaas_sel_last_error")
+            "infaas_sel_get_info", "infaas_sel_strerror", "infaas_sel_last_error",
+            "infaas_sel_exec_create", "infaas_sel_exec_destroy", "infaas_sel_exec_plan_bytes", "infaas_sel_exec_reserve",
+            "infaas_sel_exec_plan", "infaas_sel_exec_append", "infaas_sel_exec_attend", "infaas_sel_exec_sample")
 
 
 def library_path() -> str:
@@ -123,8 +145,20 @@ def load_library() -> ctypes.CDLL:
     lib.infaas_sel_strerror.restype = ctypes.c_char_p
     lib.infaas_sel_last_error.argtypes = []
     lib.infaas_sel_last_error.restype = ctypes.c_char_p
+    cp, bp, i32, i64 = ctypes.POINTER(_Cache), ctypes.POINTER(_Batch), ctypes.c_int32, ctypes.c_int64
+    lib.infaas_sel_exec_create.argtypes = [i32, ctypes.POINTER(vp)]
+    lib.infaas_sel_exec_destroy.argtypes = [vp]
+    lib.infaas_sel_exec_destroy.restype = None
+    lib.infaas_sel_exec_plan_bytes.argtypes = [cp, bp]
+    lib.infaas_sel_exec_plan_bytes.restype = i64
+    lib.infaas_sel_exec_reserve.argtypes = [vp, cp, bp]
+    lib.infaas_sel_exec_plan.argtypes = [vp, cp, bp, vp]
+    lib.infaas_sel_exec_append.argtypes = [vp, cp, bp, ctypes.POINTER(_AppendArgs), vp]
+    lib.infaas_sel_exec_attend.argtypes = [vp, cp, bp, vp, i64, i64, vp, i64, i64, ctypes.c_float, vp]
+    lib.infaas_sel_exec_sample.argtypes = [vp, i32, i32, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]
     for name in EXPORTED:
-        if name not in ("infaas_sel_destroy", "infaas_sel_strerror", "infaas_sel_last_error"):
+        if name not in ("infaas_sel_destroy", "infaas_sel_strerror", "infaas_sel_last_error", "infaas_sel_exec_destroy",
+                        "infaas_sel_exec_plan_bytes"):
             getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib

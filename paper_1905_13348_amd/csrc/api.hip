@@ -15,7 +15,7 @@ using namespace infaas;
 
 namespace {
 
-thread_local char g_last_error[320] = "";
+thread_local char g_last_error[kErrorText] = "";
 
 // Records which HIP call failed and why; returns true when the call succeeded.
 bool hip_ok(hipError_t e, const char *what)
@@ -89,6 +89,8 @@ hipError_t dev_alloc(T **p, size_t count)
 }
 
 }  // namespace
+
+char *infaas::error_text() { return g_last_error; }
 
 struct infaas_sel {
     int32_t T = 0, B = 0, device = 0;

@@ -1,0 +1,464 @@
+// Attention of a ragged batch over a paged cache, what groups of sequences share read once (infaas_sel_exec_attend):
+// the plan, the items and the merge of their results.
+#include "exec.h"
+
+namespace infaas {
+
+namespace {
+
+// ---- the plan ---------------------------------------------------------------------------------
+
+constexpr int kPlanThreads = 1024;
+
+__device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
+
+// What unit u (a sequence, or behind those a group) has to have computed: its tokens and keys.
+struct UnitRange { int t0, nt, k0, k1, seq; };
+
+__device__ __forceinline__ int seq_limit(const BatchArgs &b, const CacheArgs &c, int s) { return clampi(b.seq_len[s], 0, c.max_len); }
+
+// Group of a sequence, or -1.
+__device__ __forceinline__ int group_of(const BatchArgs &b, int s)
+{
+    int lo = 0, hi = b.num_groups;      // the last g with group_start[g] <= s
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (mid <= b.num_groups - 1 && b.group_start[mid] <= s) lo = mid;
+        else hi = mid - 1;
+    }
+    return b.num_groups > 0 && b.group_start[lo] <= s && s < b.group_start[lo + 1] ? lo : -1;
+}
+
+__device__ __forceinline__ int shared_of(const BatchArgs &b, const CacheArgs &c, int g)
+{
+    return g < 0 ? 0 : clampi(b.shared_len[g], 0, c.max_len);
+}
+
+__device__ __forceinline__ UnitRange unit_range(const BatchArgs &b, const CacheArgs &c, int u)
+{
+    UnitRange r;
+    if (u < b.num_seqs) {
+        r.seq = u;
+        r.t0 = clampi(b.seq_start[u], 0, b.num_tokens);
+        r.nt = clampi(b.seq_start[u + 1], r.t0, b.num_tokens) - r.t0;
+        r.k1 = seq_limit(b, c, u);
+        r.k0 = min(shared_of(b, c, group_of(b, u)), r.k1);
+    } else {
+        const int g = u - b.num_seqs;
+        const int a = clampi(b.group_start[g], 0, b.num_seqs), e = clampi(b.group_start[g + 1], a, b.num_seqs);
+        r.seq = a < b.num_seqs ? a : 0;
+        r.t0 = clampi(b.seq_start[a], 0, b.num_tokens);
+        r.nt = e > a ? clampi(b.seq_start[e], r.t0, b.num_tokens) - r.t0 : 0;
+        r.k0 = 0;
+        r.k1 = shared_of(b, c, g);
+    }
+    return r;
+}
+
+// One workgroup.  The cost of a tile is its keys; chunks are as long as makes kTargetItems items of all tiles, and the
+// same for all, so that items are of one length but for the last of each tile.
+__global__ __launch_bounds__(kPlanThreads) void k_plan(BatchArgs b, CacheArgs c, PlanView p, int max_items, int max_rows)
+{
+    __shared__ unsigned long long cost;
+    __shared__ long long scan[2][kPlanThreads / 64];
+    __shared__ long long totals[2];
+    const int tid = threadIdx.x, G = b.heads / b.kv_heads, per_tile = kTileRows / G, units = b.num_seqs + b.num_groups;
+    if (tid == 0) { cost = 0; totals[0] = totals[1] = 0; }
+    __syncthreads();
+    unsigned long long mine = 0;
+    for (int u = tid; u < units; u += kPlanThreads) {
+        const UnitRange r = unit_range(b, c, u);
+        mine += (unsigned long long)((r.nt + per_tile - 1) / per_tile) * (unsigned)(r.k1 - r.k0);
+    }
+    atomicAdd(&cost, mine);
+    __syncthreads();
+    const unsigned long long each = cost * (unsigned)b.kv_heads / kTargetItems + 1;
+    const int chunk = each > 0x7fffff00ull ? 0x7fffff00
+                                           : max(kMinChunk, (int)((each + kChunkStep - 1) / kChunkStep) * kChunkStep);
+
+    // first item and first row of every unit: a running sum over blocks of units
+    for (int u0 = 0; u0 < units; u0 += kPlanThreads) {
+        const int u = u0 + tid;
+        long long items = 0, rows = 0;
+        PlanUnit pu{};
+        if (u < units) {
+            const UnitRange r = unit_range(b, c, u);
+            pu.tiles = (r.nt + per_tile - 1) / per_tile;
+            pu.splits = r.nt > 0 ? (int)(((int64_t)(r.k1 - r.k0) + chunk - 1) / chunk) : 0;
+            items = (long long)pu.tiles * pu.splits;
+            rows = (long long)r.nt * G * pu.splits;
+        }
+        long long si = items, sr = rows;
+        for (int d = 1; d < 64; d <<= 1) {
+            const long long ai = __shfl_up(si, d), ar = __shfl_up(sr, d);
+            if ((tid & 63) >= d) { si += ai; sr += ar; }
+        }
+        if ((tid & 63) == 63) { scan[0][tid >> 6] = si; scan[1][tid >> 6] = sr; }
+        __syncthreads();
+        long long bi = totals[0], br = totals[1];
+        for (int w = 0; w < (tid >> 6); ++w) { bi += scan[0][w]; br += scan[1][w]; }
+        if (u < units) {
+            pu.first_item = (int)(bi + si - items);
+            pu.first_row = (int)(br + sr - rows);
+            p.units[u] = pu;
+        }
+        __syncthreads();
+        if (tid == kPlanThreads - 1) { totals[0] = bi + si; totals[1] = br + sr; }
+        __syncthreads();
+    }
+    __threadfence_block();
+    // (arrays that contradict each other, like starts that fall, can ask for more than there is room for)
+    const bool fits = totals[0] * b.kv_heads <= max_items && totals[1] <= max_rows;
+    const int n = fits ? (int)totals[0] * b.kv_heads : 0, rows1 = fits ? (int)totals[1] : 0;
+    if (tid == 0)
+        *p.head = PlanHeader{kPlanMagic, b.num_tokens, b.num_seqs, b.num_groups, b.heads, b.kv_heads, b.head_dim,
+                             c.max_len, c.table_width, c.page_shift, n, rows1, {0}};
+
+    for (int i = tid; i < n; i += kPlanThreads) {
+        int lo = 0, hi = units - 1;      // the last unit that starts at or before item i (units without items share a start)
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (p.units[mid].first_item * b.kv_heads <= i) lo = mid;
+            else hi = mid - 1;
+        }
+        const PlanUnit pu = p.units[lo];
+        const UnitRange r = unit_range(b, c, lo);
+        // tiles that read the same keys are neighbours, then the heads, then the chunks
+        const int at = i - pu.first_item * b.kv_heads, tile = at % pu.tiles, head = at / pu.tiles % b.kv_heads, split = at / pu.tiles / b.kv_heads;
+        PlanItem it{};
+        it.t0 = r.t0 + tile * per_tile;
+        it.nt = min(per_tile, r.nt - tile * per_tile);
+        it.k0 = r.k0 + (int)min((int64_t)split * chunk, (int64_t)(r.k1 - r.k0));
+        it.k1 = (int)min((int64_t)it.k0 + chunk, (int64_t)r.k1);
+        it.seq = r.seq;
+        it.head = head;
+        const bool direct = lo < b.num_seqs && pu.splits == 1 && r.k0 == 0;
+        it.base = direct ? -1 : head * rows1 + pu.first_row + (split * r.nt + tile * per_tile) * G;
+        p.items[i] = it;
+    }
+
+    for (int t = tid; t < b.num_tokens; t += kPlanThreads) {
+        PlanToken pt{};
+        const int s = b.token_seq[t];
+        if (fits && (uint32_t)s < (uint32_t)b.num_seqs) {
+            const UnitRange r = unit_range(b, c, s);
+            if (t >= r.t0 && t < r.t0 + r.nt) {
+                const PlanUnit pu = p.units[s];
+                pt.limit = clampi(b.token_pos[t], -1, r.k1 - 1) + 1;
+                pt.own_splits = pu.splits;
+                pt.own_stride = r.nt * G;
+                pt.own_base = pu.first_row + (t - r.t0) * G;
+                pt.direct = pu.splits == 1 && r.k0 == 0;
+                const int g = group_of(b, s);
+                if (g >= 0) {
+                    const UnitRange q = unit_range(b, c, b.num_seqs + g);
+                    const PlanUnit qu = p.units[b.num_seqs + g];
+                    if (t >= q.t0 && t < q.t0 + q.nt) {
+                        pt.pre_splits = qu.splits;
+                        pt.pre_stride = q.nt * G;
+                        pt.pre_base = qu.first_row + (t - q.t0) * G;
+                    }
+                }
+            }
+        }
+        p.tokens[t] = pt;
+    }
+}
+
+// Whether the plan in memory was made for the batch of this call.
+__device__ __forceinline__ bool plan_fits(const AttendArgs &a)
+{
+    const PlanHeader &h = *a.plan.head;
+    const BatchArgs &b = a.batch;
+    return h.magic == kPlanMagic && h.num_tokens == b.num_tokens && h.num_seqs == b.num_seqs && h.num_groups == b.num_groups &&
+           h.heads == b.heads && h.kv_heads == b.kv_heads && h.head_dim == b.head_dim && h.max_len == a.cache.max_len &&
+           h.table_width == a.cache.table_width && h.page_shift == a.cache.page_shift;
+}
+
+// ---- items ------------------------------------------------------------------------------------
+
+typedef __attribute__((address_space(3))) vec<short, 4> lds_short4;
+
+template <typename T> struct Mfma;
+template <> struct Mfma<bf16_t> {
+    static __device__ __forceinline__ vec<float, 16> run(vec<bf16_t, 8> a, vec<bf16_t, 8> b, vec<float, 16> c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+};
+template <> struct Mfma<fp16_t> {
+    static __device__ __forceinline__ vec<float, 16> run(vec<fp16_t, 8> a, vec<fp16_t, 8> b, vec<float, 16> c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    }
+};
+
+// Where the 16-byte piece `c` of row `r` of a staged tile is: rows that the lanes of one LDS instruction read lie in
+// different banks.  Keys are read a row per lane (32 rows, the same piece), values four rows at a time (four pieces).
+template <int CH> __device__ __forceinline__ int key_slot(int r, int c) { return r * CH + (c ^ (CH == 8 ? (r >> 1) & 7 : r & 15)); }
+template <int CH> __device__ __forceinline__ int value_slot(int r, int c) { return r * CH + (c ^ (CH == 8 ? ((r >> 1) & 1) << 2 : (r & 3) << 2)); }
+
+// exp2 on the hardware's unit: 1 ulp of 32 bits, and 0 for -infinity.
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// A workgroup of four waves takes items of up to 128 rows, 32 to a wave.  With K the A operand, S^T = K Q^T leaves a lane
+// with scores of ONE row (its column), so the running maximum and sum are a lane's own, and P^T is in registers where
+// the B operand of O^T = V^T P^T wants it: key slots of the second product are numbered as the first one leaves them.
+// V^T's rows come from LDS through the transposing read.  Keys and values of a tile go through registers to LDS, the
+// next tile's while this one is computed.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_attend_items(AttendArgs a)
+{
+    constexpr int KB = D == 256 ? 32 : 64, CH = D / 8, LOADS = KB * CH / 256;
+    __shared__ uint4 lk[2][KB * CH], lv[2][KB * CH];
+    __shared__ int seen[2][KB];
+    __shared__ int reach[4];
+    if (!plan_fits(a)) return;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 31, half = lane >> 5;
+    const int G = a.batch.heads / a.batch.kv_heads;
+    const int n = a.plan.head->num_items;
+    const uint32_t inv_g = 65536 / G + 1;          // r / G for r < 128
+    const uint4 *kp = (const uint4 *)a.cache.k, *vp = (const uint4 *)a.cache.v;
+    const int page_mask = (1 << a.cache.page_shift) - 1;
+
+    // Workgroups go to the eight dies in turn; each die takes a stretch of the list, so that neighbouring items (the
+    // tiles that read the same keys) meet in one L2.
+    const int die = blockIdx.x & 7, dies = min((int)gridDim.x, 8);
+    const int from = (int)((int64_t)n * die / dies), to = (int)((int64_t)n * (die + 1) / dies);
+    const int step = ((int)gridDim.x - die + 7) / 8;
+    for (int i = from + (int)(blockIdx.x >> 3); i < to; i += step) {
+        const PlanItem it = a.plan.items[i];
+        const int rows = it.nt * G;
+        const int r = wave * 32 + col;
+        const bool valid = r < rows;
+        const int rt = (int)((uint32_t)r * inv_g >> 16), token = it.t0 + rt, head = it.head * G + r - rt * G;
+        const int lim = valid ? min(a.plan.tokens[token].limit, it.k1) : 0;
+        vec<T, 8> q[D / 16];
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+            q[kk] = vec<T, 8>{};
+            if (valid) q[kk] = *(const vec<T, 8> *)((const T *)a.q + token * a.q_token_stride + head * a.q_head_stride + kk * 16 + half * 8);
+        }
+        // how far the wave's rows see: none (hi), all (lo)
+        int hi = lim, lo = valid ? lim : 0x7fffffff;
+        for (int d = 1; d < 32; d <<= 1) { hi = max(hi, __shfl_xor(hi, d)); lo = min(lo, __shfl_xor(lo, d)); }
+        hi = __builtin_amdgcn_readfirstlane(hi);
+        lo = __builtin_amdgcn_readfirstlane(lo);
+        __syncthreads();
+        if (lane == 0) reach[wave] = hi;
+        __syncthreads();
+        const int end = max(max(reach[0], reach[1]), max(reach[2], reach[3]));
+
+        vec<float, 16> o[D / 32];
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) o[dt] = vec<float, 16>{};
+        float m = -INFINITY, l = 0;
+
+        uint4 rk[LOADS], rv[LOADS];
+        int ok = 0;
+        auto fetch = [&](int kt) {
+            ok = 0;
+#pragma unroll
+            for (int x = 0; x < LOADS; ++x) {
+                const int slot = x * 256 + tid, row = slot / CH, c = slot % CH, key = kt + row, near = min(key, end - 1);
+                int64_t page = a.cache.table[(int64_t)it.seq * a.cache.table_width + (near >> a.cache.page_shift)];
+                const bool there = page >= 0 && page < a.cache.num_pages;
+                page = there ? page : 0;
+                const int64_t at = (page * a.cache.page_stride + (int64_t)(near & page_mask) * a.cache.slot_stride + it.head * a.cache.head_stride) / 8 + c;
+                rk[x] = kp[at];
+                rv[x] = vp[at];
+                const bool use = there && key < end;
+                if (!use) rv[x] = uint4{0, 0, 0, 0};     // (whatever is there: it may be no number)
+                ok |= (int)use << x;
+            }
+        };
+        auto stage = [&](int buf) {
+#pragma unroll
+            for (int x = 0; x < LOADS; ++x) {
+                const int slot = x * 256 + tid, row = slot / CH, c = slot % CH;
+                lk[buf][key_slot<CH>(row, c)] = rk[x];
+                lv[buf][value_slot<CH>(row, c)] = rv[x];
+                if (c == 0) seen[buf][row] = ok >> x & 1;
+            }
+        };
+        if (end > it.k0) {
+            fetch(it.k0);
+            stage(0);
+        }
+        __syncthreads();
+        int buf = 0;
+        for (int kt = it.k0; kt < end; kt += KB, buf ^= 1) {
+            const bool more = kt + KB < end;
+            if (more) fetch(kt + KB);
+            if (kt < hi) {
+                vec<float, 16> s[KB / 32];
+#pragma unroll
+                for (int kb = 0; kb < KB / 32; ++kb) {
+                    s[kb] = vec<float, 16>{};
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const vec<T, 8> k = *(const vec<T, 8> *)&lk[buf][key_slot<CH>(kb * 32 + col, kk * 2 + half)];
+                        s[kb] = Mfma<T>::run(k, q[kk], s[kb]);
+                    }
+                }
+                const unsigned long long bits = __ballot(seen[buf][lane & (KB - 1)] != 0);
+                if (kt + KB > lo || bits != ~0ull) {
+#pragma unroll
+                    for (int kb = 0; kb < KB / 32; ++kb)
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) {
+                            const int row = kb * 32 + 8 * (x / 4) + 4 * half + x % 4;
+                            const bool vis = kt + row < lim && (bits >> row & 1);
+                            s[kb][x] = vis ? s[kb][x] : -INFINITY;
+                        }
+                }
+                float top = s[0][0];
+#pragma unroll
+                for (int kb = 0; kb < KB / 32; ++kb)
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) top = fmaxf(top, s[kb][x]);
+                top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
+                if (__any(top > m)) {
+                    const float m2 = fmaxf(m, top);
+                    const float f = m2 == -INFINITY ? 1.0f : exp2_fast(m - m2);
+                    m = m2;
+                    l *= f;
+#pragma unroll
+                    for (int dt = 0; dt < D / 32; ++dt) o[dt] *= f;
+                }
+                const float ref = m == -INFINITY ? 0.0f : m;      // (a row that has seen nothing yet)
+                vec<T, 8> pt[KB / 16];
+#pragma unroll
+                for (int kb = 0; kb < KB / 32; ++kb)
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        const float e = exp2_fast(s[kb][x] * a.scale_log2 - ref);
+                        l += e;
+                        pt[kb * 2 + x / 8][x % 8] = (T)e;
+                    }
+                const int j = lane & 15, quarter = (lane >> 4) & 1;
+#pragma unroll
+                for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                    for (int g = 0; g < KB / 16; ++g) {
+                        const int row = g * 16 + half * 4 + j / 4, c = dt * 4 + quarter * 2 + (j & 3) / 2;
+                        const short *at0 = (const short *)&lv[buf][value_slot<CH>(row, c)] + (j & 1) * 4;
+                        const short *at1 = (const short *)&lv[buf][value_slot<CH>(row + 8, c)] + (j & 1) * 4;
+                        union { vec<short, 4> h[2]; vec<T, 8> v; } v;
+                        v.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)at0);
+                        v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)at1);
+                        o[dt] = Mfma<T>::run(v.v, pt[g], o[dt]);
+                    }
+            }
+            if (more) stage(buf ^ 1);
+            __syncthreads();
+        }
+
+        l += __shfl_xor(l, 32);
+        if (valid && it.base < 0) {
+            const float f = l > 0 ? 1.0f / l : (l == 0 ? 0.0f : l);     // (no key: zeros; NaN stays)
+            T *out = (T *)a.out + token * a.out_token_stride + head * a.out_head_stride;
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    vec<T, 4> y;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = (T)(o[dt][4 * x + e] * f);
+                    *(vec<T, 4> *)(out + dt * 32 + 8 * x + 4 * half) = y;
+                }
+        } else if (valid) {
+            const int64_t row = (int64_t)it.base + r;
+            if (half == 0) a.part_ml[row] = float2{m, l};
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    *(vec<float, 4> *)(a.part_o + row * D + dt * 32 + 8 * x + 4 * half) =
+                        vec<float, 4>{o[dt][4 * x], o[dt][4 * x + 1], o[dt][4 * x + 2], o[dt][4 * x + 3]};
+        }
+    }
+}
+
+// ---- merge ------------------------------------------------------------------------------------
+
+// A workgroup per (token, query head): D/4 threads side by side take four dimensions each, the others further splits.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a)
+{
+    constexpr int W = D / 4, LANES = 256 / W;
+    __shared__ float lm[LANES], ll[LANES];
+    __shared__ vec<float, 4> lo[LANES][W];
+    const int token = blockIdx.x / a.batch.heads, head = blockIdx.x % a.batch.heads;
+    const int d = threadIdx.x % W, lane = threadIdx.x / W;
+    T *out = (T *)a.out + token * a.out_token_stride + head * a.out_head_stride + d * 4;
+    if (!plan_fits(a)) {
+        if (lane == 0) *(vec<T, 4> *)out = vec<T, 4>{(T)NAN, (T)NAN, (T)NAN, (T)NAN};
+        return;
+    }
+    const PlanToken pt = a.plan.tokens[token];
+    if (pt.direct) return;
+    const int G = a.batch.heads / a.batch.kv_heads;
+    const int64_t first = (int64_t)(head / G) * a.plan.head->rows + head % G;
+    float m = -INFINITY, l = 0;
+    vec<float, 4> o = vec<float, 4>{};
+    for (int s = lane; s < pt.own_splits + pt.pre_splits; s += LANES) {
+        const int64_t row = first + (s < pt.pre_splits ? pt.pre_base + (int64_t)s * pt.pre_stride
+                                                       : pt.own_base + (int64_t)(s - pt.pre_splits) * pt.own_stride);
+        const float2 ml = a.part_ml[row];
+        const vec<float, 4> x = *(const vec<float, 4> *)(a.part_o + row * D + d * 4);
+        if (ml.x == -INFINITY && ml.y == 0) continue;        // nothing seen
+        const float m2 = fmaxf(m, ml.x), f = exp2_fast(m - m2), g = exp2_fast(ml.x - m2);
+        o = m == -INFINITY ? x * g : o * f + x * g;
+        l = m == -INFINITY ? ml.y * g : l * f + ml.y * g;
+        m = m2;
+    }
+    if (d == 0) { lm[lane] = m; ll[lane] = l; }
+    lo[lane][d] = o;
+    __syncthreads();
+    if (lane != 0) return;
+    for (int s = 1; s < LANES; ++s) {
+        if (lm[s] == -INFINITY && ll[s] == 0) continue;
+        const float m2 = fmaxf(m, lm[s]), f = exp2_fast(m - m2), g = exp2_fast(lm[s] - m2);
+        o = m == -INFINITY ? lo[s][d] * g : o * f + lo[s][d] * g;
+        l = m == -INFINITY ? ll[s] * g : l * f + ll[s] * g;
+        m = m2;
+    }
+    const float f = l > 0 ? 1.0f / l : (l == 0 ? 0.0f : l);
+    *(vec<T, 4> *)out = vec<T, 4>{(T)(o[0] * f), (T)(o[1] * f), (T)(o[2] * f), (T)(o[3] * f)};
+}
+
+template <typename T, int D>
+hipError_t attend(const AttendArgs &a, int64_t max_items, hipStream_t s)
+{
+    const int grid = (int)(max_items < 2048 ? max_items : 2048);
+    k_attend_items<T, D><<<grid, 256, 0, s>>>(a);
+    if (hipError_t e = hipGetLastError()) return e;
+    k_attend_merge<T, D><<<(unsigned)a.batch.num_tokens * a.batch.heads, 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t attend(const AttendArgs &a, int64_t max_items, hipStream_t s)
+{
+    switch (a.batch.head_dim) {
+    case 64: return attend<T, 64>(a, max_items, s);
+    case 128: return attend<T, 128>(a, max_items, s);
+    default: return attend<T, 256>(a, max_items, s);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_plan(const BatchArgs &b, const CacheArgs &c, const PlanView &p, const PlanSizes &z, hipStream_t s)
+{
+    k_plan<<<1, kPlanThreads, 0, s>>>(b, c, p, (int)z.max_items, (int)z.max_rows);
+    return hipGetLastError();
+}
+
+hipError_t launch_attend(const AttendArgs &a, int32_t type, int64_t max_items, hipStream_t s)
+{
+    return type == INFAAS_SEL_TYPE_BF16 ? attend<bf16_t>(a, max_items, s) : attend<fp16_t>(a, max_items, s);
+}
+
+}  // namespace infaas

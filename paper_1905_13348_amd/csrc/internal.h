@@ -7,6 +7,10 @@
 
 namespace infaas {
 
+// The calling thread's text for infaas_sel_last_error().
+constexpr int kErrorText = 320;
+char *error_text();
+
 constexpr int kQueriesPerTile = 512;     // queries that share one staged slice in the scan
 constexpr uint32_t kNoRank = 0xFFFFFFFFu; // "no feasible variant" in rank space
 constexpr int kLdsHistMaxSlices = 8192;   // per-workgroup LDS histogram up to this many slices

@@ -1,0 +1,188 @@
+"""What a worker does with the queries sent to it: the executor's calls of include/infaas_sel.h on torch tensors.
+
+    ex = Executor()
+    cache = ex.cache(k_pool, v_pool)                     # one layer's pools of pages
+    batch = ex.batch(cache, heads, token_seq=..., ...)   # the step's tokens and the sequences' pages
+    ex.plan(batch)                                       # once a step, for all layers
+    ex.append(cache, batch, q, k, v, q_out, freq)        # each layer
+    ex.attend(cache, batch, q_out, out, scale)
+    ex.sample(logits, draws, token, prob, top_p=...)     # behind the last layer
+
+Argument marshalling only, like ``Selector``: shapes and types are checked here, values in the library.  A cache and a
+batch keep references to their tensors; the tensors' contents may change from step to step.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional
+
+from .binding import InfaasSelError, _AppendArgs, _Batch, _Cache, _stream_ptr, _use_torch, load_library
+
+_TYPES = None        # torch type -> INFAAS_SEL_TYPE_*
+
+
+def _types():
+    global _TYPES
+    if _TYPES is None:
+        torch = _use_torch()
+        _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    return _TYPES
+
+
+def _check(status: int) -> None:
+    if status != 0:
+        lib = load_library()
+        text = lib.infaas_sel_strerror(status).decode()
+        if status in (-1, -4):
+            text += " [" + lib.infaas_sel_last_error().decode() + "]"
+        raise InfaasSelError(status, text)
+
+
+def _vector(t, dtype, name: str, size: Optional[int] = None) -> int:
+    """Raw pointer of a contiguous device tensor of one dimension."""
+    torch = _use_torch()
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or t.dim() != 1 \
+            or (size is not None and t.numel() != size):
+        raise TypeError(f"{name}: contiguous {dtype} device tensor [{'any' if size is None else size}] expected")
+    return t.data_ptr()
+
+
+class PagedCache:
+    """One layer's pools of pages (infaas_sel_cache): ``layout`` "token" for [page][slot][head][dim], "head" for
+    [page][head][slot][dim]; both pools have the same shape and strides, the last dimension consecutive."""
+
+    def __init__(self, k_pool, v_pool, layout: str = "token"):
+        torch = _use_torch()
+        if layout not in ("token", "head"):
+            raise ValueError(f"layout {layout!r}: 'token' or 'head'")
+        if not all(isinstance(p, torch.Tensor) and p.is_cuda and p.dim() == 4 for p in (k_pool, v_pool)):
+            raise TypeError("device tensors of four dimensions expected")
+        if k_pool.dtype not in (torch.bfloat16, torch.float16) or v_pool.dtype != k_pool.dtype \
+                or v_pool.shape != k_pool.shape or v_pool.stride() != k_pool.stride() or k_pool.stride(3) != 1:
+            raise TypeError("pools of one type (bfloat16 or float16), shape and strides expected, the last one 1")
+        slot, head = (1, 2) if layout == "token" else (2, 1)
+        st = k_pool.stride()
+        self.k_pool, self.v_pool, self.layout, self.dtype = k_pool, v_pool, layout, k_pool.dtype
+        self.kv_heads, self.head_dim = k_pool.shape[head], k_pool.shape[3]
+        self.page_size, self.num_pages = k_pool.shape[slot], k_pool.shape[0]
+        self._c = _Cache(d_k=k_pool.data_ptr(), d_v=v_pool.data_ptr(), type=_types()[k_pool.dtype], kv_heads=self.kv_heads,
+                         head_dim=self.head_dim, page_size=self.page_size, num_pages=self.num_pages,
+                         page_stride=st[0], slot_stride=st[slot], head_stride=st[head])
+        self._ref = ctypes.byref(self._c)
+
+
+class Batch:
+    """A step's ragged batch (infaas_sel_batch) with the memory of its plan."""
+
+    def __init__(self, cache: PagedCache, heads: int, *, token_seq, token_pos, seq_start, seq_len, page_table,
+                 group_start=None, shared_len=None, max_len: Optional[int] = None):
+        torch = _use_torch()
+        i32 = torch.int32
+        n, S = token_seq.numel(), seq_len.numel()
+        if (group_start is None) != (shared_len is None):
+            raise TypeError("group_start and shared_len belong together")
+        groups = 0 if shared_len is None else shared_len.numel()
+        if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2 or page_table.shape[0] != S \
+                or page_table.dtype != i32 or not page_table.is_cuda or not page_table.is_contiguous():
+            raise TypeError(f"page_table: contiguous int32 device tensor [{S}, pages] expected")
+        width = page_table.shape[1]
+        self.num_tokens, self.heads = n, heads
+        self._keep = (token_seq, token_pos, seq_start, seq_len, page_table, group_start, shared_len)
+        self._c = _Batch(
+            num_tokens=n, num_seqs=S, num_groups=groups, heads=heads,
+            max_len=min(width * cache.page_size, 0x7fffffff) if max_len is None else max_len, table_width=width,
+            d_token_seq=_vector(token_seq, i32, "token_seq"), d_token_pos=_vector(token_pos, i32, "token_pos", n),
+            d_seq_start=_vector(seq_start, i32, "seq_start", S + 1), d_seq_len=_vector(seq_len, i32, "seq_len"),
+            d_page_table=page_table.data_ptr(),
+            d_group_start=None if not groups else _vector(group_start, i32, "group_start", groups + 1),
+            d_shared_len=None if not groups else _vector(shared_len, i32, "shared_len"))
+        self._ref = ctypes.byref(self._c)
+        self._cache = cache      # what the plan's sizes go by (head counts, head dimension, page size)
+        size = load_library().infaas_sel_exec_plan_bytes(cache._ref, self._ref)
+        if size == 0:
+            _check(-1)
+        self.plan_memory = torch.zeros((size + 3) // 4, dtype=i32, device=token_seq.device)
+        self._c.d_plan, self._c.plan_bytes = self.plan_memory.data_ptr(), size
+
+
+class Executor:
+    """One executor handle of the library (infaas_sel_exec_create ... infaas_sel_exec_destroy)."""
+
+    def __init__(self, device: int = 0):
+        self._h = ctypes.c_void_p()
+        self._lib = load_library()
+        _check(self._lib.infaas_sel_exec_create(device, ctypes.byref(self._h)))
+        self.device = device
+
+    def cache(self, k_pool, v_pool, layout: str = "token") -> PagedCache:
+        return PagedCache(k_pool, v_pool, layout)
+
+    def batch(self, cache: PagedCache, heads: int, **arrays) -> Batch:
+        return Batch(cache, heads, **arrays)
+
+    def reserve(self, cache: PagedCache, batch: Batch) -> None:
+        _check(self._lib.infaas_sel_exec_reserve(self._h, cache._ref, batch._ref))
+
+    def plan(self, batch: Batch, stream=None) -> None:
+        _check(self._lib.infaas_sel_exec_plan(self._h, batch._cache._ref, batch._ref, _stream_ptr(stream)))
+
+    @staticmethod
+    def _rows(t, cache: PagedCache, batch: Batch, heads: int, name: str):
+        """Pointer and strides of a [tokens][heads][head_dim] tensor."""
+        if t.dtype != cache.dtype or not t.is_cuda or t.shape != (batch.num_tokens, heads, cache.head_dim):
+            raise TypeError(f"{name}: {cache.dtype} device tensor [{batch.num_tokens}, {heads}, {cache.head_dim}] expected")
+        a, b, c = t.stride()
+        if c != 1:
+            raise TypeError(f"{name}: the last dimension is not consecutive")
+        # (a dimension of one element has a stride of no meaning)
+        return t.data_ptr(), a if t.shape[0] > 1 else 0, b if heads > 1 else 0
+
+    def append(self, cache: PagedCache, batch: Batch, q, k, v, q_out, freq=None, interleaved: bool = False,
+               stream=None) -> None:
+        """Keys and values into the cache, rotated by the positions; ``freq`` (float64, a frequency per rotated pair) None:
+        not rotated; ``q`` and ``q_out`` both None: no queries."""
+        torch = _use_torch()
+        a = _AppendArgs(interleaved=1 if interleaved else 0)
+        if q is not None:
+            a.d_q, a.q_token_stride, a.q_head_stride = self._rows(q, cache, batch, batch.heads, "q")
+        if q_out is not None:
+            a.d_q_out, a.out_token_stride, a.out_head_stride = self._rows(q_out, cache, batch, batch.heads, "q_out")
+        a.d_k, a.k_token_stride, a.k_head_stride = self._rows(k, cache, batch, cache.kv_heads, "k")
+        a.d_v, a.v_token_stride, a.v_head_stride = self._rows(v, cache, batch, cache.kv_heads, "v")
+        if freq is not None:
+            a.d_freq, a.rot_dim = _vector(freq, torch.float64, "freq"), 2 * freq.numel()
+        _check(self._lib.infaas_sel_exec_append(self._h, cache._ref, batch._ref, ctypes.byref(a), _stream_ptr(stream)))
+
+    def attend(self, cache: PagedCache, batch: Batch, q, out, scale: Optional[float] = None, stream=None) -> None:
+        """Attention of the planned batch's tokens over the cache; ``scale`` None: head_dim ** -0.5."""
+        _check(self._lib.infaas_sel_exec_attend(
+            self._h, cache._ref, batch._ref, *self._rows(q, cache, batch, batch.heads, "q"),
+            *self._rows(out, cache, batch, batch.heads, "out"), cache.head_dim ** -0.5 if scale is None else scale,
+            _stream_ptr(stream)))
+
+    def sample(self, logits, draws, token, prob=None, *, temperature=None, top_k=None, top_p=None, min_p=None,
+               stream=None) -> None:
+        """A token of every row of logits [rows, vocab]; limits are tensors [rows] or None."""
+        torch = _use_torch()
+        if not isinstance(logits, torch.Tensor) or not logits.is_cuda or logits.dim() != 2 or logits.dtype not in _types() \
+                or (logits.shape[1] > 1 and logits.stride(1) != 1):
+            raise TypeError("logits: device tensor [rows, vocab] expected, the last dimension consecutive")
+        rows, vocab = logits.shape
+        f32, i32 = torch.float32, torch.int32
+        limit = lambda t, dtype, name: None if t is None else _vector(t, dtype, name, rows)
+        _check(self._lib.infaas_sel_exec_sample(
+            self._h, rows, vocab, _types()[logits.dtype], logits.data_ptr(), logits.stride(0),
+            limit(temperature, f32, "temperature"), limit(top_k, i32, "top_k"), limit(top_p, f32, "top_p"),
+            limit(min_p, f32, "min_p"), _vector(draws, f32, "draws", rows), _vector(token, i32, "token", rows),
+            limit(prob, f32, "prob"), _stream_ptr(stream)))
+
+    def destroy(self) -> None:
+        if self._h:
+            self._lib.infaas_sel_exec_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass

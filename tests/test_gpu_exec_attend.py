@@ -1,0 +1,344 @@
+"""infaas_sel_exec_plan and _attend against the definition in 64 bits: lengths, groups, head layouts, pages, splits, masks,
+numbers that are none in unused places, plans, streams and graphs."""
+import numpy as np
+import pytest
+import torch
+
+import exec_ref
+from exec_ref import Scene, attend_tolerance
+import paper_1905_13348_amd as pkg
+
+pytestmark = pytest.mark.gpu
+
+
+def _call(ex, sc, scale=None, batch=None, cache=None):
+    cache = ex.cache(sc.k_pool, sc.v_pool, layout=sc.layout) if cache is None else cache
+    batch = sc.batch(ex, cache) if batch is None else batch
+    out = torch.full((sc.n, sc.heads, sc.dim), 7.0, dtype=sc.dtype, device="cuda")
+    ex.plan(batch)
+    ex.attend(cache, batch, sc.q, out, scale)
+    torch.cuda.synchronize()
+    return out.double().cpu().numpy()
+
+
+def _check(sc, scale=None, limits=None, got=None):
+    ex = pkg.Executor()
+    got = _call(ex, sc, scale) if got is None else got
+    want, weighted, top = sc.reference(sc.dim ** -0.5 if scale is None else scale, limits)
+    tol = attend_tolerance(want, weighted, top, sc.dtype, sc.length.max())
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), f"{bad.sum()} of {bad.size} off, first {np.argwhere(bad)[:3].tolist()}, worst {np.nanmax(np.abs(got - want) / tol)}"
+    ex.destroy()
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("layout", ["token", "head"])
+@pytest.mark.parametrize("new", ["one", "some"])
+def test_types_and_layouts(dim, dtype, layout, new):
+    seqs = [(1, 1), (31, 1), (64, 1), (65, 1), (200, 1)] if new == "one" else [(5, 5), (70, 3), (130, 40), (64, 64), (33, 1)]
+    _check(Scene(seqs, dim=dim, dtype=dtype, layout=layout, seed=dim))
+
+
+@pytest.mark.parametrize("length", [1, 2, 15, 16, 17, 32, 33, 63, 64, 127, 128, 129, 255, 256, 257, 511, 513, 1000])
+def test_lengths(length):
+    _check(Scene([(length, 1), (length + 1, 2)], heads=4, kv_heads=1, dim=64, seed=length))
+
+
+@pytest.mark.parametrize("heads, kv", [(1, 1), (2, 2), (3, 1), (8, 1), (16, 1), (17, 1), (40, 8), (64, 2), (128, 1), (60, 4), (36, 12)])
+def test_head_counts(heads, kv):
+    _check(Scene([(50, 1), (130, 9)], heads=heads, kv_heads=kv, dim=64, seed=heads))
+
+
+@pytest.mark.parametrize("page", [1, 2, 8, 32, 128, 1024])
+def test_page_sizes(page):
+    _check(Scene([(100, 1), (300, 2), (7, 7)], page=page, dim=128, layout="head" if page == 8 else "token", joined=page == 32, seed=page))
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("shared", [1, 16, 40, 64, 333])
+def test_shared_prefix(dim, shared):
+    """A group whose prefix ends inside and at the end of pages and tiles; the last sequence has nothing of its own but the
+    prefix's last token."""
+    seqs = [(shared + 30, 1), (shared + 1, 1), (shared + 200, 1), (shared + 77, 1), (shared, 1)]
+    _check(Scene(seqs, groups=[0, 5], shared=[shared], dim=dim, seed=shared))
+
+
+def test_many_in_a_group():
+    """More rows than a tile has, per KV head."""
+    rng = np.random.default_rng(3)
+    seqs = [(300 + int(x), 1) for x in rng.integers(1, 60, 70)]
+    _check(Scene(seqs, groups=[0, 70], shared=[300], heads=8, kv_heads=2, dim=64, seed=4))
+
+
+def test_groups_side_by_side():
+    """Groups of different prefixes, one of them without any, one of a single sequence, one empty."""
+    seqs = [(90, 1), (80, 2), (40, 1), (41, 1), (500, 1), (70, 30), (65, 1)]
+    _check(Scene(seqs, groups=[0, 2, 4, 5, 5, 7], shared=[60, 0, 400, 10, 33], dim=128, dtype=torch.float16, seed=5))
+
+
+def test_groups_that_leave_sequences_out():
+    seqs = [(90, 1), (95, 2), (99, 1), (41, 1)]
+    sc = Scene(seqs, dim=64, seed=6)
+    sc2 = Scene(seqs, groups=[1, 3], shared=[50], dim=64, seed=6)
+    sc2.full = Scene(seqs, groups=[1, 3], shared=[50], dim=64, seed=6).full
+    _check(sc)
+    _check(sc2)
+
+
+def test_prompts_behind_a_prefix():
+    """New tokens that reach back into the shared part (their positions are below its end) and further ones."""
+    seqs = [(150, 100), (140, 20), (130, 2)]
+    _check(Scene(seqs, groups=[0, 3], shared=[120], dim=128, seed=7))
+
+
+def test_a_sequence_shorter_than_its_groups_prefix():
+    sc = Scene([(100, 1), (30, 2), (120, 1)], groups=[0, 3], shared=[64], dim=64, seed=8)
+    _check(sc)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_a_long_sequence_is_split(dim):
+    _check(Scene([(9_001, 1), (3, 1)], heads=4, kv_heads=2, dim=dim, seed=9))
+
+
+def test_many_short_and_one_long():
+    seqs = [(int(x), 1) for x in np.random.default_rng(1).integers(1, 50, 40)] + [(4_000, 3)] + [(600, 200)]
+    _check(Scene(seqs, heads=4, kv_heads=2, dim=128, seed=10))
+
+
+def test_rows_that_see_nothing():
+    """Padding, a length of zero and a sequence without tokens: zeros, and the others as ever."""
+    sc = Scene([(40, 3), (0, 0), (25, 2), (33, 0), (12, 4)], dim=64, seed=11)
+    ex = pkg.Executor()
+    pos, length = sc.pos.copy(), sc.length.copy()
+    pos[1] = -1
+    pos[4] = -5
+    length[4] = 0
+    cache = ex.cache(sc.k_pool, sc.v_pool)
+    got = _call(ex, sc, batch=sc.batch(ex, cache, pos=pos, length=length), cache=cache)
+    limits = sc.limits()
+    for t in range(sc.n):
+        if t in (1, 4) or sc.seq[t] == 4:
+            limits[t] = np.zeros(len(limits[t]), dtype=bool)
+    _check(sc, limits=limits, got=got)
+    assert (got[[1, 4, 5, 6, 7, 8]] == 0).all()
+
+
+def test_padding_behind_a_prefix_sees_nothing():
+    sc = Scene([(90, 1), (95, 1), (99, 1)], groups=[0, 3], shared=[80], dim=128, seed=12)
+    ex = pkg.Executor()
+    cache = ex.cache(sc.k_pool, sc.v_pool)
+    got = _call(ex, sc, batch=sc.batch(ex, cache, pos=np.array([89, -1, 98])), cache=cache)
+    limits = sc.limits()
+    limits[1][:] = False
+    _check(sc, limits=limits, got=got)
+
+
+@pytest.mark.parametrize("bad", [-1, 1 << 30, "pages"])
+@pytest.mark.parametrize("where", ["own", "shared"])
+def test_pages_that_are_not_there(bad, where):
+    """Keys on a page outside the pool are not seen, whoever reads them."""
+    sc = Scene([(200, 1), (210, 2)], groups=[0, 2], shared=[100], dim=64, page=16, seed=13)
+    ex = pkg.Executor()
+    cache = ex.cache(sc.k_pool, sc.v_pool)
+    table = sc.table.copy()
+    at = (0, 2) if where == "shared" else (1, 9)
+    table[at] = sc.k_pool.shape[0] if bad == "pages" else bad
+    got = _call(ex, sc, batch=sc.batch(ex, cache, table=table), cache=cache)
+    limits = sc.limits()
+    for t in range(sc.n):
+        if where == "shared" or sc.seq[t] == 1:
+            limits[t][at[1] * 16:(at[1] + 1) * 16] = False
+    _check(sc, limits=limits, got=got)
+
+
+def test_lengths_beyond_the_bound_and_the_table():
+    """Keys at or beyond max_len, or beyond the table's width, are not seen."""
+    sc = Scene([(200, 1), (90, 1)], dim=64, page=16, seed=14)
+    ex = pkg.Executor()
+    cache = ex.cache(sc.k_pool, sc.v_pool)
+    got = _call(ex, sc, batch=sc.batch(ex, cache, max_len=150), cache=cache)
+    limits = sc.limits()
+    limits[0][150:] = False
+    _check(sc, limits=limits, got=got)
+    got = _call(ex, sc, batch=sc.batch(ex, cache, table=sc.table[:, :8]), cache=cache)
+    limits[0][128:] = False
+    _check(sc, limits=limits, got=got)
+    got = _call(ex, sc, batch=sc.batch(ex, cache, length=np.array([1 << 30, 90]), pos=np.array([1 << 30, 89])), cache=cache)
+    # (what the table names beyond the sequence is there, but NaN: the first row is lost, the second is not)
+    assert np.isnan(got[0]).all() and np.isfinite(got[1]).all()
+
+
+def test_infinities_and_nan_in_masked_places():
+    """Slots behind a sequence's end hold NaN in every other test; here infinities."""
+    for x in (float("inf"), float("-inf")):
+        sc = Scene([(70, 1), (130, 3), (1, 1)], dim=128, seed=15)
+        for p in (sc.k_pool, sc.v_pool):
+            p[torch.isnan(p)] = x
+        _check(sc)
+
+
+def test_large_scores_and_values():
+    """Scores in the thousands (one key takes all) and values near the type's greatest."""
+    sc = Scene([(300, 1), (65, 2)], dim=128, dtype=torch.float16, seed=16)
+    _check(sc, scale=40.0)
+    sc = Scene([(300, 1), (2_000, 2)], dim=64, dtype=torch.float16, seed=17)
+    big = 30000.0 / 4.5
+    sc.v_pool *= big
+    sc.full[1] = [torch.from_numpy(x).to(torch.float16).cuda().mul(big).double().cpu().numpy() for x in sc.full[1]]
+    _check(sc)
+
+
+def test_rising_scores():
+    """Keys that grow along the sequence, so that the running maximum moves in every tile."""
+    sc = Scene([(700, 1), (700, 5)], heads=4, kv_heads=1, dim=64, seed=18)
+    ramp = [np.linspace(0.1, 6, len(x))[:, None, None] for x in sc.full[0]]
+    for s in range(2):
+        sc.full[0][s] = torch.from_numpy(np.abs(sc.full[0][s]) * ramp[s]).to(torch.bfloat16).double().numpy()
+        j = np.arange(700)
+        sc.k_pool[torch.from_numpy(sc.table[s, j // 16]).cuda(), torch.from_numpy(j % 16).cuda()] = \
+            torch.from_numpy(sc.full[0][s]).to(torch.bfloat16).cuda()
+    sc.q = sc.q.abs()
+    sc.q_host = np.abs(sc.q_host)
+    _check(sc, scale=0.5)
+
+
+def test_strided_queries_and_outputs():
+    sc = Scene([(100, 2), (64, 1), (31, 1)], heads=6, kv_heads=2, dim=64, seed=19)
+    ex = pkg.Executor()
+    cache = ex.cache(sc.k_pool, sc.v_pool)
+    batch = sc.batch(ex, cache)
+    wide = torch.zeros((sc.n, 10, 2, 64), dtype=sc.dtype, device="cuda")
+    wide[:, 3:9, 1] = sc.q
+    out = torch.full((8, sc.n, 72), 5.0, dtype=sc.dtype, device="cuda")
+    view = out[1:7, :, :64].transpose(0, 1)
+    ex.plan(batch)
+    ex.attend(cache, batch, wide[:, 3:9, 1], view)
+    torch.cuda.synchronize()
+    _check(sc, got=view.double().cpu().numpy())
+    assert (out[0] == 5).all() and (out[7] == 5).all() and (out[:, :, 64:] == 5).all()
+
+
+def test_a_plan_of_another_batch_gives_nan():
+    sc = Scene([(100, 2), (64, 1)], dim=64, seed=20)
+    ex = pkg.Executor()
+    cache = ex.cache(sc.k_pool, sc.v_pool)
+    batch = sc.batch(ex, cache)
+    out = torch.zeros((sc.n, sc.heads, sc.dim), dtype=sc.dtype, device="cuda")
+    ex.attend(cache, batch, sc.q, out)      # never planned
+    torch.cuda.synchronize()
+    assert torch.isnan(out).all()
+    other = sc.batch(ex, cache, max_len=80)
+    ex.plan(other)
+    batch._c.d_plan = other._c.d_plan
+    ex.attend(cache, batch, sc.q, out)
+    torch.cuda.synchronize()
+    assert torch.isnan(out).all()
+
+
+def test_contradicting_arrays_are_survived():
+    """Starts that fall and overlap, groups out of order, sequences of tokens that are not there: whatever comes out, calls
+    return and what follows is right."""
+    sc = Scene([(100, 2), (64, 1), (80, 3)], groups=[0, 3], shared=[32], dim=64, seed=21)
+    ex = pkg.Executor()
+    cache = ex.cache(sc.k_pool, sc.v_pool)
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")
+    for start, groups, seq in (([6, 0, 6, 0], [0, 3], [0, 0, 1, 2, 2, 2]), ([-5, 100, 2, 1 << 30], [3, 0], [0] * 6),
+                               ([0, 6, 0, 6], [2, 1 << 30], [7, -1, 1 << 30, 0, 1, 2]), ([0, 2, 3, 6], [-9, 9], [2, 2, 2, 0, 0, 1])):
+        batch = ex.batch(cache, sc.heads, token_seq=i32(seq), token_pos=i32(sc.pos), seq_start=i32(start), seq_len=i32(sc.length),
+                         page_table=i32(sc.table), group_start=i32(groups), shared_len=i32([1 << 30]))
+        print(start, groups, seq, flush=True)
+        _call(ex, sc, batch=batch, cache=cache)
+    _check(sc)
+
+
+def test_another_stream_and_two_executors():
+    sc = Scene([(700, 1), (64, 1), (80, 3)], dim=128, seed=22)
+    side = torch.cuda.Stream()
+    a, b = pkg.Executor(), pkg.Executor()
+    cache = a.cache(sc.k_pool, sc.v_pool)
+    batches = [sc.batch(x, cache) for x in (a, b)]
+    outs = [torch.empty((sc.n, sc.heads, sc.dim), dtype=sc.dtype, device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    for x, batch, out, stream in ((a, batches[0], outs[0], side), (b, batches[1], outs[1], torch.cuda.current_stream())):
+        x.plan(batch, stream=stream)
+        x.attend(cache, batch, sc.q, out, stream=stream)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1])
+    _check(sc, got=outs[0].double().cpu().numpy())
+
+
+def test_results_do_not_change_from_call_to_call():
+    sc = Scene([(3_000, 1)] * 3 + [(900, 20)], groups=[0, 4], shared=[500], dim=128, seed=23)
+    ex = pkg.Executor()
+    first = _call(ex, sc)
+    for _ in range(5):
+        assert np.array_equal(_call(ex, sc), first)
+
+
+def test_graph_of_a_step_with_lengths_that_grow():
+    """Plan, append and attend recorded once; every replay is the next step: positions and lengths move on the device, and
+    each replay is compared with an eager run of the same step."""
+    ex = pkg.Executor()
+    S, heads, kv, dim, page = 5, 8, 2, 64, 16
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")
+    pools = [torch.zeros((S * 8, page, kv, dim), dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+    length0 = [20, 33, 64, 17, 50]
+    for p in pools[:2]:
+        p.normal_()
+    for p, src in zip(pools[2:], pools[:2]):
+        p.copy_(src)
+    pos, length = i32([n - 1 for n in length0]), i32(length0)
+    arrays = dict(token_seq=i32(range(S)), seq_start=i32(range(S + 1)), page_table=i32(range(S * 8)).view(S, 8),
+                  group_start=i32([0, 3, 5]), shared_len=i32([16, 0]))
+    cache, eager_cache = ex.cache(*pools[:2]), ex.cache(*pools[2:])
+    batch = ex.batch(cache, heads, token_pos=pos, seq_len=length, **arrays)
+    eager = ex.batch(eager_cache, heads, token_pos=pos, seq_len=length, **arrays)
+    q, k, v = (torch.empty((S, h, dim), dtype=torch.bfloat16, device="cuda") for h in (heads, kv, kv))
+    freq = torch.from_numpy(10000.0 ** (-np.arange(dim // 2) / (dim // 2))).cuda()
+    q_out, out, q_want, want = (torch.empty_like(q) for _ in range(4))
+    ex.reserve(cache, batch)
+
+    def step(c, b, qo, o):
+        ex.plan(b)
+        ex.append(c, b, q, k, v, qo, freq)
+        ex.attend(c, b, qo, o)
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(cache, batch, q_out, out)
+        pos.add_(1)
+        length.add_(1)
+    for i in range(12):
+        for t in (q, k, v):
+            t.normal_(generator=torch.Generator(device="cuda").manual_seed(100 * i + t.shape[1]))
+        step(eager_cache, eager, q_want, want)
+        torch.cuda.synchronize()
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(q_out, q_want), i
+        assert all(torch.equal(x, y) for x, y in zip(pools[:2], pools[2:])), i
+    ex.destroy()
+
+
+def test_growth_under_capture_is_refused():
+    ex = pkg.Executor()
+    sc = Scene([(700, 1)], dim=64, seed=24)
+    cache = ex.cache(sc.k_pool, sc.v_pool)
+    batch = sc.batch(ex, cache)
+    ex.plan(batch)
+    out = torch.empty((sc.n, sc.heads, sc.dim), dtype=sc.dtype, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(pkg.InfaasSelError) as e:
+            ex.attend(cache, batch, sc.q, out)
+        out.zero_()
+    assert e.value.status == -1 and "reserve" in str(e.value)
+    ex.reserve(cache, batch)
+    ex.attend(cache, batch, sc.q, out)
+    torch.cuda.synchronize()
+    _check(sc, got=out.double().cpu().numpy())

@@ -1,0 +1,223 @@
+"""infaas_sel_exec_sample against the definition in 64 bits: limits, ties, masks, borders of the draw, strides."""
+import numpy as np
+import pytest
+import torch
+
+import exec_ref
+import paper_1905_13348_amd as pkg
+
+pytestmark = pytest.mark.gpu
+
+
+def _check(logits, draws, **limits):
+    """All rows of a device tensor; limits are numbers or lists, one to a row."""
+    ex = pkg.Executor()
+    R = logits.shape[0]
+    at = lambda x, r: x[r] if isinstance(x, (list, tuple, np.ndarray)) else x
+    kind = {"temperature": torch.float32, "top_k": torch.int32, "top_p": torch.float32, "min_p": torch.float32}
+    args = {k: torch.tensor([at(v, r) for r in range(R)], dtype=kind[k], device="cuda") for k, v in limits.items()}
+    draws = torch.tensor(np.broadcast_to(draws, (R,)).copy(), dtype=torch.float32, device="cuda")
+    token = torch.full((R,), -9, dtype=torch.int32, device="cuda")
+    prob = torch.full((R,), -9.0, device="cuda")
+    ex.sample(logits, draws, token, prob, **args)
+    alone = torch.full_like(token, -9)
+    ex.sample(logits, draws, alone, **args)
+    torch.cuda.synchronize()
+    rows = logits.double().cpu().numpy()
+    host = {k: v.double().cpu().numpy() for k, v in args.items()}
+    for r in range(R):
+        want, p = exec_ref.sample(rows[r], t=host["temperature"][r] if "temperature" in host else 1.0,
+                                  k=int(host["top_k"][r]) if "top_k" in host else 0,
+                                  top_p=host["top_p"][r] if "top_p" in host else 1.0,
+                                  min_p=host["min_p"][r] if "min_p" in host else 0.0, draw=float(draws[r]))
+        got = int(token[r])
+        assert got == want and int(alone[r]) == want, (r, got, want)
+        # the weights are whole units of 2^-43 and the quotient is rounded to 32 bits once
+        assert abs(float(prob[r]) - p) <= 2.0 ** -24 * p + 2.0 ** -42 + (0 if p else 0), (r, float(prob[r]), p)
+    ex.destroy()
+
+
+def _logits(R, V, dtype=torch.float32, seed=0, spread=2.5):
+    x = torch.randn((R, V), generator=torch.Generator().manual_seed(seed)) * spread
+    few = torch.randint(0, V, (R, min(V, 20)), generator=torch.Generator().manual_seed(seed + 1))
+    x.scatter_add_(1, few, torch.full(few.shape, 6.0) * torch.rand(few.shape, generator=torch.Generator().manual_seed(seed + 2)))
+    return x.to(dtype).cuda()
+
+
+def _draws(R, seed=0):
+    return np.random.default_rng(seed).integers(0, 1 << 24, R) / 2.0 ** 24
+
+
+DTYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [1, 2, 3, 63, 64, 65, 1000, 1023, 1025, 4096, 32_000, 50_001, 131_073])
+def test_vocabularies(V, dtype):
+    R = 6
+    _check(_logits(R, V, dtype, seed=V), _draws(R, V), temperature=0.8, top_k=[0, 1, 5, 40, V, V + 10],
+           top_p=[1.0, 0.9, 0.5, 0.95, 0.999, 0.7], min_p=[0.0, 0.1, 0.0, 0.05, 0.0, 0.2])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("limit", ["none", "top_k", "top_p", "min_p", "all", "greedy"])
+@pytest.mark.parametrize("V", [517, 20_000])
+def test_single_limits(limit, V, dtype):
+    R = 24
+    rng = np.random.default_rng(V)
+    kw = {"temperature": list(rng.uniform(0.3, 2.0, R))}
+    if limit in ("top_k", "all"):
+        kw["top_k"] = [int(x) for x in rng.integers(1, min(V, 900), R)]
+    if limit in ("top_p", "all"):
+        kw["top_p"] = list(rng.uniform(0.05, 0.9999, R))
+    if limit in ("min_p", "all"):
+        kw["min_p"] = list(10 ** rng.uniform(-5, -0.1, R))
+    if limit == "greedy":
+        kw["temperature"] = [0.0, -1.0, float("nan"), -0.0] * (R // 4)
+    _check(_logits(R, V, dtype, seed=V + 1), _draws(R, V + 2), **kw)
+
+
+@pytest.mark.parametrize("k", [1, 2, 255, 256, 257, 1000, 1024, 1025, 3000, 9999])
+def test_top_k_sizes(k):
+    _check(_logits(4, 10_000, torch.float32, seed=k), _draws(4, k), top_k=k, temperature=1.5)
+
+
+def test_no_limits_given():
+    _check(_logits(8, 3_001, seed=4), _draws(8))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_ties(dtype):
+    """Few distinct logits, so that every border runs through equal ones: the lower numbers are kept."""
+    g = torch.Generator().manual_seed(7)
+    x = torch.randint(-2, 3, (12, 5_000), generator=g).to(dtype).cuda()
+    x[:, 100:103] = 3.0
+    _check(x, _draws(12, 8), top_k=[1, 2, 3, 4, 5, 50, 500, 2_000, 0, 0, 0, 0],
+           top_p=[1, 1, 1, 1, 0.5, 0.5, 0.3, 0.9, 0.1, 0.25, 0.5, 0.75], temperature=1.0)
+
+
+def test_all_equal():
+    """Borders that are whole numbers: V tokens of weight 1."""
+    x = torch.zeros((9, 1_024), device="cuda")
+    x[4:] = -7.25
+    _check(x, [0.0, 0.5, 0.25, 1 - 2.0 ** -24, 0.0, 0.5, 511 / 1024, 512 / 1024, 1023 / 1024],
+           top_p=[1.0, 1.0, 0.5, 0.5, 0.25, 0.25, 1.0, 1.0, 1.0])
+    _check(x[:3], [0.0, 0.999, 0.5], top_k=[7, 7, 1])
+
+
+def test_zeros_of_both_signs_are_equal():
+    x = torch.full((3, 200), -1.0, device="cuda")
+    x[:, 3], x[:, 5], x[:, 7] = -0.0, 0.0, -0.0
+    _check(x, [0.0, 0.5, 0.9], top_k=2)
+    _check(x, [0.0, 0.5, 0.9], temperature=0.0)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_masks(dtype):
+    """Tokens masked by -infinity, by the type's lowest value, by NaN; rows of nothing else; +infinities."""
+    low = torch.finfo(dtype).min
+    x = _logits(10, 2_000, dtype, seed=11)
+    x[0, 10:] = float("-inf")
+    x[1, :-1] = float("-inf")
+    x[2] = float("-inf")
+    x[3, 5:] = low
+    x[4] = low
+    x[5, ::2] = float("nan")
+    x[6] = float("nan")
+    x[7, 1234] = float("inf")
+    x[8, [3, 77, 1999]] = float("inf")
+    x[9, :1000] = float("-inf")
+    for kw in (dict(), dict(top_k=50), dict(top_p=0.9), dict(min_p=0.02), dict(top_k=30, top_p=0.8, min_p=0.01), dict(temperature=0.0),
+               dict(temperature=5.0, top_p=0.9999)):
+        _check(x, _draws(10, 12), **kw)
+
+
+def test_extreme_limits():
+    x = _logits(6, 3_000, seed=13)
+    _check(x, _draws(6), temperature=[1e-30, 1e30, 1e-3, 100.0, float("inf"), 1.0])
+    _check(x, _draws(6), top_p=[0.0, -1.0, 1e-9, float("nan"), 2.0, 1 - 2.0 ** -24])
+    _check(x, _draws(6), min_p=[1.0, 1.5, -1.0, float("nan"), 1e-38, 0.0])
+    _check(x, _draws(6), top_k=[-5, 0, 1, 2 ** 31 - 1, 3_000, 2_999])
+
+
+@pytest.mark.parametrize("draw", [0.0, 2.0 ** -24, 0.5, 1 - 2.0 ** -24])
+def test_borders_of_the_draw(draw):
+    _check(_logits(5, 7_001, seed=14), draw, temperature=0.7, top_p=0.9)
+    _check(_logits(5, 7_001, seed=15), draw)
+
+
+def test_draws_out_of_range():
+    """1 and more take the last kept token, below 0 and NaN the first."""
+    x = _logits(1, 500, seed=16)
+    kept = np.sort(np.argsort(-x[0].cpu().numpy(), kind="stable")[:20])
+    ex = pkg.Executor()
+    token = torch.empty(1, dtype=torch.int32, device="cuda")
+    for d, want in ((1.0, kept[-1]), (7.0, kept[-1]), (-0.5, kept[0]), (float("nan"), kept[0])):
+        ex.sample(x, torch.tensor([d], device="cuda"), token, top_k=torch.tensor([20], dtype=torch.int32, device="cuda"))
+        torch.cuda.synchronize()
+        assert int(token[0]) == want, d
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shift", [0, 1, 3, 5])
+def test_strides_and_alignment(shift, dtype):
+    """Rows that start anywhere; what lies between them is not read."""
+    wide = torch.full((7, 4_099 + 16), float("inf"), dtype=dtype, device="cuda")
+    x = wide[:, shift:shift + 4_099]
+    x.copy_(_logits(7, 4_099, dtype, seed=17))
+    _check(x, _draws(7, shift), temperature=0.9, top_k=[0, 10, 0, 300, 0, 40, 7], top_p=[1, 1, 0.9, 0.9, 0.5, 0.99, 1])
+    _check(x[::2], _draws(4, shift))
+
+
+def test_the_largest_vocabulary():
+    _check(_logits(2, 1 << 20, torch.bfloat16, seed=18), _draws(2, 18), top_p=[0.9, 1.0], temperature=0.9)
+    _check(torch.zeros((1, 1 << 20), dtype=torch.float16, device="cuda"), [1 - 2.0 ** -24])
+
+
+def test_many_rows_and_repeats():
+    x = _logits(700, 1_003, torch.bfloat16, seed=19)
+    _check(x, _draws(700, 19), top_p=0.9)
+    ex = pkg.Executor()
+    u = torch.from_numpy(_draws(700, 20).astype(np.float32)).cuda()
+    outs = []
+    for _ in range(4):
+        t = torch.empty(700, dtype=torch.int32, device="cuda")
+        ex.sample(x, u, t)
+        outs.append(t)
+    torch.cuda.synchronize()
+    assert all(torch.equal(outs[0], o) for o in outs)
+
+
+def test_shares_follow_the_weights():
+    """Over a grid of draws each token comes up by its share."""
+    V, R = 50, 4_096
+    row = _logits(1, V, seed=21)
+    x = row.expand(R, V)
+    ex = pkg.Executor()
+    token = torch.empty(R, dtype=torch.int32, device="cuda")
+    ex.sample(x, (torch.arange(R, device="cuda", dtype=torch.float32) + 0.5) / R, token)
+    torch.cuda.synchronize()
+    got = np.bincount(token.cpu().numpy(), minlength=V)
+    want = torch.softmax(row[0].double(), 0).cpu().numpy() * R
+    assert (np.abs(got - want) <= 1).all()       # (a share of so many grid points, one more or less)
+
+
+def test_in_a_graph():
+    x = _logits(9, 2_003, torch.bfloat16, seed=22)
+    u = torch.zeros(9, device="cuda")
+    token, want = (torch.empty(9, dtype=torch.int32, device="cuda") for _ in range(2))
+    p = torch.full((9,), 0.95, device="cuda")
+    ex = pkg.Executor()
+    ex.sample(x, u, want, top_p=p)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ex.sample(x, u, token, top_p=p)
+    for i in range(6):
+        u.copy_(torch.from_numpy(_draws(9, i).astype(np.float32)))
+        x.copy_(_logits(9, 2_003, torch.bfloat16, seed=30 + i))
+        ex.sample(x, u, want, top_p=p)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(token, want), i
