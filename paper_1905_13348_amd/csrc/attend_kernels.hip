@@ -2,6 +2,8 @@
 // the plan, the items and the merge of their results.
 #include "exec.h"
 
+#include <type_traits>
+
 namespace infaas {
 
 namespace {
@@ -195,31 +197,39 @@ template <> struct Mfma<fp16_t> {
 
 // Where the 16-byte piece `c` of row `r` of a staged tile is: rows that the lanes of one LDS instruction read lie in
 // different banks.  Keys are read a row per lane (32 rows, the same piece), values four rows at a time (four pieces).
-template <int CH> __device__ __forceinline__ int key_slot(int r, int c) { return r * CH + (c ^ (CH == 8 ? (r >> 1) & 7 : r & 15)); }
-template <int CH> __device__ __forceinline__ int value_slot(int r, int c) { return r * CH + (c ^ (CH == 8 ? ((r >> 1) & 1) << 2 : (r & 3) << 2)); }
+template <int CH> __device__ __forceinline__ constexpr int key_turn(int r) { return CH == 8 ? (r >> 1) & 7 : r & 15; }
+template <int CH> __device__ __forceinline__ constexpr int value_turn(int r) { return CH == 8 ? ((r >> 1) & 1) << 2 : (r & 3) << 2; }
 
 // exp2 on the hardware's unit: 1 ulp of 32 bits, and 0 for -infinity.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(1))) void global_void;
+
 // A workgroup of four waves takes items of up to 128 rows, 32 to a wave.  With K the A operand, S^T = K Q^T leaves a lane
 // with scores of ONE row (its column), so the running maximum and sum are a lane's own, and P^T is in registers where
 // the B operand of O^T = V^T P^T wants it: key slots of the second product are numbered as the first one leaves them.
-// V^T's rows come from LDS through the transposing read.  Keys and values of a tile go through registers to LDS, the
-// next tile's while this one is computed.
+// V^T's rows come from LDS through the transposing read.  A tile of keys and values is loaded straight into LDS while the
+// one before it is computed; where its rows are (the page table's entries) is looked up two tiles ahead, because the
+// two trips to memory in a row take longer than a tile.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void k_attend_items(AttendArgs a)
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendArgs a)
 {
-    constexpr int KB = D == 256 ? 32 : 64, CH = D / 8, LOADS = KB * CH / 256;
-    __shared__ uint4 lk[2][KB * CH], lv[2][KB * CH];
-    __shared__ int seen[2][KB];
+    constexpr int KB = D == 256 ? 32 : 64, CH = D / 8, LOADS = KB * CH / 256, ROW = D * 2;
+    __shared__ uint4 lk0[KB * CH], lv0[KB * CH], lk1[KB * CH], lv1[KB * CH];
+    __shared__ int64_t where[4][KB];      // of the next tiles' rows, in pieces; -1: not seen
     __shared__ int reach[4];
     if (!plan_fits(a)) return;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 31, half = lane >> 5;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
     const int G = a.batch.heads / a.batch.kv_heads;
     const int n = a.plan.head->num_items;
     const uint32_t inv_g = 65536 / G + 1;          // r / G for r < 128
     const uint4 *kp = (const uint4 *)a.cache.k, *vp = (const uint4 *)a.cache.v;
     const int page_mask = (1 << a.cache.page_shift) - 1;
+    // where a lane reads in a staged tile: pieces of a key by kk, of a value by dt
+    const int key_at = col * ROW + ((half ^ key_turn<CH>(col)) << 4);
+    const int vrow = half * 4 + (lane & 15) / 4;
+    const int value_at = vrow * ROW + (((((lane >> 4) & 1) * 2 + (lane & 3) / 2) ^ value_turn<CH>(vrow)) << 4) + (lane & 1) * 8;
 
     // Workgroups go to the eight dies in turn; each die takes a stretch of the list, so that neighbouring items (the
     // tiles that read the same keys) meet in one L2.
@@ -254,69 +264,80 @@ __global__ __launch_bounds__(256) void k_attend_items(AttendArgs a)
         for (int dt = 0; dt < D / 32; ++dt) o[dt] = vec<float, 16>{};
         float m = -INFINITY, l = 0;
 
-        uint4 rk[LOADS], rv[LOADS];
-        int ok = 0;
-        auto fetch = [&](int kt) {
-            ok = 0;
+        // each wave looks up its quarter of a tile's rows
+        constexpr int MINE = KB / 4;
+        const int32_t *table = a.cache.table + (int64_t)it.seq * a.cache.table_width;
+        auto entry = [&](int kt) {
+            const int key = kt + wave * MINE + lane;
+            const int page = table[min(key, end - 1) >> a.cache.page_shift];      // (no branch: it would wait for the load)
+            return key < end ? page : -1;
+        };
+        auto note = [&](int kt, int64_t page, int slot) {
+            const int key = kt + wave * MINE + lane;
+            if (lane < MINE)
+                where[slot][wave * MINE + lane] = page >= 0 && page < a.cache.num_pages
+                    ? (page * a.cache.page_stride + (int64_t)(key & page_mask) * a.cache.slot_stride + it.head * a.cache.head_stride) / 8 : -1;
+        };
+        auto load = [&](auto buf, int slot) {
+            uint4 *const lk = buf.value ? lk1 : lk0, *const lv = buf.value ? lv1 : lv0;
 #pragma unroll
             for (int x = 0; x < LOADS; ++x) {
-                const int slot = x * 256 + tid, row = slot / CH, c = slot % CH, key = kt + row, near = min(key, end - 1);
-                int64_t page = a.cache.table[(int64_t)it.seq * a.cache.table_width + (near >> a.cache.page_shift)];
-                const bool there = page >= 0 && page < a.cache.num_pages;
-                page = there ? page : 0;
-                const int64_t at = (page * a.cache.page_stride + (int64_t)(near & page_mask) * a.cache.slot_stride + it.head * a.cache.head_stride) / 8 + c;
-                rk[x] = kp[at];
-                rv[x] = vp[at];
-                const bool use = there && key < end;
-                if (!use) rv[x] = uint4{0, 0, 0, 0};     // (whatever is there: it may be no number)
-                ok |= (int)use << x;
+                const int row = (x * 256 + wave * 64 + lane) / CH, c = lane % CH;
+                const int64_t at = max(where[slot][row], (int64_t)0);      // (unseen: any row that is there)
+                __builtin_amdgcn_global_load_lds((global_void *)(kp + at + (c ^ key_turn<CH>(row))), (lds_void *)(lk + x * 256 + wave * 64), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((global_void *)(vp + at + (c ^ value_turn<CH>(row))), (lds_void *)(lv + x * 256 + wave * 64), 16, 0, 0);
             }
         };
-        auto stage = [&](int buf) {
-#pragma unroll
-            for (int x = 0; x < LOADS; ++x) {
-                const int slot = x * 256 + tid, row = slot / CH, c = slot % CH;
-                lk[buf][key_slot<CH>(row, c)] = rk[x];
-                lv[buf][value_slot<CH>(row, c)] = rv[x];
-                if (c == 0) seen[buf][row] = ok >> x & 1;
+        auto compute = [&](auto buf, int kt, int slot) {
+            const char *const lk = (const char *)(buf.value ? lk1 : lk0);
+            const char *const lv = (const char *)(buf.value ? lv1 : lv0);
+            const unsigned long long bits = __ballot(where[slot][lane & (KB - 1)] >= 0);
+            if (bits != ~0ull) {       // values that nothing sees may be no numbers: zeros
+                for (int x = tid; x < KB * CH; x += 256)
+                    if (!(bits >> (x / CH) & 1)) ((uint4 *)lv)[x] = uint4{0, 0, 0, 0};
+                __syncthreads();
             }
-        };
-        if (end > it.k0) {
-            fetch(it.k0);
-            stage(0);
-        }
-        __syncthreads();
-        int buf = 0;
-        for (int kt = it.k0; kt < end; kt += KB, buf ^= 1) {
-            const bool more = kt + KB < end;
-            if (more) fetch(kt + KB);
-            if (kt < hi) {
-                vec<float, 16> s[KB / 32];
+            if (kt >= hi) return;
+            // Thirty-two keys at a time.  What comes from LDS is read a phase ahead: values before the weights are computed,
+            // the next keys before the product with the values.  (Left to itself the compiler reads each operand where it
+            // is used and waits for it there: the barriers keep the phases in order.)
+            int key_from = key_at, value_from = value_at;
+            asm volatile("" : "+v"(key_from), "+v"(value_from));      // (a dozen exclusive-ors a tile instead of as many registers)
+            vec<T, 8> kf[D / 16];
+            auto read_keys = [&](int kb) {
 #pragma unroll
-                for (int kb = 0; kb < KB / 32; ++kb) {
-                    s[kb] = vec<float, 16>{};
+                for (int kk = 0; kk < D / 16; ++kk) kf[kk] = *(const vec<T, 8> *)(lk + (key_from ^ (kk << 5)) + kb * 32 * ROW);
+            };
+            read_keys(0);
 #pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk) {
-                        const vec<T, 8> k = *(const vec<T, 8> *)&lk[buf][key_slot<CH>(kb * 32 + col, kk * 2 + half)];
-                        s[kb] = Mfma<T>::run(k, q[kk], s[kb]);
+            for (int kb = 0; kb < KB / 32; ++kb) {
+                vec<float, 16> s = vec<float, 16>{};
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk) s = Mfma<T>::run(kf[kk], q[kk], s);
+                union { vec<short, 4> h[2]; vec<T, 8> v; } vf[D / 32][2];
+#pragma unroll
+                for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        const char *at = lv + (value_from ^ (dt << 6)) + (kb * 2 + g) * 16 * ROW;
+                        vf[dt][g].h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)at);
+                        vf[dt][g].h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(at + 8 * ROW));
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+                if (kt + KB > lo || bits != ~0ull) {
+                    const int left = lim - kt - kb * 32 - 4 * half;          // (rows counted from the lane's first)
+                    const uint32_t b = (uint32_t)(bits >> (kb * 32 + 4 * half));
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        const int row = 8 * (x / 4) + x % 4;
+                        const bool vis = row < left && (b & 1u << row);
+                        s[x] = vis ? s[x] : -INFINITY;
                     }
                 }
-                const unsigned long long bits = __ballot(seen[buf][lane & (KB - 1)] != 0);
-                if (kt + KB > lo || bits != ~0ull) {
+                float top = s[0];
 #pragma unroll
-                    for (int kb = 0; kb < KB / 32; ++kb)
-#pragma unroll
-                        for (int x = 0; x < 16; ++x) {
-                            const int row = kb * 32 + 8 * (x / 4) + 4 * half + x % 4;
-                            const bool vis = kt + row < lim && (bits >> row & 1);
-                            s[kb][x] = vis ? s[kb][x] : -INFINITY;
-                        }
-                }
-                float top = s[0][0];
-#pragma unroll
-                for (int kb = 0; kb < KB / 32; ++kb)
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) top = fmaxf(top, s[kb][x]);
+                for (int x = 1; x < 16; ++x) top = fmaxf(top, s[x]);
                 top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
                 if (__any(top > m)) {
                     const float m2 = fmaxf(m, top);
@@ -327,32 +348,46 @@ __global__ __launch_bounds__(256) void k_attend_items(AttendArgs a)
                     for (int dt = 0; dt < D / 32; ++dt) o[dt] *= f;
                 }
                 const float ref = m == -INFINITY ? 0.0f : m;      // (a row that has seen nothing yet)
-                vec<T, 8> pt[KB / 16];
+                vec<T, 8> pt[2];
 #pragma unroll
-                for (int kb = 0; kb < KB / 32; ++kb)
+                for (int x = 0; x < 16; x += 2) {
+                    const vec<float, 2> e = {exp2_fast(s[x] * a.scale_log2 - ref), exp2_fast(s[x + 1] * a.scale_log2 - ref)};
+                    l += e[0];
+                    l += e[1];
+                    const vec<T, 2> y = __builtin_convertvector(e, vec<T, 2>);
+                    pt[x / 8][x % 8] = y[0];
+                    pt[x / 8][x % 8 + 1] = y[1];
+                }
+                if (kb + 1 < KB / 32) read_keys(kb + 1);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        const float e = exp2_fast(s[kb][x] * a.scale_log2 - ref);
-                        l += e;
-                        pt[kb * 2 + x / 8][x % 8] = (T)e;
-                    }
-                const int j = lane & 15, quarter = (lane >> 4) & 1;
+                for (int g = 0; g < 2; ++g)
 #pragma unroll
-                for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-                    for (int g = 0; g < KB / 16; ++g) {
-                        const int row = g * 16 + half * 4 + j / 4, c = dt * 4 + quarter * 2 + (j & 3) / 2;
-                        const short *at0 = (const short *)&lv[buf][value_slot<CH>(row, c)] + (j & 1) * 4;
-                        const short *at1 = (const short *)&lv[buf][value_slot<CH>(row + 8, c)] + (j & 1) * 4;
-                        union { vec<short, 4> h[2]; vec<T, 8> v; } v;
-                        v.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)at0);
-                        v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)at1);
-                        o[dt] = Mfma<T>::run(v.v, pt[g], o[dt]);
-                    }
+                    for (int dt = 0; dt < D / 32; ++dt) o[dt] = Mfma<T>::run(vf[dt][g].v, pt[g], o[dt]);
             }
-            if (more) stage(buf ^ 1);
+        };
+        if (end > it.k0) {
+            note(it.k0, entry(it.k0), 0);
+            note(it.k0 + KB, entry(it.k0 + KB), 1);
             __syncthreads();
+            load(std::integral_constant<int, 0>(), 0);
         }
+        for (int kt = it.k0, t = 0; kt < end; kt += KB, ++t) {
+            auto tile = [&](auto buf) {
+                __builtin_amdgcn_s_waitcnt(0x0f70);       // this tile is there
+                __syncthreads();
+                const int e = entry(kt + 2 * KB);
+                load(std::integral_constant<int, 1 - buf.value>(), (t + 1) & 3);      // (behind the last tile: any row)
+                compute(buf, kt, t & 3);
+                note(kt + 2 * KB, e, (t + 2) & 3);
+            };
+            tile(std::integral_constant<int, 0>());
+            kt += KB;
+            ++t;
+            if (kt >= end) break;
+            tile(std::integral_constant<int, 1>());
+        }
+        __builtin_amdgcn_s_waitcnt(0x0f70);       // (nothing is under way to LDS when the next item or the end comes)
 
         l += __shfl_xor(l, 32);
         if (valid && it.base < 0) {
