@@ -14,7 +14,7 @@ constexpr int kPlanThreads = 1024;
 
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
 
-// What unit u (a sequence, or behind those a group) has to have computed: its tokens and keys.
+// What unit u (a group, or behind those a sequence) has to have computed: its tokens and keys.
 struct UnitRange { int t0, nt, k0, k1, seq; };
 
 __device__ __forceinline__ int seq_limit(const BatchArgs &b, const CacheArgs &c, int s) { return clampi(b.seq_len[s], 0, c.max_len); }
@@ -39,14 +39,15 @@ __device__ __forceinline__ int shared_of(const BatchArgs &b, const CacheArgs &c,
 __device__ __forceinline__ UnitRange unit_range(const BatchArgs &b, const CacheArgs &c, int u)
 {
     UnitRange r;
-    if (u < b.num_seqs) {
-        r.seq = u;
-        r.t0 = clampi(b.seq_start[u], 0, b.num_tokens);
-        r.nt = clampi(b.seq_start[u + 1], r.t0, b.num_tokens) - r.t0;
-        r.k1 = seq_limit(b, c, u);
-        r.k0 = min(shared_of(b, c, group_of(b, u)), r.k1);
+    if (u >= b.num_groups) {
+        const int s = u - b.num_groups;
+        r.seq = s;
+        r.t0 = clampi(b.seq_start[s], 0, b.num_tokens);
+        r.nt = clampi(b.seq_start[s + 1], r.t0, b.num_tokens) - r.t0;
+        r.k1 = seq_limit(b, c, s);
+        r.k0 = min(shared_of(b, c, group_of(b, s)), r.k1);
     } else {
-        const int g = u - b.num_seqs;
+        const int g = u;
         const int a = clampi(b.group_start[g], 0, b.num_seqs), e = clampi(b.group_start[g + 1], a, b.num_seqs);
         r.seq = a < b.num_seqs ? a : 0;
         r.t0 = clampi(b.seq_start[a], 0, b.num_tokens);
@@ -62,10 +63,10 @@ __device__ __forceinline__ UnitRange unit_range(const BatchArgs &b, const CacheA
 __global__ __launch_bounds__(kPlanThreads) void k_plan(BatchArgs b, CacheArgs c, PlanView p, int max_items, int max_rows)
 {
     __shared__ unsigned long long cost;
-    __shared__ long long scan[2][kPlanThreads / 64];
-    __shared__ long long totals[2];
+    __shared__ long long scan[3][kPlanThreads / 64];
+    __shared__ long long totals[3];
     const int tid = threadIdx.x, G = b.heads / b.kv_heads, per_tile = kTileRows / G, units = b.num_seqs + b.num_groups;
-    if (tid == 0) { cost = 0; totals[0] = totals[1] = 0; }
+    if (tid == 0) { cost = 0; totals[0] = totals[1] = totals[2] = 0; }
     __syncthreads();
     unsigned long long mine = 0;
     for (int u = tid; u < units; u += kPlanThreads) {
@@ -78,10 +79,10 @@ __global__ __launch_bounds__(kPlanThreads) void k_plan(BatchArgs b, CacheArgs c,
     const int chunk = each > 0x7fffff00ull ? 0x7fffff00
                                            : max(kMinChunk, (int)((each + kChunkStep - 1) / kChunkStep) * kChunkStep);
 
-    // first item and first row of every unit: a running sum over blocks of units
+    // first item, first row and cost in front of every unit: running sums over blocks of units
     for (int u0 = 0; u0 < units; u0 += kPlanThreads) {
         const int u = u0 + tid;
-        long long items = 0, rows = 0;
+        long long items = 0, rows = 0, costs = 0;
         PlanUnit pu{};
         if (u < units) {
             const UnitRange r = unit_range(b, c, u);
@@ -89,32 +90,54 @@ __global__ __launch_bounds__(kPlanThreads) void k_plan(BatchArgs b, CacheArgs c,
             pu.splits = r.nt > 0 ? (int)(((int64_t)(r.k1 - r.k0) + chunk - 1) / chunk) : 0;
             items = (long long)pu.tiles * pu.splits;
             rows = (long long)r.nt * G * pu.splits;
+            pu.cost = min(chunk, r.k1 - r.k0) + kItemCost;
+            costs = items * pu.cost;
         }
-        long long si = items, sr = rows;
+        long long si = items, sr = rows, sc = costs;
         for (int d = 1; d < 64; d <<= 1) {
-            const long long ai = __shfl_up(si, d), ar = __shfl_up(sr, d);
-            if ((tid & 63) >= d) { si += ai; sr += ar; }
+            const long long ai = __shfl_up(si, d), ar = __shfl_up(sr, d), ac = __shfl_up(sc, d);
+            if ((tid & 63) >= d) { si += ai; sr += ar; sc += ac; }
         }
-        if ((tid & 63) == 63) { scan[0][tid >> 6] = si; scan[1][tid >> 6] = sr; }
+        if ((tid & 63) == 63) { scan[0][tid >> 6] = si; scan[1][tid >> 6] = sr; scan[2][tid >> 6] = sc; }
         __syncthreads();
-        long long bi = totals[0], br = totals[1];
-        for (int w = 0; w < (tid >> 6); ++w) { bi += scan[0][w]; br += scan[1][w]; }
+        long long bi = totals[0], br = totals[1], bc = totals[2];
+        for (int w = 0; w < (tid >> 6); ++w) { bi += scan[0][w]; br += scan[1][w]; bc += scan[2][w]; }
         if (u < units) {
             pu.first_item = (int)(bi + si - items);
             pu.first_row = (int)(br + sr - rows);
+            pu.first_cost = bc + sc - costs;
             p.units[u] = pu;
         }
         __syncthreads();
-        if (tid == kPlanThreads - 1) { totals[0] = bi + si; totals[1] = br + sr; }
+        if (tid == kPlanThreads - 1) { totals[0] = bi + si; totals[1] = br + sr; totals[2] = bc + sc; }
         __syncthreads();
     }
-    __threadfence_block();
     // (arrays that contradict each other, like starts that fall, can ask for more than there is room for)
     const bool fits = totals[0] * b.kv_heads <= max_items && totals[1] <= max_rows;
     const int n = fits ? (int)totals[0] * b.kv_heads : 0, rows1 = fits ? (int)totals[1] : 0;
-    if (tid == 0)
-        *p.head = PlanHeader{kPlanMagic, b.num_tokens, b.num_seqs, b.num_groups, b.heads, b.kv_heads, b.head_dim,
-                             c.max_len, c.table_width, c.page_shift, n, rows1, {0}};
+    if (tid == 0) {
+        PlanHeader &h = *p.head;
+        h.magic = kPlanMagic;
+        h.num_tokens = b.num_tokens; h.num_seqs = b.num_seqs; h.num_groups = b.num_groups;
+        h.heads = b.heads; h.kv_heads = b.kv_heads; h.head_dim = b.head_dim;
+        h.max_len = c.max_len; h.table_width = c.table_width; h.page_shift = c.page_shift;
+        h.num_items = n; h.rows = rows1;
+    }
+    if (tid <= kDies) {      // the item at which so many eighths of the cost are reached
+        int at = n;
+        if (n > 0 && tid < kDies) {
+            const long long want = totals[2] * b.kv_heads / kDies * tid;
+            int lo = 0, hi = units - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) / 2;
+                if (p.units[mid].first_cost * b.kv_heads <= want) lo = mid;
+                else hi = mid - 1;
+            }
+            const PlanUnit pu = p.units[lo];
+            at = pu.first_item * b.kv_heads + (pu.cost > 0 ? (int)((want - pu.first_cost * b.kv_heads) / pu.cost) : 0);
+        }
+        p.head->die_start[tid] = min(at, n);
+    }
 
     for (int i = tid; i < n; i += kPlanThreads) {
         int lo = 0, hi = units - 1;      // the last unit that starts at or before item i (units without items share a start)
@@ -134,7 +157,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_plan(BatchArgs b, CacheArgs c,
         it.k1 = (int)min((int64_t)it.k0 + chunk, (int64_t)r.k1);
         it.seq = r.seq;
         it.head = head;
-        const bool direct = lo < b.num_seqs && pu.splits == 1 && r.k0 == 0;
+        const bool direct = lo >= b.num_groups && pu.splits == 1 && r.k0 == 0;
         it.base = direct ? -1 : head * rows1 + pu.first_row + (split * r.nt + tile * per_tile) * G;
         p.items[i] = it;
     }
@@ -143,9 +166,9 @@ __global__ __launch_bounds__(kPlanThreads) void k_plan(BatchArgs b, CacheArgs c,
         PlanToken pt{};
         const int s = b.token_seq[t];
         if (fits && (uint32_t)s < (uint32_t)b.num_seqs) {
-            const UnitRange r = unit_range(b, c, s);
+            const UnitRange r = unit_range(b, c, b.num_groups + s);
             if (t >= r.t0 && t < r.t0 + r.nt) {
-                const PlanUnit pu = p.units[s];
+                const PlanUnit pu = p.units[b.num_groups + s];
                 pt.limit = clampi(b.token_pos[t], -1, r.k1 - 1) + 1;
                 pt.own_splits = pu.splits;
                 pt.own_stride = r.nt * G;
@@ -153,8 +176,8 @@ __global__ __launch_bounds__(kPlanThreads) void k_plan(BatchArgs b, CacheArgs c,
                 pt.direct = pu.splits == 1 && r.k0 == 0;
                 const int g = group_of(b, s);
                 if (g >= 0) {
-                    const UnitRange q = unit_range(b, c, b.num_seqs + g);
-                    const PlanUnit qu = p.units[b.num_seqs + g];
+                    const UnitRange q = unit_range(b, c, g);
+                    const PlanUnit qu = p.units[g];
                     if (t >= q.t0 && t < q.t0 + q.nt) {
                         pt.pre_splits = qu.splits;
                         pt.pre_stride = q.nt * G;
@@ -203,6 +226,15 @@ template <int CH> __device__ __forceinline__ constexpr int value_turn(int r) { r
 // exp2 on the hardware's unit: 1 ulp of 32 bits, and 0 for -infinity.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// The greater of a lane's value and that of the lane 32 away.  (Swapping the upper half of one copy with the lower half of
+// another leaves both values in the two of every lane.)
+__device__ __forceinline__ float max_of_halves(float x)
+{
+    const uint32_t v = __float_as_uint(x);
+    const auto y = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) void global_void;
 
@@ -222,7 +254,6 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
     if (!plan_fits(a)) return;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
     const int G = a.batch.heads / a.batch.kv_heads;
-    const int n = a.plan.head->num_items;
     const uint32_t inv_g = 65536 / G + 1;          // r / G for r < 128
     const uint4 *kp = (const uint4 *)a.cache.k, *vp = (const uint4 *)a.cache.v;
     const int page_mask = (1 << a.cache.page_shift) - 1;
@@ -231,12 +262,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
     const int vrow = half * 4 + (lane & 15) / 4;
     const int value_at = vrow * ROW + (((((lane >> 4) & 1) * 2 + (lane & 3) / 2) ^ value_turn<CH>(vrow)) << 4) + (lane & 1) * 8;
 
-    // Workgroups go to the eight dies in turn; each die takes a stretch of the list, so that neighbouring items (the
-    // tiles that read the same keys) meet in one L2.
-    const int die = blockIdx.x & 7, dies = min((int)gridDim.x, 8);
-    const int from = (int)((int64_t)n * die / dies), to = (int)((int64_t)n * (die + 1) / dies);
-    const int step = ((int)gridDim.x - die + 7) / 8;
-    for (int i = from + (int)(blockIdx.x >> 3); i < to; i += step) {
+    // Workgroups go to the dies in turn; each die takes a stretch of the list, so that neighbouring items (the tiles that
+    // read the same keys) meet in one L2.  Stretches are of equal cost: of equal numbers of items, the dies with the
+    // sequences' own parts were done in half the time of those with the long prefixes.
+    const int die = blockIdx.x & (kDies - 1), to = a.plan.head->die_start[die + 1], step = gridDim.x / kDies;
+    for (int i = a.plan.head->die_start[die] + (int)(blockIdx.x / kDies); i < to; i += step) {
         const PlanItem it = a.plan.items[i];
         const int rows = it.nt * G;
         const int r = wave * 32 + col;
@@ -338,7 +368,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
                 float top = s[0];
 #pragma unroll
                 for (int x = 1; x < 16; ++x) top = fmaxf(top, s[x]);
-                top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
+                top = max_of_halves(top) * a.scale_log2;
                 if (__any(top > m)) {
                     const float m2 = fmaxf(m, top);
                     const float f = m2 == -INFINITY ? 1.0f : exp2_fast(m - m2);
@@ -417,59 +447,65 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
 
 // ---- merge ------------------------------------------------------------------------------------
 
-// A workgroup per (token, query head): D/4 threads side by side take four dimensions each, the others further splits.
-template <typename T, int D>
+// D/4 threads side by side take four dimensions of a (token, query head) each.  A workgroup takes ROWS of those; the
+// threads that are left over take further splits, merged through LDS at the end.  One row to a workgroup for few rows
+// (which may have a hundred splits each), as many as fit for many: 80,000 rows of three splits 145 us with one row each.
+template <typename T, int D, int ROWS>
 __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a)
 {
-    constexpr int W = D / 4, LANES = 256 / W;
-    __shared__ float lm[LANES], ll[LANES];
-    __shared__ vec<float, 4> lo[LANES][W];
-    const int token = blockIdx.x / a.batch.heads, head = blockIdx.x % a.batch.heads;
-    const int d = threadIdx.x % W, lane = threadIdx.x / W;
+    constexpr int W = D / 4, LANES = 256 / W / ROWS;
+    __shared__ float lm[ROWS][LANES], ll[ROWS][LANES];
+    __shared__ vec<float, 4> lo[LANES > 1 ? ROWS * LANES : 1][W];
+    const int sub = threadIdx.x / (W * LANES), d = threadIdx.x % W, lane = threadIdx.x / W % LANES;
+    const int64_t item = (int64_t)blockIdx.x * ROWS + sub;
+    const bool there = item < (int64_t)a.batch.num_tokens * a.batch.heads;
+    const int token = there ? (int)(item / a.batch.heads) : 0, head = there ? (int)(item % a.batch.heads) : 0;
     T *out = (T *)a.out + token * a.out_token_stride + head * a.out_head_stride + d * 4;
     if (!plan_fits(a)) {
-        if (lane == 0) *(vec<T, 4> *)out = vec<T, 4>{(T)NAN, (T)NAN, (T)NAN, (T)NAN};
+        if (there && lane == 0) *(vec<T, 4> *)out = vec<T, 4>{(T)NAN, (T)NAN, (T)NAN, (T)NAN};
         return;
     }
     const PlanToken pt = a.plan.tokens[token];
-    if (pt.direct) return;
     const int G = a.batch.heads / a.batch.kv_heads;
     const int64_t first = (int64_t)(head / G) * a.plan.head->rows + head % G;
+    const bool work = there && !pt.direct;
     float m = -INFINITY, l = 0;
     vec<float, 4> o = vec<float, 4>{};
-    for (int s = lane; s < pt.own_splits + pt.pre_splits; s += LANES) {
-        const int64_t row = first + (s < pt.pre_splits ? pt.pre_base + (int64_t)s * pt.pre_stride
-                                                       : pt.own_base + (int64_t)(s - pt.pre_splits) * pt.own_stride);
-        const float2 ml = a.part_ml[row];
-        const vec<float, 4> x = *(const vec<float, 4> *)(a.part_o + row * D + d * 4);
-        if (ml.x == -INFINITY && ml.y == 0) continue;        // nothing seen
-        const float m2 = fmaxf(m, ml.x), f = exp2_fast(m - m2), g = exp2_fast(ml.x - m2);
-        o = m == -INFINITY ? x * g : o * f + x * g;
-        l = m == -INFINITY ? ml.y * g : l * f + ml.y * g;
+    auto join = [&](float m1, float l1, vec<float, 4> o1) {
+        if (m1 == -INFINITY && l1 == 0) return;        // nothing seen
+        const float m2 = fmaxf(m, m1), f = exp2_fast(m - m2), g = exp2_fast(m1 - m2);
+        o = m == -INFINITY ? o1 * g : o * f + o1 * g;
+        l = m == -INFINITY ? l1 * g : l * f + l1 * g;
         m = m2;
-    }
-    if (d == 0) { lm[lane] = m; ll[lane] = l; }
-    lo[lane][d] = o;
-    __syncthreads();
-    if (lane != 0) return;
-    for (int s = 1; s < LANES; ++s) {
-        if (lm[s] == -INFINITY && ll[s] == 0) continue;
-        const float m2 = fmaxf(m, lm[s]), f = exp2_fast(m - m2), g = exp2_fast(lm[s] - m2);
-        o = m == -INFINITY ? lo[s][d] * g : o * f + lo[s][d] * g;
-        l = m == -INFINITY ? ll[s] * g : l * f + ll[s] * g;
-        m = m2;
+    };
+    if (work)
+        for (int s = lane; s < pt.own_splits + pt.pre_splits; s += LANES) {
+            const int64_t row = first + (s < pt.pre_splits ? pt.pre_base + (int64_t)s * pt.pre_stride
+                                                           : pt.own_base + (int64_t)(s - pt.pre_splits) * pt.own_stride);
+            const float2 ml = a.part_ml[row];
+            join(ml.x, ml.y, *(const vec<float, 4> *)(a.part_o + row * D + d * 4));
+        }
+    if (LANES > 1) {
+        if (d == 0) { lm[sub][lane] = m; ll[sub][lane] = l; }
+        lo[sub * LANES + lane][d] = o;
+        __syncthreads();
+        if (lane != 0) return;
+        for (int s = 1; s < LANES; ++s) join(lm[sub][s], ll[sub][s], lo[sub * LANES + s][d]);
     }
     const float f = l > 0 ? 1.0f / l : (l == 0 ? 0.0f : l);
-    *(vec<T, 4> *)out = vec<T, 4>{(T)(o[0] * f), (T)(o[1] * f), (T)(o[2] * f), (T)(o[3] * f)};
+    if (work) *(vec<T, 4> *)out = vec<T, 4>{(T)(o[0] * f), (T)(o[1] * f), (T)(o[2] * f), (T)(o[3] * f)};
 }
 
 template <typename T, int D>
 hipError_t attend(const AttendArgs &a, int64_t max_items, hipStream_t s)
 {
-    const int grid = (int)(max_items < 2048 ? max_items : 2048);
+    const int grid = (int)(max_items < 2048 ? max_items : 2048) / kDies * kDies;
     k_attend_items<T, D><<<grid, 256, 0, s>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
-    k_attend_merge<T, D><<<(unsigned)a.batch.num_tokens * a.batch.heads, 256, 0, s>>>(a);
+    const unsigned rows = (unsigned)a.batch.num_tokens * a.batch.heads;
+    constexpr int MANY = 256 / (D / 4);
+    if (rows < 2048) k_attend_merge<T, D, 1><<<rows, 256, 0, s>>>(a);
+    else k_attend_merge<T, D, MANY><<<(rows + MANY - 1) / MANY, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 

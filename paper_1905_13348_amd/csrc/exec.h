@@ -24,15 +24,20 @@ constexpr int kTargetItems = 1024;
 constexpr int kMinChunk = 256;       // keys of an item, at least: below, the merge costs more than the split gains
 constexpr int kChunkStep = 64;
 
+constexpr int kDies = 8;             // workgroups go to the dies in turn, each with an L2 of its own
+// What an item costs besides its keys (queries, first loads, results), in keys.
+constexpr int kItemCost = 128;
+
 struct PlanHeader {
     uint32_t magic;
     int32_t num_tokens, num_seqs, num_groups, heads, kv_heads, head_dim;
     int32_t max_len, table_width, page_shift;
     int32_t num_items;               // over all KV heads
     int32_t rows;                    // partial rows of one KV head
-    int32_t pad[4];
+    int32_t die_start[kDies + 1];    // items of each die: stretches of equal cost
+    int32_t pad[11];
 };
-static_assert(sizeof(PlanHeader) == 64, "");
+static_assert(sizeof(PlanHeader) == 128, "");
 constexpr uint32_t kPlanMagic = 0x1f5e9a7du;
 
 // One workgroup's work: the tokens t0 .. t0+nt-1 for one KV head and the keys k0 .. k1-1 in the pages of one sequence.
@@ -51,10 +56,12 @@ struct PlanToken {
     int32_t direct;                  // the result is written by the only item there is
 };
 
-// Sequences, then groups, as the plan divides them.
+// Groups, then sequences, as the plan divides them: the longest items come first.
 struct PlanUnit {
-    int32_t first_item, first_row;   // of one KV head
+    int64_t first_cost;              // of what is in front of it, of one KV head
+    int32_t first_item, first_row;   // the same
     int32_t splits, tiles;
+    int64_t cost;                    // of one of its items
 };
 
 struct PlanSizes {
