@@ -478,13 +478,27 @@ __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a)
         l = m == -INFINITY ? l1 * g : l * f + l1 * g;
         m = m2;
     };
-    if (work)
-        for (int s = lane; s < pt.own_splits + pt.pre_splits; s += LANES) {
-            const int64_t row = first + (s < pt.pre_splits ? pt.pre_base + (int64_t)s * pt.pre_stride
-                                                           : pt.own_base + (int64_t)(s - pt.pre_splits) * pt.own_stride);
-            const float2 ml = a.part_ml[row];
-            join(ml.x, ml.y, *(const vec<float, 4> *)(a.part_o + row * D + d * 4));
+    if (work) {
+        const int splits = pt.own_splits + pt.pre_splits;
+        auto row_of = [&](int s) {
+            return first + (s < pt.pre_splits ? pt.pre_base + (int64_t)s * pt.pre_stride
+                                              : pt.own_base + (int64_t)(s - pt.pre_splits) * pt.own_stride);
+        };
+        constexpr int AHEAD = 4;      // splits under way at a time
+        for (int s0 = lane; s0 < splits; s0 += AHEAD * LANES) {
+            float2 ml[AHEAD];
+            vec<float, 4> x[AHEAD];
+#pragma unroll
+            for (int e = 0; e < AHEAD; ++e) {
+                const int s = s0 + e * LANES;
+                const int64_t row = row_of(s < splits ? s : s0);
+                ml[e] = s < splits ? a.part_ml[row] : float2{-INFINITY, 0};
+                x[e] = *(const vec<float, 4> *)(a.part_o + row * D + d * 4);
+            }
+#pragma unroll
+            for (int e = 0; e < AHEAD; ++e) join(ml[e].x, ml[e].y, x[e]);
         }
+    }
     if (LANES > 1) {
         if (d == 0) { lm[sub][lane] = m; ll[sub][lane] = l; }
         lo[sub * LANES + lane][d] = o;
@@ -504,7 +518,7 @@ hipError_t attend(const AttendArgs &a, int64_t max_items, hipStream_t s)
     if (hipError_t e = hipGetLastError()) return e;
     const unsigned rows = (unsigned)a.batch.num_tokens * a.batch.heads;
     constexpr int MANY = 256 / (D / 4);
-    if (rows < 2048) k_attend_merge<T, D, 1><<<rows, 256, 0, s>>>(a);
+    if (rows < 32768) k_attend_merge<T, D, 1><<<rows, 256, 0, s>>>(a);
     else k_attend_merge<T, D, MANY><<<(rows + MANY - 1) / MANY, 256, 0, s>>>(a);
     return hipGetLastError();
 }

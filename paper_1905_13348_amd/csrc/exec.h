@@ -20,7 +20,10 @@ template <typename T, int N> using vec = T __attribute__((ext_vector_type(N)));
 constexpr int kTileRows = 128;
 // Items that a plan aims at: two to each of the two workgroups that a compute unit holds, so that the end of one
 // launch is a quarter of a workgroup's time at most.
-constexpr int kTargetItems = 1024;
+#ifndef TGT
+#define TGT 1024
+#endif
+constexpr int kTargetItems = TGT;
 constexpr int kMinChunk = 256;       // keys of an item, at least: below, the merge costs more than the split gains
 constexpr int kChunkStep = 64;
 

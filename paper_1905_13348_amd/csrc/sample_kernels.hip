@@ -6,9 +6,13 @@ namespace infaas {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kSegments = 2048;              // stretches of a row whose sums are kept for the draw
+constexpr int kMostSegments = 4352;          // of a row: 2^20 logits of 32 bits at any alignment are 4112
+constexpr int kMostListed = 2048;            // candidates that are put in order in LDS, two to a thread
+constexpr int kBuckets = 2048;               // of logits by their distance from the greatest
 constexpr int kShift = 43;                   // a weight of 1 is 2^43: 2^20 of them stay below 2^63
+constexpr float kFar = 44.0f;                // in halvings: weights further down are 0 units
 constexpr uint32_t kNever = 0x007fffffu;     // order key of -infinity
+constexpr int kLastIndex = 0x7fffffff;
 
 typedef unsigned long long u64;
 
@@ -21,25 +25,34 @@ __device__ __forceinline__ uint32_t key_of(float x)
 }
 __device__ __forceinline__ float value_of(uint32_t k) { return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k); }
 
-template <typename T> __device__ __forceinline__ uint32_t load_key(const T *row, int i) { return key_of((float)row[i]); }
-
-// exp((x - top) / temperature) in 64 bits; among +infinities 1.
+// Weights exp((x - top) / temperature) in units of 2^-43: 2^t, t = (x - top) * log2(e) / temperature, as 2^round(t) times
+// the Taylor series of 2^f = e^(f ln 2), |f| <= 1/2, to the eleventh power: what is left out is 0.347^12 / 12! = 6e-15 of
+// it, less than the rounding to units.  Among +infinities 1.
 struct Weights {
-    double top, per_t;
+    double top, halvings;
     bool infinite;
-    __device__ __forceinline__ double real(uint32_t k) const
+    __device__ __forceinline__ u64 operator()(uint32_t k) const
     {
-        if (k <= kNever) return 0.0;
-        const float x = value_of(k);
-        if (infinite) return x == INFINITY ? 1.0 : 0.0;
-        const double y = ((double)x - top) * per_t;
-        return y < -40.0 ? 0.0 : exp(y);
+        if (infinite) return value_of(k) == INFINITY ? 1ull << kShift : 0;
+        const double t = ((double)value_of(k) - top) * halvings;
+        constexpr double whole = 6755399441055744.0;       // 1.5 * 2^52: adding it rounds to an integer, in the low bits
+        const double r = t + whole, f = t - (r - whole);
+        constexpr double c[] = {1.0, 0.69314718055994531, 0.24022650695910072, 0.055504108664821580, 0.0096181291076284772,
+                                0.0013333558146428443, 1.5403530393381610e-4, 1.5252733804059840e-5, 1.3215486790144309e-6,
+                                1.0178086009239699e-7, 7.0549116208011233e-9, 4.4455382718708116e-10};
+        double p = c[11];
+#pragma unroll
+        for (int i = 10; i >= 0; --i) p = __builtin_fma(p, f, c[i]);
+        // p * 2^(round(t) + 43), rounded to an integer by adding 2^52; t below the range (-infinity, too) gives 0
+        const int e = (int)__double_as_longlong(r) + kShift;
+        const u64 scaled = __double_as_longlong(p) + ((u64)(uint32_t)e << 52);
+        const u64 units = __double_as_longlong(__longlong_as_double(scaled) + 4503599627370496.0) - 0x4330000000000000ull;
+        return t > -(double)kFar ? units : 0;
     }
-    __device__ __forceinline__ u64 fixed(double w) const { return (u64)rint(w * (double)(1ull << kShift)); }
-    __device__ __forceinline__ u64 operator()(uint32_t k) const { return fixed(real(k)); }
 };
 
-// What is kept: everything above `key`, and of the tokens at `key` those numbered up to `last`.
+// What is kept: everything above `key`, and of the tokens at `key` those numbered up to `last`; of that, weights from
+// `least` units on.
 struct Kept {
     uint32_t key;
     int last;
@@ -47,14 +60,16 @@ struct Kept {
 };
 
 struct Shared {
-    u64 mass[256];
-    uint32_t count[256];
-    u64 seg[kSegments];
+    u64 seg[kMostSegments];
+    u64 list[kMostListed];
+    u64 mass[kBuckets];
+    uint32_t count[kBuckets];
     u64 wave_sum[kWaves];
+    uint32_t wave_count[2][kWaves];
     uint32_t key;
-    u64 left;
+    uint32_t listed;
     int index;
-    u64 total;
+    u64 left;
 };
 
 __device__ __forceinline__ u64 wave_sum(u64 v)
@@ -63,17 +78,68 @@ __device__ __forceinline__ u64 wave_sum(u64 v)
     return v;
 }
 
-// Running sums over sh.seg[0 .. n-1] in place (each entry: what is in front of it); returns the total.  All threads.
-__device__ u64 scan_segments(Shared &sh, int n)
-{
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    constexpr int EACH = kSegments / kThreads;
-    u64 v[EACH], sum = 0;
-    for (int e = 0; e < EACH; ++e) {
-        const int i = tid * EACH + e;
-        v[e] = i < n ? sh.seg[i] : 0;
-        sum += v[e];
+// A row in pieces of 16 bytes, at the addresses that are multiples of 16, a piece per thread at a time, so that the
+// pieces of a wave in one round are a segment of the row, and the segments in the order of rounds and waves are in the
+// order of tokens. 
+template <typename T>
+struct Row {
+    static constexpr int E = 16 / sizeof(T);
+    const T *row;
+    int V, shift, rounds;
+
+    __device__ __forceinline__ void init(const T *p, int n)
+    {
+        row = p;
+        V = n;
+        shift = (int)((uintptr_t)p / sizeof(T) % E);
+        rounds = ((V + shift + E - 1) / E + kThreads - 1) / kThreads;
     }
+    __device__ __forceinline__ int first(int piece) const { return piece * E - shift; }
+    __device__ __forceinline__ int segments() const { return rounds * kWaves; }
+    __device__ __forceinline__ int segment_of(int i) const { return (i + shift) / (E * 64); }
+
+    __device__ __forceinline__ uint4 read(int piece) const
+    {
+        const int i = first(piece);
+        uint4 v;
+        if (i >= 0 && i + E <= V) v = *(const uint4 *)(row + i);
+        else {
+            T x[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = i + e >= 0 && i + e < V ? row[i + e] : (T)-INFINITY;
+            __builtin_memcpy(&v, x, 16);
+        }
+        return v;
+    }
+    // f(key, token) of every token of a piece
+    template <typename F> __device__ __forceinline__ void each(uint4 v, int piece, F f) const
+    {
+        T x[E];
+        __builtin_memcpy(x, &v, 16);
+#pragma unroll
+        for (int e = 0; e < E; ++e) f(key_of((float)x[e]), first(piece) + e);
+    }
+    // body(piece's contents, piece, round) for all rounds, AHEAD loads under way at a time.
+    template <typename F> __device__ __forceinline__ void all(F body) const
+    {
+        constexpr int AHEAD = 4;
+        for (int r0 = 0; r0 < rounds; r0 += AHEAD) {
+            uint4 v[AHEAD];
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) v[a] = read((r0 + a) * kThreads + threadIdx.x);
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a)
+                if (r0 + a < rounds) body(v[a], (r0 + a) * kThreads + (int)threadIdx.x, r0 + a);
+        }
+    }
+};
+
+// Running sums over v[0 .. n-1] in place (each entry: what is in front of it); returns the total.  All threads.
+__device__ u64 scan(Shared &sh, u64 *v, int n)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, each = (n + kThreads - 1) / kThreads;
+    u64 sum = 0;
+    for (int i = tid * each; i < min(n, (tid + 1) * each); ++i) sum += v[i];
     u64 inc = sum;
     for (int d = 1; d < 64; d <<= 1) {
         const u64 o = __shfl_up(inc, d);
@@ -86,20 +152,33 @@ __device__ u64 scan_segments(Shared &sh, int n)
         if (w < wave) before += sh.wave_sum[w];
         all += sh.wave_sum[w];
     }
-    for (int e = 0; e < EACH; ++e) {
-        const int i = tid * EACH + e;
-        if (i < n) sh.seg[i] = before;
-        before += v[e];
+    for (int i = tid * each; i < min(n, (tid + 1) * each); ++i) {
+        const u64 x = v[i];
+        v[i] = before;
+        before += x;
     }
     __syncthreads();
     return all;
 }
 
-// The token, in the order of numbers, whose measure f(i), added to what is in front of it, first exceeds `at`
-// (at < the sum of all).  sh.seg holds the running sums of the segments.  All threads get the answer.
-template <typename F> __device__ int find_in_order(Shared &sh, int V, int seg_len, int segs, u64 at, F f)
+// Sums of f(key, token) over the segments, into sh.seg.
+template <typename R, typename F> __device__ __forceinline__ void segment_sums(Shared &sh, R &row, F f)
 {
-    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = threadIdx.x >> 6;
+    row.all([&](uint4 v, int piece, int round) {
+        u64 c = 0;
+        row.each(v, piece, [&](uint32_t k, int i) { c += f(k, i); });
+        c = wave_sum(c);
+        if ((threadIdx.x & 63) == 0) sh.seg[round * kWaves + wave] = c;
+    });
+    __syncthreads();
+}
+
+// The token whose measure f(key, token), added to those of the tokens with lower numbers, first exceeds `at` (which is
+// less than the sum of all).  sh.seg holds the running sums of the segments.  All threads get the answer.
+template <typename R, typename F> __device__ int find_in_order(Shared &sh, R &row, u64 at, F f)
+{
+    const int tid = threadIdx.x, lane = tid & 63, segs = row.segments();
     for (int i = tid; i < segs; i += kThreads) {
         const u64 next = i + 1 < segs ? sh.seg[i + 1] : ~0ull;
         if (sh.seg[i] <= at && at < next) sh.index = i;      // (of segments that add nothing the last: one thread)
@@ -108,46 +187,84 @@ template <typename F> __device__ int find_in_order(Shared &sh, int V, int seg_le
     const int seg = sh.index;
     __syncthreads();
     if (tid < 64) {
-        u64 before = sh.seg[seg];
-        const int end = min(V, (seg + 1) * seg_len);
-        int found = -1;
-        for (int i0 = seg * seg_len; i0 < end && found < 0; i0 += 64) {
-            const int i = i0 + lane;
-            const u64 w = i < end ? f(i) : 0;
-            u64 inc = w;
-            for (int d = 1; d < 64; d <<= 1) {
-                const u64 o = __shfl_up(inc, d);
-                if (lane >= d) inc += o;
-            }
-            const u64 hit = __ballot(w > 0 && before + inc > at);
-            if (hit) found = i0 + __ffsll(hit) - 1;
-            before += __shfl(inc, 63);
+        const int piece = seg * 64 + lane;
+        const uint4 v = row.read(piece);
+        u64 mine = 0;
+        row.each(v, piece, [&](uint32_t k, int i) { mine += f(k, i); });
+        u64 inc = mine;
+        for (int d = 1; d < 64; d <<= 1) {
+            const u64 o = __shfl_up(inc, d);
+            if (lane >= d) inc += o;
         }
+        u64 before = sh.seg[seg] + inc - mine;
+        int found = kLastIndex;
+        row.each(v, piece, [&](uint32_t k, int i) {
+            const u64 w = f(k, i);
+            before += w;
+            if (w > 0 && before > at) found = min(found, i);
+        });
+        for (int d = 32; d; d >>= 1) found = min(found, __shfl_xor(found, d));
         if (lane == 0) sh.index = found;
     }
     __syncthreads();
     return sh.index;
 }
 
-// Of the tokens in `within`, from the greatest: the one at which the number of tokens (by_mass: the sum of their
-// weights) reaches `target` >= 1, as the border of what is then kept.  If it is never reached, everything is.
-template <typename T, bool by_mass>
-__device__ Kept select(Shared &sh, const T *row, int V, int seg_len, int segs, const Weights &wt, Kept within, u64 target)
+// Adds (key, token) to sh.list where `take` is set; counts on beyond the list's end.
+__device__ __forceinline__ void put(Shared &sh, bool take, uint32_t k, int i)
 {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const u64 mask = __ballot(take);
+    if (!mask) return;
+    uint32_t base = 0;
+    const int lane = threadIdx.x & 63, leader = __ffsll(mask) - 1;
+    if (lane == leader) base = atomicAdd(&sh.listed, (uint32_t)__popcll(mask));
+    base = __shfl(base, leader) + __popcll(mask & ((1ull << lane) - 1));
+    if (take && base < kMostListed) sh.list[base] = (u64)~k << 32 | (uint32_t)i;
+}
+
+// Puts the n entries of sh.list in order, the greatest key first, equal ones by number.
+__device__ void sort_list(Shared &sh, int n)
+{
+    int m = 64;
+    while (m < n) m *= 2;
+    for (int i = n + threadIdx.x; i < m; i += kThreads) sh.list[i] = ~0ull;
+    __syncthreads();
+    for (int size = 2; size <= m; size *= 2)
+        for (int step = size / 2; step; step /= 2) {
+            const int t = threadIdx.x;
+            if (t < m / 2) {
+                const int i = (t / step) * step * 2 + t % step, j = i + step;
+                const bool up = (i & size) == 0;
+                const u64 x = sh.list[i], y = sh.list[j];
+                if ((x > y) == up) { sh.list[i] = y; sh.list[j] = x; }
+            }
+            __syncthreads();
+        }
+}
+__device__ __forceinline__ uint32_t listed_key(u64 x) { return ~(uint32_t)(x >> 32); }
+
+// Of the tokens in `within`, from the greatest: the one at which the number of tokens (by_mass: the sum of their
+// weights) reaches `target` >= 1, as the border of what is then kept.  If it is never reached, everything is.  Eight bits
+// of the key at a time: right for every row, and slow (each of the four passes ends in atomics on few counters), it
+// is there for what the lists are too short for.
+template <bool by_mass, typename R>
+__device__ __forceinline__ Kept select(Shared &sh, R &row, const Weights &wt, Kept within, u64 target)
+{
+    const int tid = threadIdx.x;
     uint32_t prefix = 0;
     u64 left = target, ties = 0;
     for (int shift = 24; shift >= 0; shift -= 8) {
         for (int i = tid; i < 256; i += kThreads) sh.count[i] = 0, sh.mass[i] = 0;
         __syncthreads();
         const uint32_t mask = shift == 24 ? 0u : ~0u << (shift + 8);
-        for (int i = tid; i < V; i += kThreads) {
-            const uint32_t k = load_key(row, i);
-            if ((k & mask) == prefix && k > kNever && within.has(k, i)) {
-                atomicAdd(&sh.count[k >> shift & 255], 1u);
-                if (by_mass) atomicAdd(&sh.mass[k >> shift & 255], wt(k));
-            }
-        }
+        row.all([&](uint4 v, int piece, int) {
+            row.each(v, piece, [&](uint32_t k, int i) {
+                if ((k & mask) == prefix && k > kNever && within.has(k, i)) {
+                    atomicAdd(&sh.count[k >> shift & 255], 1u);
+                    if (by_mass) atomicAdd(&sh.mass[k >> shift & 255], wt(k));
+                }
+            });
+        });
         __syncthreads();
         if (tid == 0) {
             int b = 255;
@@ -169,91 +286,203 @@ __device__ Kept select(Shared &sh, const T *row, int V, int seg_len, int segs, c
         __syncthreads();
     }
     // of the tokens with this key the first so many
-    u64 m = by_mass ? (left + wt(prefix) - 1) / wt(prefix) : left;
-    if (m >= ties) return Kept{prefix, prefix == within.key ? within.last : 0x7fffffff};
-    for (int s = wave; s < segs; s += kWaves) {
-        u64 c = 0;
-        for (int i = s * seg_len + lane; i < min(V, (s + 1) * seg_len); i += 64) c += load_key(row, i) == prefix;
-        c = wave_sum(c);
-        if (lane == 0) sh.seg[s] = c;
-    }
-    __syncthreads();
-    scan_segments(sh, segs);
-    const int last = find_in_order(sh, V, seg_len, segs, m - 1, [&](int i) -> u64 { return load_key(row, i) == prefix; });
-    return Kept{prefix, last};
+    const u64 m = by_mass ? (left + wt(prefix) - 1) / wt(prefix) : left;
+    if (m >= ties) return Kept{prefix, prefix == within.key ? within.last : kLastIndex};
+    auto is = [&](uint32_t k, int) -> u64 { return k == prefix; };
+    segment_sums(sh, row, is);
+    scan(sh, sh.seg, row.segments());
+    return Kept{prefix, find_in_order(sh, row, m - 1, is)};
 }
 
-// A workgroup per row.
+// A workgroup per row: the greatest logit, then what is kept, by whichever way is short for the row's limits, with the
+// sums of its weights by segments, then the segment that the draw falls into.
+//   top-k up to kThreads: the k-th of the threads' greatest logits is a bound that k tokens at least reach, and few more;
+//     those are listed, put in order, and cut by all limits there.
+//   top-p alone: weights summed into buckets of logits; the bucket that the border is in is listed and put in order.
+//   neither: nothing to find.
+// Where the lists are too short (top-k above kThreads, thousands of equal logits at a border) the border is found eight
+// bits at a time.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
 {
     __shared__ Shared sh;
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.vocab;
-    const T *row = (const T *)a.logits + r * a.row_stride;
-    const int seg_len = 64 * ((V + 64 * kSegments - 1) / (64 * kSegments)), segs = (V + seg_len - 1) / seg_len;
+    Row<T> row;
+    row.init((const T *)a.logits + r * a.row_stride, V);
+    const int segs = row.segments();
+    const float t = a.temperature ? a.temperature[r] : 1.0f;
+    const float top_p = a.top_p ? a.top_p[r] : 1.0f, min_p = a.min_p && a.min_p[r] > 0 ? a.min_p[r] : 0.0f;
+    const bool greedy = !(t > 0) || min_p > 1.0f;
+    const int k = a.top_k ? a.top_k[r] : 0;
 
-    if (tid == 0) sh.key = 0;
-    __syncthreads();
-    uint32_t top = 0;
-    for (int i = tid; i < V; i += kThreads) top = max(top, load_key(row, i));
+    if (tid == 0) { sh.key = 0; sh.listed = 0; sh.index = kLastIndex; }
+    uint32_t mine = 0;
+    int at_token = 0;
+    if (greedy)
+        row.all([&](uint4 v, int piece, int) {
+            row.each(v, piece, [&](uint32_t x, int i) { if (x > mine) { mine = x; at_token = i; } });
+        });
+    else
+        row.all([&](uint4 v, int piece, int) { row.each(v, piece, [&](uint32_t x, int) { mine = max(mine, x); }); });
+    uint32_t top = mine;
     for (int d = 32; d; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+    __syncthreads();
     if (lane == 0) atomicMax(&sh.key, top);
     __syncthreads();
     top = sh.key;
-    __syncthreads();
-
-    if (top <= kNever) {
+    if (top <= kNever || greedy) {
+        if (mine == top && greedy) atomicMin(&sh.index, at_token);
+        __syncthreads();
         if (tid == 0) {
-            a.token[r] = -1;
-            if (a.prob) a.prob[r] = 0.0f;
+            a.token[r] = top <= kNever ? -1 : sh.index;
+            if (a.prob) a.prob[r] = top <= kNever ? 0.0f : 1.0f;
         }
         return;
     }
-    const float t = a.temperature ? a.temperature[r] : 1.0f;
-    const float top_p = a.top_p ? a.top_p[r] : 1.0f, min_p = a.min_p && a.min_p[r] > 0 ? a.min_p[r] : 0.0f;
-    const bool first = !(t > 0) || min_p > 1.0f;
-    const int k = first ? 1 : a.top_k ? a.top_k[r] : 0;
     Weights wt;
     wt.top = value_of(top);
     wt.infinite = value_of(top) == INFINITY;
-    wt.per_t = first ? 1.0 : 1.0 / (double)t;
+    wt.halvings = 1.4426950408889634 / (double)t;
+    // the least weight that is kept, in units: w >= min_p as numbers is rint(2^43 w) >= this but for what is nearer to the
+    // border than half a unit
+    const u64 least = max((u64)rint((double)min_p * (double)(1ull << kShift)), 1ull);
+    const double need_share = (double)top_p;
+    auto needed = [&](u64 total) {       // units in front of which a token is still kept
+        const double need = ceil(need_share * (double)total);
+        return need >= 1.0 ? (u64)need : 1ull;
+    };
 
-    Kept kept{kNever, 0x7fffffff};
-    if (k > 0 && k < V) kept = select<T, false>(sh, row, V, seg_len, segs, wt, kept, (u64)k);
-    auto sums = [&](double least) {      // of what is kept, in segments
-        for (int s = wave; s < segs; s += kWaves) {
-            u64 c = 0;
-            for (int i = s * seg_len + lane; i < min(V, (s + 1) * seg_len); i += 64) {
-                const uint32_t x = load_key(row, i);
-                if (kept.has(x, i)) {
-                    const double w = wt.real(x);
-                    if (w >= least) c += wt.fixed(w);
+    Kept kept{kNever, kLastIndex};
+    bool summed = false;                 // sh.seg holds the sums of what is kept
+    auto measure = [&](uint32_t x, int i) -> u64 {
+        if (!kept.has(x, i)) return 0;
+        const u64 w = wt(x);
+        return w >= least ? w : 0;
+    };
+    const bool by_p = top_p < 1.0f;
+    if (k > 0 && k < V) {
+        uint32_t bound = 0;
+        if (k <= kThreads) {             // the k-th greatest of the threads' greatest, bit by bit
+            for (int bit = 31; bit >= (sizeof(T) == 2 ? 13 : 0); --bit) {
+                const uint32_t with = bound | 1u << bit;
+                const uint32_t c = __popcll(__ballot(mine >= with));
+                if (lane == 0) sh.wave_count[bit & 1][wave] = c;
+                __syncthreads();
+                uint32_t all = 0;
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) all += sh.wave_count[bit & 1][w];
+                if (all >= (uint32_t)k) bound = with;
+            }
+            row.all([&](uint4 v, int piece, int) {
+                row.each(v, piece, [&](uint32_t x, int i) { put(sh, x >= bound && x > kNever, x, i); });
+            });
+            __syncthreads();
+        }
+        const int n = (int)sh.listed;
+        if (k <= kThreads && n <= kMostListed && n > 0) {
+            for (int s = tid; s < segs; s += kThreads) sh.seg[s] = 0;
+            sort_list(sh, n);
+            if (tid == 0) sh.index = 0;
+            u64 *w = sh.mass;            // (as many entries as the list)
+            for (int i = tid; i < n; i += kThreads) w[i] = i < k ? wt(listed_key(sh.list[i])) : 0;
+            __syncthreads();
+            const u64 total = scan(sh, w, n);
+            const u64 need = by_p ? needed(total) : ~0ull;
+            for (int i = tid; i < n; i += kThreads) {
+                const u64 x = (i + 1 < n ? w[i + 1] : total) - w[i];
+                if (i < k && w[i] < need && x >= least) {
+                    atomicMax(&sh.index, i);
+                    atomicAdd(&sh.seg[row.segment_of((int)sh.list[i])], x);
                 }
             }
-            c = wave_sum(c);
-            if (lane == 0) sh.seg[s] = c;
+            __syncthreads();
+            const u64 last = sh.list[sh.index];
+            kept = Kept{listed_key(last), (int)last};
+            summed = true;
+            __syncthreads();
+        } else {
+            __syncthreads();
+            kept = select<false>(sh, row, wt, kept, (u64)k);
+            if (by_p) {
+                segment_sums(sh, row, [&](uint32_t x, int i) -> u64 { return kept.has(x, i) ? wt(x) : 0; });
+                kept = select<true>(sh, row, wt, kept, needed(scan(sh, sh.seg, segs)));
+            }
         }
+    } else if (by_p) {
+        const float topf = value_of(top), per = fminf((float)(wt.halvings * (kBuckets / (double)kFar)), 3e38f);
+        auto bucket = [&](uint32_t x) { return (int)fminf((topf - value_of(x)) * per, (float)(kBuckets - 1)); };
+        for (int i = tid; i < kBuckets; i += kThreads) sh.mass[i] = 0, sh.count[i] = 0;
         __syncthreads();
-        return scan_segments(sh, segs);
-    };
-    if (!first && top_p < 1.0f) {
-        const u64 total = sums(0.0);
-        const double need = ceil((double)top_p * (double)total);
-        kept = select<T, true>(sh, row, V, seg_len, segs, wt, kept, need >= 1.0 ? (u64)need : 1ull);
+        if (!wt.infinite)
+            row.all([&](uint4 v, int piece, int) {
+                row.each(v, piece, [&](uint32_t x, int) {
+                    const u64 w = wt(x);
+                    if (w) {
+                        const int b = bucket(x);
+                        atomicAdd(&sh.mass[b], w);
+                        atomicAdd(&sh.count[b], 1u);
+                    }
+                });
+            });
+        __syncthreads();
+        const u64 total = scan(sh, sh.mass, kBuckets);
+        const u64 need = needed(total);
+        if (!wt.infinite)
+            for (int i = tid; i < kBuckets; i += kThreads)
+                if (sh.mass[i] < need && need <= (i + 1 < kBuckets ? sh.mass[i + 1] : total)) sh.index = i;
+        __syncthreads();
+        const int border = sh.index;
+        if (!wt.infinite && sh.count[border] <= (uint32_t)kMostListed) {
+            const u64 inside = need - sh.mass[border];
+            const int n = (int)sh.count[border];
+            __syncthreads();
+            row.all([&](uint4 v, int piece, int round) {
+                u64 c = 0;
+                row.each(v, piece, [&](uint32_t x, int i) {
+                    const int b = x > kNever ? bucket(x) : kBuckets;
+                    bool take = false;
+                    if (b <= border) {
+                        const u64 w = wt(x);
+                        take = b == border && w > 0;
+                        c += b < border && w >= least ? w : 0;
+                    }
+                    put(sh, take, x, i);
+                });
+                c = wave_sum(c);
+                if (lane == 0) sh.seg[round * kWaves + wave] = c;
+            });
+            __syncthreads();
+            sort_list(sh, n);
+            if (tid == 0) sh.index = 0;
+            u64 *w = sh.mass;
+            for (int i = tid; i < n; i += kThreads) w[i] = wt(listed_key(sh.list[i]));
+            __syncthreads();
+            const u64 all = scan(sh, w, n);
+            for (int i = tid; i < n; i += kThreads)
+                if (w[i] < inside) {
+                    const u64 x = (i + 1 < n ? w[i + 1] : all) - w[i];
+                    atomicMax(&sh.index, i);
+                    if (x >= least) atomicAdd(&sh.seg[row.segment_of((int)sh.list[i])], x);
+                }
+            __syncthreads();
+            const u64 last = sh.list[sh.index];
+            kept = Kept{listed_key(last), (int)last};
+            summed = true;
+            __syncthreads();
+        } else {
+            __syncthreads();
+            segment_sums(sh, row, [&](uint32_t x, int) -> u64 { return x > kNever ? wt(x) : 0; });
+            kept = select<true>(sh, row, wt, kept, needed(scan(sh, sh.seg, segs)));
+        }
     }
-    const double least = first ? 0.0 : (double)min_p;
-    const u64 total = sums(least);
+    if (!summed) segment_sums(sh, row, measure);
+    const u64 total = scan(sh, sh.seg, segs);
     const double at = floor((double)(a.draw[r]) * (double)total);
     const u64 pick = at > 0 ? min((u64)at, total - 1) : 0;
-    const int token = find_in_order(sh, V, seg_len, segs, pick, [&](int i) -> u64 {
-        const uint32_t x = load_key(row, i);
-        if (!kept.has(x, i)) return 0;
-        const double w = wt.real(x);
-        return w >= least ? wt.fixed(w) : 0;
-    });
+    const int token = find_in_order(sh, row, pick, measure);
     if (tid == 0) {
         a.token[r] = token;
-        if (a.prob) a.prob[r] = (float)((double)wt(load_key(row, token)) / (double)total);
+        if (a.prob) a.prob[r] = (float)((double)wt(key_of((float)row.row[token])) / (double)total);
     }
 }
 
