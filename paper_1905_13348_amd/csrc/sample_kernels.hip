@@ -16,12 +16,11 @@ constexpr int kLastIndex = 0x7fffffff;
 
 typedef unsigned long long u64;
 
-// Logits as 32-bit numbers in their order: equal logits (-0 and +0, too) have equal keys; NaN counts as -infinity.
+// Logits that are numbers as 32-bit keys in their order: equal logits (-0 and +0, too) have equal keys.
 __device__ __forceinline__ uint32_t key_of(float x)
 {
     const uint32_t b = __float_as_uint(x + 0.0f);
-    const uint32_t k = b >> 31 ? ~b : b | 0x80000000u;
-    return x != x ? kNever : k;
+    return b >> 31 ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float value_of(uint32_t k) { return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k); }
 
@@ -31,10 +30,10 @@ __device__ __forceinline__ float value_of(uint32_t k) { return __uint_as_float(k
 struct Weights {
     double top, halvings;
     bool infinite;
-    __device__ __forceinline__ u64 operator()(uint32_t k) const
+    __device__ __forceinline__ u64 operator()(float x) const
     {
-        if (infinite) return value_of(k) == INFINITY ? 1ull << kShift : 0;
-        const double t = ((double)value_of(k) - top) * halvings;
+        if (infinite) return x == INFINITY ? 1ull << kShift : 0;
+        const double t = ((double)x - top) * halvings;
         constexpr double whole = 6755399441055744.0;       // 1.5 * 2^52: adding it rounds to an integer, in the low bits
         const double r = t + whole, f = t - (r - whole);
         constexpr double c[] = {1.0, 0.69314718055994531, 0.24022650695910072, 0.055504108664821580, 0.0096181291076284772,
@@ -51,12 +50,11 @@ struct Weights {
     }
 };
 
-// What is kept: everything above `key`, and of the tokens at `key` those numbered up to `last`; of that, weights from
-// `least` units on.
+// What is kept: everything above `value`, and of the tokens at it those numbered up to `last`.  (Never NaN.)
 struct Kept {
-    uint32_t key;
+    float value;
     int last;
-    __device__ __forceinline__ bool has(uint32_t k, int i) const { return k > key || (k == key && i <= last); }
+    __device__ __forceinline__ bool has(float x, int i) const { return x > value || (x == value && i <= last); }
 };
 
 struct Shared {
@@ -66,7 +64,7 @@ struct Shared {
     uint32_t count[kBuckets];
     u64 wave_sum[kWaves];
     uint32_t wave_count[2][kWaves];
-    uint32_t key;
+    float wave_top[kWaves];
     uint32_t listed;
     int index;
     u64 left;
@@ -111,13 +109,13 @@ struct Row {
         }
         return v;
     }
-    // f(key, token) of every token of a piece
+    // f(logit, token) of every token of a piece; what is no token counts as -infinity, what is no number may come as it is
     template <typename F> __device__ __forceinline__ void each(uint4 v, int piece, F f) const
     {
         T x[E];
         __builtin_memcpy(x, &v, 16);
 #pragma unroll
-        for (int e = 0; e < E; ++e) f(key_of((float)x[e]), first(piece) + e);
+        for (int e = 0; e < E; ++e) f((float)x[e], first(piece) + e);
     }
     // body(piece's contents, piece, round) for all rounds, AHEAD loads under way at a time.
     template <typename F> __device__ __forceinline__ void all(F body) const
@@ -161,20 +159,20 @@ __device__ u64 scan(Shared &sh, u64 *v, int n)
     return all;
 }
 
-// Sums of f(key, token) over the segments, into sh.seg.
+// Sums of f(logit, token) over the segments, into sh.seg.
 template <typename R, typename F> __device__ __forceinline__ void segment_sums(Shared &sh, R &row, F f)
 {
     const int wave = threadIdx.x >> 6;
     row.all([&](uint4 v, int piece, int round) {
         u64 c = 0;
-        row.each(v, piece, [&](uint32_t k, int i) { c += f(k, i); });
+        row.each(v, piece, [&](float x, int i) { c += f(x, i); });
         c = wave_sum(c);
         if ((threadIdx.x & 63) == 0) sh.seg[round * kWaves + wave] = c;
     });
     __syncthreads();
 }
 
-// The token whose measure f(key, token), added to those of the tokens with lower numbers, first exceeds `at` (which is
+// The token whose measure f(logit, token), added to those of the tokens with lower numbers, first exceeds `at` (which is
 // less than the sum of all).  sh.seg holds the running sums of the segments.  All threads get the answer.
 template <typename R, typename F> __device__ int find_in_order(Shared &sh, R &row, u64 at, F f)
 {
@@ -190,7 +188,7 @@ template <typename R, typename F> __device__ int find_in_order(Shared &sh, R &ro
         const int piece = seg * 64 + lane;
         const uint4 v = row.read(piece);
         u64 mine = 0;
-        row.each(v, piece, [&](uint32_t k, int i) { mine += f(k, i); });
+        row.each(v, piece, [&](float x, int i) { mine += f(x, i); });
         u64 inc = mine;
         for (int d = 1; d < 64; d <<= 1) {
             const u64 o = __shfl_up(inc, d);
@@ -198,8 +196,8 @@ template <typename R, typename F> __device__ int find_in_order(Shared &sh, R &ro
         }
         u64 before = sh.seg[seg] + inc - mine;
         int found = kLastIndex;
-        row.each(v, piece, [&](uint32_t k, int i) {
-            const u64 w = f(k, i);
+        row.each(v, piece, [&](float x, int i) {
+            const u64 w = f(x, i);
             before += w;
             if (w > 0 && before > at) found = min(found, i);
         });
@@ -210,8 +208,8 @@ template <typename R, typename F> __device__ int find_in_order(Shared &sh, R &ro
     return sh.index;
 }
 
-// Adds (key, token) to sh.list where `take` is set; counts on beyond the list's end.
-__device__ __forceinline__ void put(Shared &sh, bool take, uint32_t k, int i)
+// Adds (logit, token) to sh.list where `take` is set; counts on beyond the list's end.
+__device__ __forceinline__ void put(Shared &sh, bool take, float x, int i)
 {
     const u64 mask = __ballot(take);
     if (!mask) return;
@@ -219,10 +217,10 @@ __device__ __forceinline__ void put(Shared &sh, bool take, uint32_t k, int i)
     const int lane = threadIdx.x & 63, leader = __ffsll(mask) - 1;
     if (lane == leader) base = atomicAdd(&sh.listed, (uint32_t)__popcll(mask));
     base = __shfl(base, leader) + __popcll(mask & ((1ull << lane) - 1));
-    if (take && base < kMostListed) sh.list[base] = (u64)~k << 32 | (uint32_t)i;
+    if (take && base < kMostListed) sh.list[base] = (u64)~key_of(x) << 32 | (uint32_t)i;
 }
 
-// Puts the n entries of sh.list in order, the greatest key first, equal ones by number.
+// Puts the n entries of sh.list in order, the greatest logit first, equal ones by number.
 __device__ void sort_list(Shared &sh, int n)
 {
     int m = 64;
@@ -241,7 +239,7 @@ __device__ void sort_list(Shared &sh, int n)
             __syncthreads();
         }
 }
-__device__ __forceinline__ uint32_t listed_key(u64 x) { return ~(uint32_t)(x >> 32); }
+__device__ __forceinline__ float listed(u64 x) { return value_of(~(uint32_t)(x >> 32)); }
 
 // Of the tokens in `within`, from the greatest: the one at which the number of tokens (by_mass: the sum of their
 // weights) reaches `target` >= 1, as the border of what is then kept.  If it is never reached, everything is.  Eight bits
@@ -258,10 +256,11 @@ __device__ __forceinline__ Kept select(Shared &sh, R &row, const Weights &wt, Ke
         __syncthreads();
         const uint32_t mask = shift == 24 ? 0u : ~0u << (shift + 8);
         row.all([&](uint4 v, int piece, int) {
-            row.each(v, piece, [&](uint32_t k, int i) {
-                if ((k & mask) == prefix && k > kNever && within.has(k, i)) {
+            row.each(v, piece, [&](float x, int i) {
+                const uint32_t k = key_of(x);
+                if ((k & mask) == prefix && x > -INFINITY && within.has(x, i)) {
                     atomicAdd(&sh.count[k >> shift & 255], 1u);
-                    if (by_mass) atomicAdd(&sh.mass[k >> shift & 255], wt(k));
+                    if (by_mass) atomicAdd(&sh.mass[k >> shift & 255], wt(x));
                 }
             });
         });
@@ -285,13 +284,14 @@ __device__ __forceinline__ Kept select(Shared &sh, R &row, const Weights &wt, Ke
         prefix |= (uint32_t)b << shift;
         __syncthreads();
     }
-    // of the tokens with this key the first so many
-    const u64 m = by_mass ? (left + wt(prefix) - 1) / wt(prefix) : left;
-    if (m >= ties) return Kept{prefix, prefix == within.key ? within.last : kLastIndex};
-    auto is = [&](uint32_t k, int) -> u64 { return k == prefix; };
+    // of the tokens with this logit the first so many
+    const float value = value_of(prefix);
+    const u64 m = by_mass ? (left + wt(value) - 1) / wt(value) : left;
+    if (m >= ties) return Kept{value, value == within.value ? within.last : kLastIndex};
+    auto is = [&](float x, int) -> u64 { return x == value; };
     segment_sums(sh, row, is);
     scan(sh, sh.seg, row.segments());
-    return Kept{prefix, find_in_order(sh, row, m - 1, is)};
+    return Kept{value, find_in_order(sh, row, m - 1, is)};
 }
 
 // A workgroup per row: the greatest logit, then what is kept, by whichever way is short for the row's limits, with the
@@ -315,33 +315,30 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     const bool greedy = !(t > 0) || min_p > 1.0f;
     const int k = a.top_k ? a.top_k[r] : 0;
 
-    if (tid == 0) { sh.key = 0; sh.listed = 0; sh.index = kLastIndex; }
-    uint32_t mine = 0;
-    int at_token = 0;
-    if (greedy)
-        row.all([&](uint4 v, int piece, int) {
-            row.each(v, piece, [&](uint32_t x, int i) { if (x > mine) { mine = x; at_token = i; } });
-        });
-    else
-        row.all([&](uint4 v, int piece, int) { row.each(v, piece, [&](uint32_t x, int) { mine = max(mine, x); }); });
-    uint32_t top = mine;
-    for (int d = 32; d; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+    if (tid == 0) { sh.listed = 0; sh.index = kLastIndex; }
+    float mine = -INFINITY;
+    int at_token = kLastIndex;
+    if (greedy) row.all([&](uint4 v, int piece, int) { row.each(v, piece, [&](float x, int i) { if (x > mine) { mine = x; at_token = i; } }); });
+    else row.all([&](uint4 v, int piece, int) { row.each(v, piece, [&](float x, int) { mine = fmaxf(mine, x); }); });
+    float top = mine;
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    if (lane == 0) sh.wave_top[wave] = top;
     __syncthreads();
-    if (lane == 0) atomicMax(&sh.key, top);
-    __syncthreads();
-    top = sh.key;
-    if (top <= kNever || greedy) {
+    top = sh.wave_top[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sh.wave_top[w]);
+    if (top == -INFINITY || greedy) {
         if (mine == top && greedy) atomicMin(&sh.index, at_token);
         __syncthreads();
         if (tid == 0) {
-            a.token[r] = top <= kNever ? -1 : sh.index;
-            if (a.prob) a.prob[r] = top <= kNever ? 0.0f : 1.0f;
+            a.token[r] = top == -INFINITY ? -1 : sh.index;
+            if (a.prob) a.prob[r] = top == -INFINITY ? 0.0f : 1.0f;
         }
         return;
     }
     Weights wt;
-    wt.top = value_of(top);
-    wt.infinite = value_of(top) == INFINITY;
+    wt.top = top;
+    wt.infinite = top == INFINITY;
     wt.halvings = 1.4426950408889634 / (double)t;
     // the least weight that is kept, in units: w >= min_p as numbers is rint(2^43 w) >= this but for what is nearer to the
     // border than half a unit
@@ -352,20 +349,21 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         return need >= 1.0 ? (u64)need : 1ull;
     };
 
-    Kept kept{kNever, kLastIndex};
+    Kept kept{-INFINITY, -1};
     bool summed = false;                 // sh.seg holds the sums of what is kept
-    auto measure = [&](uint32_t x, int i) -> u64 {
+    auto measure = [&](float x, int i) -> u64 {
         if (!kept.has(x, i)) return 0;
         const u64 w = wt(x);
         return w >= least ? w : 0;
     };
     const bool by_p = top_p < 1.0f;
     if (k > 0 && k < V) {
-        uint32_t bound = 0;
-        if (k <= kThreads) {             // the k-th greatest of the threads' greatest, bit by bit
+        if (k <= kThreads) {
+            uint32_t bound = 0;
+            const uint32_t mine_key = key_of(mine);             // the k-th greatest of the threads' greatest, bit by bit
             for (int bit = 31; bit >= (sizeof(T) == 2 ? 13 : 0); --bit) {
                 const uint32_t with = bound | 1u << bit;
-                const uint32_t c = __popcll(__ballot(mine >= with));
+                const uint32_t c = __popcll(__ballot(mine_key >= with));
                 if (lane == 0) sh.wave_count[bit & 1][wave] = c;
                 __syncthreads();
                 uint32_t all = 0;
@@ -373,8 +371,10 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
                 for (int w = 0; w < kWaves; ++w) all += sh.wave_count[bit & 1][w];
                 if (all >= (uint32_t)k) bound = with;
             }
+            // (a bound of no number: fewer threads than k have logits at all)
+            const float from = bound <= kNever ? -INFINITY : value_of(bound);
             row.all([&](uint4 v, int piece, int) {
-                row.each(v, piece, [&](uint32_t x, int i) { put(sh, x >= bound && x > kNever, x, i); });
+                row.each(v, piece, [&](float x, int i) { put(sh, x >= from && x > -INFINITY, x, i); });
             });
             __syncthreads();
         }
@@ -384,7 +384,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
             sort_list(sh, n);
             if (tid == 0) sh.index = 0;
             u64 *w = sh.mass;            // (as many entries as the list)
-            for (int i = tid; i < n; i += kThreads) w[i] = i < k ? wt(listed_key(sh.list[i])) : 0;
+            for (int i = tid; i < n; i += kThreads) w[i] = i < k ? wt(listed(sh.list[i])) : 0;
             __syncthreads();
             const u64 total = scan(sh, w, n);
             const u64 need = by_p ? needed(total) : ~0ull;
@@ -397,25 +397,25 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
             }
             __syncthreads();
             const u64 last = sh.list[sh.index];
-            kept = Kept{listed_key(last), (int)last};
+            kept = Kept{listed(last), (int)last};
             summed = true;
             __syncthreads();
         } else {
             __syncthreads();
             kept = select<false>(sh, row, wt, kept, (u64)k);
             if (by_p) {
-                segment_sums(sh, row, [&](uint32_t x, int i) -> u64 { return kept.has(x, i) ? wt(x) : 0; });
+                segment_sums(sh, row, [&](float x, int i) -> u64 { return kept.has(x, i) ? wt(x) : 0; });
                 kept = select<true>(sh, row, wt, kept, needed(scan(sh, sh.seg, segs)));
             }
         }
     } else if (by_p) {
-        const float topf = value_of(top), per = fminf((float)(wt.halvings * (kBuckets / (double)kFar)), 3e38f);
-        auto bucket = [&](uint32_t x) { return (int)fminf((topf - value_of(x)) * per, (float)(kBuckets - 1)); };
+        const float per = fminf((float)(wt.halvings * (kBuckets / (double)kFar)), 3e38f);
+        auto bucket = [&](float x) { return (int)fminf((top - x) * per, (float)(kBuckets - 1)); };
         for (int i = tid; i < kBuckets; i += kThreads) sh.mass[i] = 0, sh.count[i] = 0;
         __syncthreads();
         if (!wt.infinite)
             row.all([&](uint4 v, int piece, int) {
-                row.each(v, piece, [&](uint32_t x, int) {
+                row.each(v, piece, [&](float x, int) {
                     const u64 w = wt(x);
                     if (w) {
                         const int b = bucket(x);
@@ -438,8 +438,8 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
             __syncthreads();
             row.all([&](uint4 v, int piece, int round) {
                 u64 c = 0;
-                row.each(v, piece, [&](uint32_t x, int i) {
-                    const int b = x > kNever ? bucket(x) : kBuckets;
+                row.each(v, piece, [&](float x, int i) {
+                    const int b = x > -INFINITY ? bucket(x) : kBuckets;
                     bool take = false;
                     if (b <= border) {
                         const u64 w = wt(x);
@@ -455,7 +455,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
             sort_list(sh, n);
             if (tid == 0) sh.index = 0;
             u64 *w = sh.mass;
-            for (int i = tid; i < n; i += kThreads) w[i] = wt(listed_key(sh.list[i]));
+            for (int i = tid; i < n; i += kThreads) w[i] = wt(listed(sh.list[i]));
             __syncthreads();
             const u64 all = scan(sh, w, n);
             for (int i = tid; i < n; i += kThreads)
@@ -466,12 +466,12 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
                 }
             __syncthreads();
             const u64 last = sh.list[sh.index];
-            kept = Kept{listed_key(last), (int)last};
+            kept = Kept{listed(last), (int)last};
             summed = true;
             __syncthreads();
         } else {
             __syncthreads();
-            segment_sums(sh, row, [&](uint32_t x, int) -> u64 { return x > kNever ? wt(x) : 0; });
+            segment_sums(sh, row, [&](float x, int) -> u64 { return wt(x); });
             kept = select<true>(sh, row, wt, kept, needed(scan(sh, sh.seg, segs)));
         }
     }
@@ -482,7 +482,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     const int token = find_in_order(sh, row, pick, measure);
     if (tid == 0) {
         a.token[r] = token;
-        if (a.prob) a.prob[r] = (float)((double)wt(key_of((float)row.row[token])) / (double)total);
+        if (a.prob) a.prob[r] = (float)((double)wt((float)row.row[token]) / (double)total);
     }
 }
 
