@@ -13,6 +13,7 @@ constexpr int kShift = 43;                   // a weight of 1 is 2^43: 2^20 of t
 constexpr float kFar = 44.0f;                // in halvings: weights further down are 0 units
 constexpr uint32_t kNever = 0x007fffffu;     // order key of -infinity
 constexpr int kLastIndex = 0x7fffffff;
+constexpr unsigned long long kRaw = 0x4330000000000000ull;   // the bits of 2^52
 
 typedef unsigned long long u64;
 
@@ -30,11 +31,13 @@ __device__ __forceinline__ float value_of(uint32_t k) { return __uint_as_float(k
 struct Weights {
     double top, halvings;
     bool infinite;
-    __device__ __forceinline__ u64 operator()(float x) const
+    // The units plus kRaw (for sums of many: one subtraction at the end instead of one each).  A weight is rounded to units
+    // by adding 2^52 to the double, whose bits are then those of the units behind the exponent; t below the range gives 0.
+    __device__ __forceinline__ u64 raw(float x) const
     {
-        if (infinite) return x == INFINITY ? 1ull << kShift : 0;
+        if (infinite) return kRaw + (x == INFINITY ? 1ull << kShift : 0);
         const double t = ((double)x - top) * halvings;
-        constexpr double whole = 6755399441055744.0;       // 1.5 * 2^52: adding it rounds to an integer, in the low bits
+        constexpr double whole = 6755399441055744.0 + kShift;      // 1.5 * 2^52: adding it rounds to an integer, in the low bits
         const double r = t + whole, f = t - (r - whole);
         constexpr double c[] = {1.0, 0.69314718055994531, 0.24022650695910072, 0.055504108664821580, 0.0096181291076284772,
                                 0.0013333558146428443, 1.5403530393381610e-4, 1.5252733804059840e-5, 1.3215486790144309e-6,
@@ -42,12 +45,11 @@ struct Weights {
         double p = c[11];
 #pragma unroll
         for (int i = 10; i >= 0; --i) p = __builtin_fma(p, f, c[i]);
-        // p * 2^(round(t) + 43), rounded to an integer by adding 2^52; t below the range (-infinity, too) gives 0
-        const int e = (int)__double_as_longlong(r) + kShift;
-        const u64 scaled = __double_as_longlong(p) + ((u64)(uint32_t)e << 52);
-        const u64 units = __double_as_longlong(__longlong_as_double(scaled) + 4503599627370496.0) - 0x4330000000000000ull;
-        return t > -(double)kFar ? units : 0;
+        const u64 scaled = __double_as_longlong(p) + ((u64)(uint32_t)__double_as_longlong(r) << 52);
+        const u64 bits = __double_as_longlong(__longlong_as_double(scaled) + 4503599627370496.0);
+        return t > -(double)kFar ? bits : kRaw;
     }
+    __device__ __forceinline__ u64 operator()(float x) const { return raw(x) - kRaw; }
 };
 
 // What is kept: everything above `value`, and of the tokens at it those numbered up to `last`.  (Never NaN.)
@@ -61,7 +63,7 @@ struct Shared {
     u64 seg[kMostSegments];
     u64 list[kMostListed];
     u64 mass[kBuckets];
-    uint32_t count[kBuckets];
+    uint32_t count[256];
     u64 wave_sum[kWaves];
     uint32_t wave_count[2][kWaves];
     float wave_top[kWaves];
@@ -117,18 +119,30 @@ struct Row {
 #pragma unroll
         for (int e = 0; e < E; ++e) f((float)x[e], first(piece) + e);
     }
-    // body(piece's contents, piece, round) for all rounds, AHEAD loads under way at a time.
+    // body(piece's contents, piece, round) for all rounds: those that lie within the row without a look at its ends, the
+    // next AHEAD pieces under way while these are worked on; then the one or two others.
     template <typename F> __device__ __forceinline__ void all(F body) const
     {
-        constexpr int AHEAD = 4;
-        for (int r0 = 0; r0 < rounds; r0 += AHEAD) {
-            uint4 v[AHEAD];
+        constexpr int AHEAD = 16 / E;
+        const int lo = shift ? 1 : 0, hi = max(lo, (V + shift) / (E * kThreads)), tid = threadIdx.x;
+        if (lo < hi) {
+            const T *const from = row - shift;
+            uint4 next[AHEAD];
 #pragma unroll
-            for (int a = 0; a < AHEAD; ++a) v[a] = read((r0 + a) * kThreads + threadIdx.x);
+            for (int a = 0; a < AHEAD; ++a) next[a] = *(const uint4 *)(from + (int64_t)(min(lo + a, hi - 1) * kThreads + tid) * E);
+            for (int r0 = lo; r0 < hi; r0 += AHEAD) {
+                uint4 v[AHEAD];
 #pragma unroll
-            for (int a = 0; a < AHEAD; ++a)
-                if (r0 + a < rounds) body(v[a], (r0 + a) * kThreads + (int)threadIdx.x, r0 + a);
+                for (int a = 0; a < AHEAD; ++a) v[a] = next[a];
+#pragma unroll
+                for (int a = 0; a < AHEAD; ++a) next[a] = *(const uint4 *)(from + (int64_t)(min(r0 + AHEAD + a, hi - 1) * kThreads + tid) * E);
+#pragma unroll
+                for (int a = 0; a < AHEAD; ++a)
+                    if (r0 + a < hi) body(v[a], (r0 + a) * kThreads + tid, r0 + a);
+            }
         }
+#pragma unroll 1
+        for (int r = lo ? 0 : hi; r < rounds; r = r < lo ? hi : r + 1) body(read(r * kThreads + tid), r * kThreads + tid, r);
     }
 };
 
@@ -166,6 +180,27 @@ template <typename R, typename F> __device__ __forceinline__ void segment_sums(S
     row.all([&](uint4 v, int piece, int round) {
         u64 c = 0;
         row.each(v, piece, [&](float x, int i) { c += f(x, i); });
+        c = wave_sum(c);
+        if ((threadIdx.x & 63) == 0) sh.seg[round * kWaves + wave] = c;
+    });
+    __syncthreads();
+}
+
+// The same of all weights from `least` units on.
+template <typename R> __device__ __forceinline__ void segment_weights(Shared &sh, R &row, const Weights &wt, u64 least)
+{
+    const int wave = threadIdx.x >> 6;
+    row.all([&](uint4 v, int piece, int round) {
+        u64 c = 0;
+        if (least <= 1) {
+            row.each(v, piece, [&](float x, int) { c += wt.raw(x); });
+            c -= R::E * kRaw;
+        } else {
+            row.each(v, piece, [&](float x, int) {
+                const u64 w = wt(x);
+                c += w >= least ? w : 0;
+            });
+        }
         c = wave_sum(c);
         if ((threadIdx.x & 63) == 0) sh.seg[round * kWaves + wave] = c;
     });
@@ -356,7 +391,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         const u64 w = wt(x);
         return w >= least ? w : 0;
     };
-    const bool by_p = top_p < 1.0f;
+    const bool by_p = top_p < 1.0f, everything = !by_p && !(k > 0 && k < V);
     if (k > 0 && k < V) {
         if (k <= kThreads) {
             uint32_t bound = 0;
@@ -411,17 +446,13 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
     } else if (by_p) {
         const float per = fminf((float)(wt.halvings * (kBuckets / (double)kFar)), 3e38f);
         auto bucket = [&](float x) { return (int)fminf((top - x) * per, (float)(kBuckets - 1)); };
-        for (int i = tid; i < kBuckets; i += kThreads) sh.mass[i] = 0, sh.count[i] = 0;
+        for (int i = tid; i < kBuckets; i += kThreads) sh.mass[i] = 0;
         __syncthreads();
         if (!wt.infinite)
             row.all([&](uint4 v, int piece, int) {
                 row.each(v, piece, [&](float x, int) {
                     const u64 w = wt(x);
-                    if (w) {
-                        const int b = bucket(x);
-                        atomicAdd(&sh.mass[b], w);
-                        atomicAdd(&sh.count[b], 1u);
-                    }
+                    if (w) atomicAdd(&sh.mass[bucket(x)], w);
                 });
             });
         __syncthreads();
@@ -432,9 +463,10 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
                 if (sh.mass[i] < need && need <= (i + 1 < kBuckets ? sh.mass[i + 1] : total)) sh.index = i;
         __syncthreads();
         const int border = sh.index;
-        if (!wt.infinite && sh.count[border] <= (uint32_t)kMostListed) {
-            const u64 inside = need - sh.mass[border];
-            const int n = (int)sh.count[border];
+        int n = kMostListed + 1;
+        u64 inside = 0;
+        if (!wt.infinite) {
+            inside = need - sh.mass[border];
             __syncthreads();
             row.all([&](uint4 v, int piece, int round) {
                 u64 c = 0;
@@ -452,6 +484,9 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
                 if (lane == 0) sh.seg[round * kWaves + wave] = c;
             });
             __syncthreads();
+            n = (int)sh.listed;
+        }
+        if (n <= kMostListed) {
             sort_list(sh, n);
             if (tid == 0) sh.index = 0;
             u64 *w = sh.mass;
@@ -471,11 +506,12 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
             __syncthreads();
         } else {
             __syncthreads();
-            segment_sums(sh, row, [&](float x, int) -> u64 { return wt(x); });
+            segment_weights(sh, row, wt, 1);
             kept = select<true>(sh, row, wt, kept, needed(scan(sh, sh.seg, segs)));
         }
     }
-    if (!summed) segment_sums(sh, row, measure);
+    if (everything) segment_weights(sh, row, wt, least);
+    else if (!summed) segment_sums(sh, row, measure);
     const u64 total = scan(sh, sh.seg, segs);
     const double at = floor((double)(a.draw[r]) * (double)total);
     const u64 pick = at > 0 ? min((u64)at, total - 1) : 0;
