@@ -21,6 +21,16 @@ from .binding import InfaasSelError, _AppendArgs, _Batch, _Cache, _stream_ptr, _
 _TYPES = None        # torch type -> INFAAS_SEL_TYPE_*
 
 
+_tensor_class = None
+
+
+def _tensor():
+    global _tensor_class
+    if _tensor_class is None:
+        _tensor_class = _use_torch().Tensor
+    return _tensor_class
+
+
 def _types():
     global _TYPES
     if _TYPES is None:
@@ -40,8 +50,7 @@ def _check(status: int) -> None:
 
 def _vector(t, dtype, name: str, size: Optional[int] = None) -> int:
     """Raw pointer of a contiguous device tensor of one dimension."""
-    torch = _use_torch()
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or t.dim() != 1 \
+    if not isinstance(t, _tensor()) or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous() or t.dim() != 1 \
             or (size is not None and t.numel() != size):
         raise TypeError(f"{name}: contiguous {dtype} device tensor [{'any' if size is None else size}] expected")
     return t.data_ptr()
@@ -97,6 +106,7 @@ class Batch:
             d_group_start=None if not groups else _vector(group_start, i32, "group_start", groups + 1),
             d_shared_len=None if not groups else _vector(shared_len, i32, "shared_len"))
         self._ref = ctypes.byref(self._c)
+        self._q_shape, self._kv_shape = (n, heads, cache.head_dim), (n, cache.kv_heads, cache.head_dim)
         self._cache = cache      # what the plan's sizes go by (head counts, head dimension, page size)
         size = load_library().infaas_sel_exec_plan_bytes(cache._ref, self._ref)
         if size == 0:
@@ -127,38 +137,40 @@ class Executor:
         _check(self._lib.infaas_sel_exec_plan(self._h, batch._cache._ref, batch._ref, _stream_ptr(stream)))
 
     @staticmethod
-    def _rows(t, cache: PagedCache, batch: Batch, heads: int, name: str):
+    def _rows(t, cache: PagedCache, batch: Batch, shape, name: str):
         """Pointer and strides of a [tokens][heads][head_dim] tensor."""
-        if t.dtype != cache.dtype or not t.is_cuda or t.shape != (batch.num_tokens, heads, cache.head_dim):
-            raise TypeError(f"{name}: {cache.dtype} device tensor [{batch.num_tokens}, {heads}, {cache.head_dim}] expected")
+        if t.dtype is not cache.dtype or not t.is_cuda or t.shape != shape:
+            raise TypeError(f"{name}: {cache.dtype} device tensor {list(shape)} expected")
         a, b, c = t.stride()
         if c != 1:
             raise TypeError(f"{name}: the last dimension is not consecutive")
         # (a dimension of one element has a stride of no meaning)
-        return t.data_ptr(), a if t.shape[0] > 1 else 0, b if heads > 1 else 0
+        return t.data_ptr(), a if shape[0] > 1 else 0, b if shape[1] > 1 else 0
 
     def append(self, cache: PagedCache, batch: Batch, q, k, v, q_out, freq=None, interleaved: bool = False,
                stream=None) -> None:
         """Keys and values into the cache, rotated by the positions; ``freq`` (float64, a frequency per rotated pair) None:
         not rotated; ``q`` and ``q_out`` both None: no queries."""
-        torch = _use_torch()
-        a = _AppendArgs(interleaved=1 if interleaved else 0)
-        if q is not None:
-            a.d_q, a.q_token_stride, a.q_head_stride = self._rows(q, cache, batch, batch.heads, "q")
-        if q_out is not None:
-            a.d_q_out, a.out_token_stride, a.out_head_stride = self._rows(q_out, cache, batch, batch.heads, "q_out")
-        a.d_k, a.k_token_stride, a.k_head_stride = self._rows(k, cache, batch, cache.kv_heads, "k")
-        a.d_v, a.v_token_stride, a.v_head_stride = self._rows(v, cache, batch, cache.kv_heads, "v")
-        if freq is not None:
-            a.d_freq, a.rot_dim = _vector(freq, torch.float64, "freq"), 2 * freq.numel()
-        _check(self._lib.infaas_sel_exec_append(self._h, cache._ref, batch._ref, ctypes.byref(a), _stream_ptr(stream)))
+        rows, q_shape, kv_shape = self._rows, batch._q_shape, batch._kv_shape
+        qp, qt, qh = (None, 0, 0) if q is None else rows(q, cache, batch, q_shape, "q")
+        op, ot, oh = (None, 0, 0) if q_out is None else rows(q_out, cache, batch, q_shape, "q_out")
+        kp, kt, kh = rows(k, cache, batch, kv_shape, "k")
+        vp, vt, vh = rows(v, cache, batch, kv_shape, "v")
+        fp, rot = (None, 0) if freq is None else (_vector(freq, _use_torch().float64, "freq"), 2 * freq.numel())
+        a = _AppendArgs(qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, fp, rot, 1 if interleaved else 0)
+        status = self._lib.infaas_sel_exec_append(self._h, cache._ref, batch._ref, a, _stream_ptr(stream))
+        if status:
+            _check(status)
 
     def attend(self, cache: PagedCache, batch: Batch, q, out, scale: Optional[float] = None, stream=None) -> None:
         """Attention of the planned batch's tokens over the cache; ``scale`` None: head_dim ** -0.5."""
-        _check(self._lib.infaas_sel_exec_attend(
-            self._h, cache._ref, batch._ref, *self._rows(q, cache, batch, batch.heads, "q"),
-            *self._rows(out, cache, batch, batch.heads, "out"), cache.head_dim ** -0.5 if scale is None else scale,
-            _stream_ptr(stream)))
+        shape = batch._q_shape
+        status = self._lib.infaas_sel_exec_attend(
+            self._h, cache._ref, batch._ref, *self._rows(q, cache, batch, shape, "q"),
+            *self._rows(out, cache, batch, shape, "out"), cache.head_dim ** -0.5 if scale is None else scale,
+            _stream_ptr(stream))
+        if status:
+            _check(status)
 
     def sample(self, logits, draws, token, prob=None, *, temperature=None, top_k=None, top_p=None, min_p=None,
                stream=None) -> None:
@@ -169,12 +181,16 @@ class Executor:
             raise TypeError("logits: device tensor [rows, vocab] expected, the last dimension consecutive")
         rows, vocab = logits.shape
         f32, i32 = torch.float32, torch.int32
-        limit = lambda t, dtype, name: None if t is None else _vector(t, dtype, name, rows)
-        _check(self._lib.infaas_sel_exec_sample(
+        status = self._lib.infaas_sel_exec_sample(
             self._h, rows, vocab, _types()[logits.dtype], logits.data_ptr(), logits.stride(0),
-            limit(temperature, f32, "temperature"), limit(top_k, i32, "top_k"), limit(top_p, f32, "top_p"),
-            limit(min_p, f32, "min_p"), _vector(draws, f32, "draws", rows), _vector(token, i32, "token", rows),
-            limit(prob, f32, "prob"), _stream_ptr(stream)))
+            temperature if temperature is None else _vector(temperature, f32, "temperature", rows),
+            top_k if top_k is None else _vector(top_k, i32, "top_k", rows),
+            top_p if top_p is None else _vector(top_p, f32, "top_p", rows),
+            min_p if min_p is None else _vector(min_p, f32, "min_p", rows),
+            _vector(draws, f32, "draws", rows), _vector(token, i32, "token", rows),
+            prob if prob is None else _vector(prob, f32, "prob", rows), _stream_ptr(stream))
+        if status:
+            _check(status)
 
     def destroy(self) -> None:
         if self._h:
