@@ -58,24 +58,28 @@ __device__ __forceinline__ UnitRange unit_range(const BatchArgs &b, const CacheA
     return r;
 }
 
-// One workgroup.  The cost of a tile is its keys; chunks are as long as makes kTargetItems items of all tiles, and the
-// same for all, so that items are of one length but for the last of each tile.
+// One workgroup.  The cost of a tile is its keys; chunks are as long as makes so many items of all tiles, and the same for
+// all, so that items are of one length but for the last of each tile.  How many depends on the rows of the tiles (their
+// mean by cost): see kFewItems.
 __global__ __launch_bounds__(kPlanThreads) void k_plan(BatchArgs b, CacheArgs c, PlanView p, int max_items, int max_rows)
 {
-    __shared__ unsigned long long cost;
+    __shared__ unsigned long long cost, row_cost;
     __shared__ long long scan[3][kPlanThreads / 64];
     __shared__ long long totals[3];
     const int tid = threadIdx.x, G = b.heads / b.kv_heads, per_tile = kTileRows / G, units = b.num_seqs + b.num_groups;
-    if (tid == 0) { cost = 0; totals[0] = totals[1] = totals[2] = 0; }
+    if (tid == 0) { cost = row_cost = 0; totals[0] = totals[1] = totals[2] = 0; }
     __syncthreads();
-    unsigned long long mine = 0;
+    unsigned long long mine = 0, mine_rows = 0;
     for (int u = tid; u < units; u += kPlanThreads) {
         const UnitRange r = unit_range(b, c, u);
         mine += (unsigned long long)((r.nt + per_tile - 1) / per_tile) * (unsigned)(r.k1 - r.k0);
+        mine_rows += (unsigned long long)r.nt * G * (unsigned)(r.k1 - r.k0);
     }
     atomicAdd(&cost, mine);
+    atomicAdd(&row_cost, mine_rows);
     __syncthreads();
-    const unsigned long long each = cost * (unsigned)b.kv_heads / kTargetItems + 1;
+    const int target = row_cost / kFewRows <= cost ? kFewItems : kTargetItems;
+    const unsigned long long each = cost * (unsigned)b.kv_heads / target + 1;
     const int chunk = each > 0x7fffff00ull ? 0x7fffff00
                                            : max(kMinChunk, (int)((each + kChunkStep - 1) / kChunkStep) * kChunkStep);
 
@@ -123,11 +127,16 @@ __global__ __launch_bounds__(kPlanThreads) void k_plan(BatchArgs b, CacheArgs c,
         h.max_len = c.max_len; h.table_width = c.table_width; h.page_shift = c.page_shift;
         h.num_items = n; h.rows = rows1;
     }
-    if (tid <= kDies) {      // the item at which so many eighths of the cost are reached
-        int at = n;
-        if (n > 0 && tid < kDies) {
-            const long long want = totals[2] * b.kv_heads / kDies * tid;
-            int lo = 0, hi = units - 1;
+    // the items at which so many eighths of the cost are reached, of groups and of sequences
+    if (tid <= kDies || (tid >= 64 && tid <= 64 + kDies)) {
+        const bool own = tid >= 64;
+        const int die = tid & 63, u0 = own ? b.num_groups : 0, u1 = own ? units : b.num_groups;
+        const int end = u1 == units ? n : min(p.units[u1].first_item * b.kv_heads, n);
+        int at = end;
+        if (n > 0 && u0 < u1 && die < kDies) {
+            const long long c0 = p.units[u0].first_cost, c1 = u1 == units ? totals[2] : p.units[u1].first_cost;
+            const long long want = c0 * b.kv_heads + (c1 - c0) * b.kv_heads / kDies * die;
+            int lo = u0, hi = u1 - 1;
             while (lo < hi) {
                 const int mid = (lo + hi + 1) / 2;
                 if (p.units[mid].first_cost * b.kv_heads <= want) lo = mid;
@@ -136,7 +145,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_plan(BatchArgs b, CacheArgs c,
             const PlanUnit pu = p.units[lo];
             at = pu.first_item * b.kv_heads + (pu.cost > 0 ? (int)((want - pu.first_cost * b.kv_heads) / pu.cost) : 0);
         }
-        p.head->die_start[tid] = min(at, n);
+        p.head->die_start[own][die] = clampi(at, 0, end);
     }
 
     for (int i = tid; i < n; i += kPlanThreads) {
@@ -235,6 +244,20 @@ __device__ __forceinline__ float max_of_halves(float x)
     return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
 }
 
+// Zeros in the place of infinities and NaN among eight values; whether there were any.
+template <typename T> __device__ __forceinline__ bool take_out(vec<uint32_t, 4> &v)
+{
+    constexpr uint32_t kExponent = std::is_same<T, bf16_t>::value ? 0x7f80 : 0x7c00;
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bool lo = (v[i] & kExponent) == kExponent, hi = (v[i] >> 16 & kExponent) == kExponent;
+        v[i] &= (lo ? 0 : 0xffffu) | (hi ? 0 : 0xffff0000u);
+        any |= lo | hi;
+    }
+    return any;
+}
+
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) void global_void;
 
@@ -250,7 +273,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
     constexpr int KB = D == 256 ? 32 : 64, CH = D / 8, LOADS = KB * CH / 256, ROW = D * 2;
     __shared__ uint4 lk0[KB * CH], lv0[KB * CH], lk1[KB * CH], lv1[KB * CH];
     __shared__ int64_t where[4][KB];      // of the next tiles' rows, in pieces; -1: not seen
-    __shared__ int reach[4];
+    __shared__ int reach[4], least[4];
+    __shared__ int odd;                   // values were taken out of a tile
     if (!plan_fits(a)) return;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
     const int G = a.batch.heads / a.batch.kv_heads;
@@ -262,12 +286,16 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
     const int vrow = half * 4 + (lane & 15) / 4;
     const int value_at = vrow * ROW + (((((lane >> 4) & 1) * 2 + (lane & 3) / 2) ^ value_turn<CH>(vrow)) << 4) + (lane & 1) * 8;
 
-    // Workgroups go to the dies in turn; each die takes a stretch of the list, so that neighbouring items (the tiles that
-    // read the same keys) meet in one L2.  Stretches are of equal cost: of equal numbers of items, the dies with the
-    // sequences' own parts were done in half the time of those with the long prefixes.
-    const int die = blockIdx.x & (kDies - 1), to = a.plan.head->die_start[die + 1], step = gridDim.x / kDies;
-    for (int i = a.plan.head->die_start[die] + (int)(blockIdx.x / kDies); i < to; i += step) {
-        const PlanItem it = a.plan.items[i];
+    // Workgroups go to the dies in turn; each die takes a stretch of the groups' items, and behind them one of the
+    // sequences', so that neighbouring items (the tiles that read the same keys) meet in one L2 and are there at the same
+    // time.  Stretches are of equal cost.  Of 256 sequences behind 32k prefixes: one stretch of both kinds to a die 458 us
+    // (some dies wait for their products, the others for an eighth of the memory's rate each), the kinds in turns 511 (tiles
+    // of the same keys drift apart), this 443.
+    const int die = blockIdx.x & (kDies - 1), step = gridDim.x / kDies;
+    const int first0 = a.plan.head->die_start[0][die], first1 = a.plan.head->die_start[1][die];
+    const int n0 = a.plan.head->die_start[0][die + 1] - first0, n = n0 + a.plan.head->die_start[1][die + 1] - first1;
+    for (int i = blockIdx.x / kDies; i < n; i += step) {
+        const PlanItem it = a.plan.items[i < n0 ? first0 + i : first1 + i - n0];
         const int rows = it.nt * G;
         const int r = wave * 32 + col;
         const bool valid = r < rows;
@@ -285,9 +313,12 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
         hi = __builtin_amdgcn_readfirstlane(hi);
         lo = __builtin_amdgcn_readfirstlane(lo);
         __syncthreads();
-        if (lane == 0) reach[wave] = hi;
+        if (lane == 0) { reach[wave] = hi; least[wave] = lo; }
+        if (tid == 0) odd = 0;
         __syncthreads();
         const int end = max(max(reach[0], reach[1]), max(reach[2], reach[3]));
+        const int all = min(min(least[0], least[1]), min(least[2], least[3]));
+        const int odd_from = all < end ? all - KB : 0x7fffffff;      // in tiles behind this key rows differ in what they see
 
         vec<float, 16> o[D / 32];
 #pragma unroll
@@ -320,11 +351,23 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
         };
         auto compute = [&](auto buf, int kt, int slot) {
             const char *const lk = (const char *)(buf.value ? lk1 : lk0);
-            const char *const lv = (const char *)(buf.value ? lv1 : lv0);
+            char *const lv = (char *)(buf.value ? lv1 : lv0);
             const unsigned long long bits = __ballot(where[slot][lane & (KB - 1)] >= 0);
-            if (bits != ~0ull) {       // values that nothing sees may be no numbers: zeros
-                for (int x = tid; x < KB * CH; x += 256)
-                    if (!(bits >> (x / CH) & 1)) ((uint4 *)lv)[x] = uint4{0, 0, 0, 0};
+            // Values that nothing sees may be no numbers: zeros.  Where some rows see keys that others do not, values that
+            // are no numbers are taken out, too, and added at the end where they are seen (a weight of zero would make
+            // NaN of them).
+            const bool some = kt > odd_from;
+            if (bits != ~0ull || some) {
+                for (int x = tid; x < KB * CH; x += 256) {
+                    vec<uint32_t, 4> v = ((const vec<uint32_t, 4> *)lv)[x];
+                    if (bits >> (x / CH) & 1) {
+                        if (!some || !take_out<T>(v)) continue;
+                        odd = 1;
+                    } else {
+                        v = vec<uint32_t, 4>{};
+                    }
+                    ((vec<uint32_t, 4> *)lv)[x] = v;
+                }
                 __syncthreads();
             }
             if (kt >= hi) return;
@@ -419,6 +462,22 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
         }
         __builtin_amdgcn_s_waitcnt(0x0f70);       // (nothing is under way to LDS when the next item or the end comes)
 
+        __syncthreads();
+        if (odd) {      // the values that were taken out, of the tiles that they were taken out of
+            for (int key = it.k0 + max(0, odd_from + KB - it.k0) / KB * KB; key < lim; ++key) {
+                const int64_t page = table[key >> a.cache.page_shift];
+                if (page < 0 || page >= a.cache.num_pages) continue;
+                const T *v = (const T *)a.cache.v + page * a.cache.page_stride + (key & page_mask) * a.cache.slot_stride +
+                             it.head * a.cache.head_stride + 4 * half;
+#pragma unroll
+                for (int x = 0; x < D / 8; ++x) {
+                    const vec<T, 4> y = *(const vec<T, 4> *)(v + 8 * x);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (!(fabsf((float)y[e]) < INFINITY)) o[x / 4][x % 4 * 4 + e] += (float)y[e];
+                }
+            }
+        }
         l += __shfl_xor(l, 32);
         if (valid && it.base < 0) {
             const float f = l > 0 ? 1.0f / l : (l == 0 ? 0.0f : l);     // (no key: zeros; NaN stays)
@@ -513,7 +572,8 @@ __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a)
 template <typename T, int D>
 hipError_t attend(const AttendArgs &a, int64_t max_items, hipStream_t s)
 {
-    const int grid = (int)(max_items < 2048 ? max_items : 2048) / kDies * kDies;
+    // (twice the items, because dies with shorter ones have more of them)
+    const int grid = ((int)(max_items < 1024 ? 2 * max_items : 2048) / kDies + 1) * kDies;
     k_attend_items<T, D><<<grid, 256, 0, s>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
     const unsigned rows = (unsigned)a.batch.num_tokens * a.batch.heads;

@@ -18,13 +18,15 @@ template <typename T, int N> using vec = T __attribute__((ext_vector_type(N)));
 
 // The rows of a tile are the (token, query head) pairs of whole tokens for one KV head, token-major.
 constexpr int kTileRows = 128;
-// Items that a plan aims at: two to each of the two workgroups that a compute unit holds, so that the end of one
-// launch is a quarter of a workgroup's time at most.
-#ifndef TGT
-#define TGT 1024
-#endif
-constexpr int kTargetItems = TGT;
-constexpr int kMinChunk = 256;       // keys of an item, at least: below, the merge costs more than the split gains
+// Items that a plan aims at.  Tiles of many rows wait for their products: two items to each of the two workgroups that a
+// compute unit holds, so that the end of a launch is a quarter of a workgroup's time at most.  Tiles of few rows wait for
+// memory, whose rate those that are left share: one item to each, with the fewest starts and the least to merge.  (1024, so
+// 512: prompts behind 16k keys 925 us, so 943; one sequence of 131k keys 122, so 116; 256 sequences behind 32k 448, so 414.
+// In between, with a part of the workgroups going twice, prompts took 1447 at 640.)
+constexpr int kTargetItems = 1024, kFewItems = 512;
+constexpr int kFewRows = kTileRows / 2;
+// Keys of an item, at least: a tile.  (Four sequences of 700 keys: 15.8 us with 256, 13.5 with 128, 12.2 with 64.)
+constexpr int kMinChunk = 64;
 constexpr int kChunkStep = 64;
 
 constexpr int kDies = 8;             // workgroups go to the dies in turn, each with an L2 of its own
@@ -37,8 +39,8 @@ struct PlanHeader {
     int32_t max_len, table_width, page_shift;
     int32_t num_items;               // over all KV heads
     int32_t rows;                    // partial rows of one KV head
-    int32_t die_start[kDies + 1];    // items of each die: stretches of equal cost
-    int32_t pad[11];
+    int32_t die_start[2][kDies + 1]; // items of each die, of groups and of sequences: stretches of equal cost
+    int32_t pad[2];
 };
 static_assert(sizeof(PlanHeader) == 128, "");
 constexpr uint32_t kPlanMagic = 0x1f5e9a7du;

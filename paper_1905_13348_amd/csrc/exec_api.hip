@@ -72,6 +72,7 @@ int check_pools(const infaas_sel_cache *c)
     if (c->num_pages < 1) return refuse("cache: %lld pages", (long long)c->num_pages);
     if (!vector_stride(c->page_stride) || !vector_stride(c->slot_stride) || !vector_stride(c->head_stride))
         return refuse("cache: strides are not multiples of 8 elements");
+    if (c->page_stride < 0 || c->slot_stride < 0 || c->head_stride < 0) return refuse("cache: a negative stride");
     return INFAAS_SEL_OK;
 }
 
@@ -112,7 +113,8 @@ bool plan_sizes(const infaas_sel_cache *c, const infaas_sel_batch *b, PlanSizes 
     const int64_t units = (int64_t)b->num_seqs + b->num_groups, per_tile = kTileRows / G;
     // tokens are in a tile of their own and one of their group's; the division into chunks adds what was aimed at
     const int64_t tiles = 2 * (n / per_tile) + units;
-    z->max_items = kTargetItems + H * (1 + tiles);
+    // (an item has kMinChunk keys but for the last of each tile)
+    z->max_items = std::min(kTargetItems + H * (1 + tiles), H * tiles * (b->max_len / kMinChunk + 1));
     z->max_rows = (int64_t)kTileRows * (kTargetItems / H + 2) + 2 * n * G;
     z->tokens_at = sizeof(PlanHeader);
     z->units_at = z->tokens_at + n * (int64_t)sizeof(PlanToken);

@@ -158,3 +158,9 @@ def test_python_side_refuses_shapes_and_types():
         pkg.PagedCache(x, x)           # not on a device
     with pytest.raises(ValueError):
         pkg.PagedCache(x, x, layout="other")
+
+
+@pytest.mark.parametrize("name", ["page_stride", "slot_stride", "head_stride"])
+def test_negative_strides_of_a_cache(lib, name):
+    _refused(lib, _attend(lib, _cache(**{name: -256}), _batch()), "cache", "negative")
+    _refused(lib, _append(lib, _cache(**{name: -256}), _batch()), "cache", "negative")

@@ -179,6 +179,30 @@ def test_infinities_and_nan_in_masked_places():
         _check(sc)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("groups", [False, True])
+def test_values_that_only_later_tokens_see_are_no_numbers(dim, dtype, groups):
+    """Infinities and NaN among a prompt's own values: tokens in front of them are as ever, the tokens that see them have
+    them in the result (where both infinities are, NaN)."""
+    shared = dict(groups=[0, 2], shared=[30]) if groups else {}
+    sc = Scene([(150, 110), (70, 36), (40, 40), (21, 1)], heads=4, kv_heads=2, dim=dim, dtype=dtype, seed=25, **shared)
+    want, weighted, top = sc.reference(dim ** -0.5)
+    for s, key, head, d, x in ((0, 75, 0, 3, np.nan), (0, 90, 1, 5, np.inf), (0, 140, 1, 5, -np.inf), (0, 64, 0, 60, -np.inf),
+                               (1, 69, 1, 9, np.inf), (2, 0, 0, 0, np.nan), (2, 39, 1, 63, -np.inf), (3, 20, 0, 1, np.inf)):
+        sc.v_pool[sc.table[s, key // 16], key % 16, head, d] = x
+        for t in range(sc.n):
+            if sc.seq[t] == s and sc.pos[t] >= key:
+                with np.errstate(invalid="ignore"):      # (infinities of both signs)
+                    want[t, 2 * head:2 * head + 2, d] += x
+    ex = pkg.Executor()
+    got = _call(ex, sc)
+    odd = ~np.isfinite(want)
+    assert np.array_equal(got[odd], want[odd], equal_nan=True)
+    tol = attend_tolerance(np.where(odd, 0, want), weighted, top, dtype, sc.length.max())
+    assert (np.abs(got[~odd] - want[~odd]) <= tol[~odd]).all()
+
+
 def test_large_scores_and_values():
     """Scores in the thousands (one key takes all) and values near the type's greatest."""
     sc = Scene([(300, 1), (65, 2)], dim=128, dtype=torch.float16, seed=16)
