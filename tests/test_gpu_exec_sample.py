@@ -221,3 +221,46 @@ def test_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(token, want), i
+
+
+@pytest.mark.parametrize("case", ["beyond 128", "below -128", "near zero", "only near zero", "zeros at the border", "few values", "negative",
+                                  "masked", "one value", "infinite"])
+def test_rows_of_few_values(case):
+    """bf16 rows long enough to be counted by value, and what that has to leave to the other ways."""
+    R, V = 14, 9_001
+    x = _logits(R, V, torch.float32, seed=40)
+    if case == "beyond 128":
+        x[:, 77] = torch.linspace(120, 3e38, R)
+    elif case == "below -128":
+        x[:, ::3] -= torch.linspace(100, 400, R, device="cuda")[:, None]
+        x[:, 1::3] = torch.finfo(torch.bfloat16).min
+    elif case == "near zero":
+        x[:, :1_500] *= 1e-4
+        x[7:, :4_000] *= 1e-5
+    elif case == "only near zero":
+        x *= 1e-5
+    elif case == "zeros at the border":
+        x = torch.where(x.abs() < 2, torch.zeros_like(x), x)
+        x[::2, 1_500:] -= 4
+    elif case == "few values":
+        x = x.round()
+    elif case == "negative":
+        x = -x.abs() - 0.01
+    elif case == "masked":
+        x[:, 5:] = -torch.inf
+        x[3] = torch.nan
+        x[4, :5] = torch.nan
+        x[5, ::2] = torch.nan
+    elif case == "one value":
+        x[:] = 1.5
+    elif case == "infinite":
+        x[:, [8, 4_000]] = torch.inf
+    x = x.bfloat16()
+    rng = np.random.default_rng(41)
+    for temperature in (0.7, 3.0, 40.0):
+        _check(x, _draws(R, 42), temperature=temperature)
+        _check(x, _draws(R, 43), temperature=temperature, top_p=[float(p) for p in rng.uniform(0.05, 0.999, R)])
+        _check(x, _draws(R, 44), temperature=temperature, top_k=[1, 2, 3, 5, 17, 100, 500, 1_000, 1_500, 3_000, 6_000, 9_000, 9_001, 0])
+        _check(x, _draws(R, 45), temperature=temperature, top_k=[int(k) for k in rng.integers(1, V, R)],
+               top_p=[float(p) for p in rng.uniform(0.05, 0.999, R)], min_p=[0.0, 0.3] * (R // 2))
+        _check(x, _draws(R, 46), temperature=temperature, min_p=[float(p) for p in 10 ** rng.uniform(-6, 0, R)])
