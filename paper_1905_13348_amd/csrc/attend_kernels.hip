@@ -261,6 +261,8 @@ template <typename T> __device__ __forceinline__ bool take_out(vec<uint32_t, 4> 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) void global_void;
 
+constexpr float kSlack = 8.0f;       // halvings
+
 // A workgroup of four waves takes items of up to 128 rows, 32 to a wave.  With K the A operand, S^T = K Q^T leaves a lane
 // with scores of ONE row (its column), so the running maximum and sum are a lane's own, and P^T is in registers where
 // the B operand of O^T = V^T P^T wants it: key slots of the second product are numbered as the first one leaves them.
@@ -272,7 +274,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
 {
     constexpr int KB = D == 256 ? 32 : 64, CH = D / 8, LOADS = KB * CH / 256, ROW = D * 2;
     __shared__ uint4 lk0[KB * CH], lv0[KB * CH], lk1[KB * CH], lv1[KB * CH];
-    __shared__ int64_t where[4][KB];      // of the next tiles' rows, in pieces; -1: not seen
+    __shared__ int64_t where[4][KB];      // of the next tiles' rows, in pieces (of what is not there: any that is)
+    constexpr int MINE = KB / 4;          // rows of a tile that each wave looks up
+    typedef std::conditional_t<MINE == 16, uint16_t, uint8_t> Seen;
+    __shared__ __align__(8) Seen seen[4][4];      // which of them are there
     __shared__ int reach[4], least[4];
     __shared__ int odd;                   // values were taken out of a tile
     if (!plan_fits(a)) return;
@@ -325,8 +330,6 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
         for (int dt = 0; dt < D / 32; ++dt) o[dt] = vec<float, 16>{};
         float m = -INFINITY, l = 0;
 
-        // each wave looks up its quarter of a tile's rows
-        constexpr int MINE = KB / 4;
         const int32_t *table = a.cache.table + (int64_t)it.seq * a.cache.table_width;
         auto entry = [&](int kt) {
             const int key = kt + wave * MINE + lane;
@@ -335,16 +338,19 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
         };
         auto note = [&](int kt, int64_t page, int slot) {
             const int key = kt + wave * MINE + lane;
+            const bool there = lane < MINE && page >= 0 && page < a.cache.num_pages;
             if (lane < MINE)
-                where[slot][wave * MINE + lane] = page >= 0 && page < a.cache.num_pages
-                    ? (page * a.cache.page_stride + (int64_t)(key & page_mask) * a.cache.slot_stride + it.head * a.cache.head_stride) / 8 : -1;
+                where[slot][wave * MINE + lane] = there
+                    ? (page * a.cache.page_stride + (int64_t)(key & page_mask) * a.cache.slot_stride + it.head * a.cache.head_stride) / 8 : 0;
+            const unsigned long long bits = __ballot(there);
+            if (lane == 0) seen[slot][wave] = (Seen)bits;
         };
         auto load = [&](auto buf, int slot) {
             uint4 *const lk = buf.value ? lk1 : lk0, *const lv = buf.value ? lv1 : lv0;
 #pragma unroll
             for (int x = 0; x < LOADS; ++x) {
                 const int row = (x * 256 + wave * 64 + lane) / CH, c = lane % CH;
-                const int64_t at = max(where[slot][row], (int64_t)0);      // (unseen: any row that is there)
+                const int64_t at = where[slot][row];
                 __builtin_amdgcn_global_load_lds((global_void *)(kp + at + (c ^ key_turn<CH>(row))), (lds_void *)(lk + x * 256 + wave * 64), 16, 0, 0);
                 __builtin_amdgcn_global_load_lds((global_void *)(vp + at + (c ^ value_turn<CH>(row))), (lds_void *)(lv + x * 256 + wave * 64), 16, 0, 0);
             }
@@ -352,7 +358,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
         auto compute = [&](auto buf, int kt, int slot) {
             const char *const lk = (const char *)(buf.value ? lk1 : lk0);
             char *const lv = (char *)(buf.value ? lv1 : lv0);
-            const unsigned long long bits = __ballot(where[slot][lane & (KB - 1)] >= 0);
+            unsigned long long bits = ~0ull;
+            __builtin_memcpy(&bits, seen[slot], sizeof(seen[slot]));
+            bits = (unsigned long long)__builtin_amdgcn_readfirstlane((int)(bits >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)bits);
             // Values that nothing sees may be no numbers: zeros.  Where some rows see keys that others do not, values that
             // are no numbers are taken out, too, and added at the end where they are seen (a weight of zero would make
             // NaN of them).
@@ -371,23 +379,51 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
                 __syncthreads();
             }
             if (kt >= hi) return;
-            // Thirty-two keys at a time.  What comes from LDS is read a phase ahead: values before the weights are computed,
-            // the next keys before the product with the values.  (Left to itself the compiler reads each operand where it
-            // is used and waits for it there: the barriers keep the phases in order.)
+            // All scores of the tile, so that the rows' maxima are looked at once, then the weights and the product with the
+            // values thirty-two keys at a time.  The order within is the compiler's: with operands read a phase ahead and the
+            // phases held apart, prompts behind 16k keys 895 us, so 853; one sequence of 131k keys 115, so 107.
             int key_from = key_at, value_from = value_at;
             asm volatile("" : "+v"(key_from), "+v"(value_from));      // (a dozen exclusive-ors a tile instead of as many registers)
-            vec<T, 8> kf[D / 16];
-            auto read_keys = [&](int kb) {
+            constexpr int NB = KB / 32;
+            vec<float, 16> s[NB];
 #pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk) kf[kk] = *(const vec<T, 8> *)(lk + (key_from ^ (kk << 5)) + kb * 32 * ROW);
-            };
-            read_keys(0);
+            for (int kb = 0; kb < NB; ++kb) {
+                s[kb] = vec<float, 16>{};
 #pragma unroll
-            for (int kb = 0; kb < KB / 32; ++kb) {
-                vec<float, 16> s = vec<float, 16>{};
-                __builtin_amdgcn_sched_barrier(0);
+                for (int kk = 0; kk < D / 16; ++kk)
+                    s[kb] = Mfma<T>::run(*(const vec<T, 8> *)(lk + (key_from ^ (kk << 5)) + kb * 32 * ROW), q[kk], s[kb]);
+            }
+            if (kt + KB > lo || bits != ~0ull) {
 #pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk) s = Mfma<T>::run(kf[kk], q[kk], s);
+                for (int kb = 0; kb < NB; ++kb) {
+                    const int left = lim - kt - kb * 32 - 4 * half;          // (rows counted from the lane's first)
+                    const uint32_t b = (uint32_t)(bits >> (kb * 32 + 4 * half));
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        const int row = 8 * (x / 4) + x % 4;
+                        const bool vis = row < left && (b & 1u << row);
+                        s[kb][x] = vis ? s[kb][x] : -INFINITY;
+                    }
+                }
+            }
+            float top = s[0][0];
+#pragma unroll
+            for (int x = 1; x < 16 * NB; ++x) top = fmaxf(top, s[x / 16][x % 16]);
+            top = max_of_halves(top) * a.scale_log2;
+            // The reference of the weights follows the maximum only when that is kSlack above it: weights up to 2^kSlack
+            // lose nothing in either type, and the results are scaled once or twice a row, not whenever one of a wave's
+            // rows has a new maximum (in two tiles of five over 8000 keys).
+            if (__any(top > m + kSlack)) {
+                const float m2 = fmaxf(m, top);
+                const float f = m2 == -INFINITY ? 1.0f : exp2_fast(m - m2);
+                m = m2;
+                l *= f;
+#pragma unroll
+                for (int dt = 0; dt < D / 32; ++dt) o[dt] *= f;
+            }
+            const float ref = m == -INFINITY ? 0.0f : m;      // (a row that has seen nothing yet)
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb) {
                 union { vec<short, 4> h[2]; vec<T, 8> v; } vf[D / 32][2];
 #pragma unroll
                 for (int dt = 0; dt < D / 32; ++dt)
@@ -397,42 +433,16 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
                         vf[dt][g].h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)at);
                         vf[dt][g].h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)(at + 8 * ROW));
                     }
-                __builtin_amdgcn_sched_barrier(0);
-                if (kt + KB > lo || bits != ~0ull) {
-                    const int left = lim - kt - kb * 32 - 4 * half;          // (rows counted from the lane's first)
-                    const uint32_t b = (uint32_t)(bits >> (kb * 32 + 4 * half));
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        const int row = 8 * (x / 4) + x % 4;
-                        const bool vis = row < left && (b & 1u << row);
-                        s[x] = vis ? s[x] : -INFINITY;
-                    }
-                }
-                float top = s[0];
-#pragma unroll
-                for (int x = 1; x < 16; ++x) top = fmaxf(top, s[x]);
-                top = max_of_halves(top) * a.scale_log2;
-                if (__any(top > m)) {
-                    const float m2 = fmaxf(m, top);
-                    const float f = m2 == -INFINITY ? 1.0f : exp2_fast(m - m2);
-                    m = m2;
-                    l *= f;
-#pragma unroll
-                    for (int dt = 0; dt < D / 32; ++dt) o[dt] *= f;
-                }
-                const float ref = m == -INFINITY ? 0.0f : m;      // (a row that has seen nothing yet)
                 vec<T, 8> pt[2];
 #pragma unroll
                 for (int x = 0; x < 16; x += 2) {
-                    const vec<float, 2> e = {exp2_fast(s[x] * a.scale_log2 - ref), exp2_fast(s[x + 1] * a.scale_log2 - ref)};
+                    const vec<float, 2> e = {exp2_fast(s[kb][x] * a.scale_log2 - ref), exp2_fast(s[kb][x + 1] * a.scale_log2 - ref)};
                     l += e[0];
                     l += e[1];
                     const vec<T, 2> y = __builtin_convertvector(e, vec<T, 2>);
                     pt[x / 8][x % 8] = y[0];
                     pt[x / 8][x % 8 + 1] = y[1];
                 }
-                if (kb + 1 < KB / 32) read_keys(kb + 1);
-                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int g = 0; g < 2; ++g)
 #pragma unroll
