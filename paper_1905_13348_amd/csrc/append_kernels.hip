@@ -21,6 +21,8 @@ __device__ __forceinline__ void store8(void *p, int64_t at, vec<T, 8> v)
 // cosine are computed once for all of them.  Rotated pairs lie in two vectors of eight: dimensions c*8.. and c*8 +
 // rot/2.. (halves), or 16c.. (neighbours).
 // What bounds it: memory from a few hundred tokens on (every element is read once and written once), below that the launch.
+// 16,001 tokens of 32 + 8 + 8 heads of 128 in fp16, 393 MB: 89 us, 4.4 TB/s, where a large copy reaches 4.9; 1 and 128
+// tokens: 7.2 us.
 template <typename T>
 __global__ __launch_bounds__(256) void k_append(AppendArgs p)
 {

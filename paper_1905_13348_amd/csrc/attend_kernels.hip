@@ -60,7 +60,7 @@ __device__ __forceinline__ UnitRange unit_range(const BatchArgs &b, const CacheA
 
 // One workgroup.  The cost of a tile is its keys; chunks are as long as makes so many items of all tiles, and the same for
 // all, so that items are of one length but for the last of each tile.  How many depends on the rows of the tiles (their
-// mean by cost): see kFewItems.
+// mean by cost): see kFewItems.  10 us for few sequences, 18 for 256 behind prefixes: once a step, for all layers.
 __global__ __launch_bounds__(kPlanThreads) void k_plan(BatchArgs b, CacheArgs c, PlanView p, int max_items, int max_rows)
 {
     __shared__ unsigned long long cost, row_cost;
@@ -269,6 +269,12 @@ constexpr float kSlack = 8.0f;       // halvings
 // V^T's rows come from LDS through the transposing read.  A tile of keys and values is loaded straight into LDS while the
 // one before it is computed; where its rows are (the page table's entries) is looked up two tiles ahead, because the
 // two trips to memory in a row take longer than a tile.
+// What bounds it (bf16, 32 query heads on 8 KV heads of 128 dimensions; both kernels together): memory where few rows see
+// many keys, one token behind 131,072 keys 107 us, 5.0 TB/s, 256 tokens behind four prefixes of up to 32,768 and own parts of
+// up to 2048 370 us, 4.8 TB/s (a large copy: 4.9); issue where tiles are full, prompts of up to 512 tokens behind 16,000 keys
+// (fp16, on 4 KV heads) 853 us, 730 TFLOP/s: the matrix units work half of the time, 7.5 other vector instructions come
+// to a product, and two waves on a SIMD do not hide all of them.  Few short sequences wait for the chain of loads from the
+// plan to the first tile: four of up to 700 keys 11.9 us, 4.4 of them the merge's.
 template <typename T, int D>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendArgs a)
 {
@@ -517,8 +523,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
 // ---- merge ------------------------------------------------------------------------------------
 
 // D/4 threads side by side take four dimensions of a (token, query head) each.  A workgroup takes ROWS of those; the
-// threads that are left over take further splits, merged through LDS at the end.  One row to a workgroup for few rows
-// (which may have a hundred splits each), as many as fit for many: 80,000 rows of three splits 145 us with one row each.
+// threads that are left over take further splits, merged through LDS at the end.  Bound by the reads of the results, from
+// L2 and memory: 80,000 rows of three splits 26 us.  One row to a workgroup for few rows
+// (which may have a hundred splits each), as many as fit for many: those 80,000 rows took 145 us with one row each.
 template <typename T, int D, int ROWS>
 __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a)
 {

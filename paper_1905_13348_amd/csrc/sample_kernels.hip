@@ -404,9 +404,9 @@ __device__ __forceinline__ u64 needed(float top_p, u64 total)
 // exponential, and the first needs no maximum in front of it.  For top-p alone and for a top-k that the list is too short
 // for: 512 x 128,000 with top-p 221 us by buckets of weights, so 110; one row of 4096 18.3, so 15.6.  (A top-k that fits
 // the list is done sooner by it: 64 x 128,000 34 us, by bins 53; without limits the passes cost as much as the weights.)
-// Returns false (all threads do) where that is not enough:
-// logits of 128 and more, a border or the maximum among those near zero, or too many of these.  Otherwise `wt` and `kept`
-// are set and sh.seg has the sums of what is kept, by segments.  Nothing is expected of sh.
+// Returns false (all threads do) where that is not enough: logits of 128 and more, a border or the maximum among those near
+// zero, or too many of these.  Otherwise `wt` and `kept` are set and sh.seg has the sums of what is kept, by segments.
+// Nothing is expected of sh.
 template <typename R>
 __device__ bool by_bins(Shared &sh, R &row, Weights &wt, Kept &kept, float temperature, int k, bool by_k, float top_p, bool by_p,
                         u64 least)
@@ -588,6 +588,10 @@ __device__ bool by_bins(Shared &sh, R &row, Weights &wt, Kept &kept, float tempe
 //   neither: nothing to find.
 // Where the lists are too short (top-k above kThreads, thousands of equal logits at a border) the border is found eight
 // bits at a time.
+// What bounds it: issue, in passes over a row by one compute unit (two at least: what is kept goes by the greatest, or by
+// what is counted).  256 x 128,000 fp32 without limits 60 us, half of it weights, 512 x 128,000 bf16 with top-p 111 (two
+// rounds, 0.23 ns a token and row), one row of 32,768 fp32 with all limits 25, where every pass waits for its loads and each
+// new piece of code for its instructions.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
 {

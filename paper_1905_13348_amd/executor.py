@@ -78,6 +78,7 @@ class PagedCache:
                          head_dim=self.head_dim, page_size=self.page_size, num_pages=self.num_pages,
                          page_stride=st[0], slot_stride=st[slot], head_stride=st[head])
         self._ref = ctypes.byref(self._c)
+        self._sizes = (self.kv_heads, self.head_dim, self.page_size)      # what a batch's caches have in common
 
 
 class Batch:
@@ -107,7 +108,8 @@ class Batch:
             d_shared_len=None if not groups else _vector(shared_len, i32, "shared_len"))
         self._ref = ctypes.byref(self._c)
         self._q_shape, self._kv_shape = (n, heads, cache.head_dim), (n, cache.kv_heads, cache.head_dim)
-        self._cache = cache      # what the plan's sizes go by (head counts, head dimension, page size)
+        self._cache = cache      # what the plan's sizes go by
+        self._sizes = cache._sizes
         size = load_library().infaas_sel_exec_plan_bytes(cache._ref, self._ref)
         if size == 0:
             _check(-1)
@@ -131,10 +133,16 @@ class Executor:
         return Batch(cache, heads, **arrays)
 
     def reserve(self, cache: PagedCache, batch: Batch) -> None:
+        self._agree(cache, batch)
         _check(self._lib.infaas_sel_exec_reserve(self._h, cache._ref, batch._ref))
 
     def plan(self, batch: Batch, stream=None) -> None:
         _check(self._lib.infaas_sel_exec_plan(self._h, batch._cache._ref, batch._ref, _stream_ptr(stream)))
+
+    @staticmethod
+    def _agree(cache: PagedCache, batch: Batch) -> None:
+        if cache._sizes != batch._sizes:
+            raise ValueError(f"a cache of (KV heads, head dimension, page size) {cache._sizes} with a batch made for {batch._sizes}")
 
     @staticmethod
     def _rows(t, cache: PagedCache, batch: Batch, shape, name: str):
@@ -151,6 +159,8 @@ class Executor:
                stream=None) -> None:
         """Keys and values into the cache, rotated by the positions; ``freq`` (float64, a frequency per rotated pair) None:
         not rotated; ``q`` and ``q_out`` both None: no queries."""
+        if cache is not batch._cache:
+            self._agree(cache, batch)
         rows, q_shape, kv_shape = self._rows, batch._q_shape, batch._kv_shape
         qp, qt, qh = (None, 0, 0) if q is None else rows(q, cache, batch, q_shape, "q")
         op, ot, oh = (None, 0, 0) if q_out is None else rows(q_out, cache, batch, q_shape, "q_out")
@@ -164,6 +174,8 @@ class Executor:
 
     def attend(self, cache: PagedCache, batch: Batch, q, out, scale: Optional[float] = None, stream=None) -> None:
         """Attention of the planned batch's tokens over the cache; ``scale`` None: head_dim ** -0.5."""
+        if cache is not batch._cache:
+            self._agree(cache, batch)
         shape = batch._q_shape
         status = self._lib.infaas_sel_exec_attend(
             self._h, cache._ref, batch._ref, *self._rows(q, cache, batch, shape, "q"),

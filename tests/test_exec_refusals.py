@@ -164,3 +164,19 @@ def test_python_side_refuses_shapes_and_types():
 def test_negative_strides_of_a_cache(lib, name):
     _refused(lib, _attend(lib, _cache(**{name: -256}), _batch()), "cache", "negative")
     _refused(lib, _append(lib, _cache(**{name: -256}), _batch()), "cache", "negative")
+
+
+def test_caches_of_other_sizes_than_the_batch():
+    """Shapes are checked by the batch's sizes, so the cache of a call has to have them."""
+    from types import SimpleNamespace
+    ex = pkg.Executor()
+    made_for = SimpleNamespace(_sizes=(2, 128, 16), _ref=None)
+    batch = SimpleNamespace(_sizes=made_for._sizes, _cache=made_for, _q_shape=(3, 8, 128), _kv_shape=(3, 2, 128), _ref=None)
+    for sizes in ((4, 128, 16), (2, 64, 16), (2, 128, 32)):
+        cache = SimpleNamespace(_sizes=sizes, _ref=None)
+        with pytest.raises(ValueError, match="KV heads"):
+            ex.append(cache, batch, None, None, None, None)
+        with pytest.raises(ValueError, match="KV heads"):
+            ex.attend(cache, batch, None, None)
+        with pytest.raises(ValueError, match="KV heads"):
+            ex.reserve(cache, batch)
