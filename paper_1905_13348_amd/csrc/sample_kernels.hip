@@ -314,28 +314,43 @@ __device__ __forceinline__ void put(Shared &sh, float x, int i)
     if (at < kMostListed) sh.list[at] = (u64)~key_of(x) << 32 | (uint32_t)i;
 }
 
-// Puts the n entries of sh.list in order, the greatest logit first, equal ones by number.
+// Puts the n entries of sh.list in order, the greatest logit first, equal ones by number.  Up to kThreads of them each find
+// their place by counting those in front of it, which takes three barriers instead of one for each step of the sort; several
+// threads share an entry's count.  (With a shorter search for the bound: one row of 32,768 fp32 with all limits 26 us, so 22.)
 __device__ void sort_list(Shared &sh, int n)
 {
+    const int tid = threadIdx.x;
     int m = 64;
     while (m < n) m *= 2;
 #pragma unroll 1
-    for (int i = n + threadIdx.x; i < m; i += kThreads) sh.list[i] = ~0ull;
+    for (int i = n + tid; i < m; i += kThreads) sh.list[i] = ~0ull;
+    if (m <= kThreads) {
+        sh.tiny[tid] = 0;
+        __syncthreads();
+        const int entry = tid & (m - 1), part = tid / m, each = m / (kThreads / m);
+        const u64 mine = sh.list[entry];
+        int before = 0;
+#pragma unroll 4
+        for (int j = 0; j < each; ++j) before += sh.list[part * each + j] < mine;
+        if (before) atomicAdd(&sh.tiny[entry], before);
+        __syncthreads();
+        if (tid < n) sh.list[sh.tiny[tid]] = mine;
+        __syncthreads();
+        return;
+    }
     __syncthreads();
 #pragma unroll 1
     for (int size = 2; size <= m; size *= 2)
 #pragma unroll 1
         for (int step = size / 2; step; step /= 2) {
-            const int t = threadIdx.x;
-            if (t < m / 2) {
-                const int i = (t / step) * step * 2 + t % step, j = i + step;
-                const bool up = (i & size) == 0;
-                const u64 x = sh.list[i], y = sh.list[j];
-                if ((x > y) == up) { sh.list[i] = y; sh.list[j] = x; }
-            }
+            const int i = (tid / step) * step * 2 + tid % step, j = i + step;
+            const bool up = (i & size) == 0;
+            const u64 x = sh.list[i], y = sh.list[j];
+            if ((x > y) == up) { sh.list[i] = y; sh.list[j] = x; }
             __syncthreads();
         }
 }
+static_assert(kMostListed == 2 * kThreads && kMostTiny >= kThreads, "");
 __device__ __forceinline__ float listed(u64 x) { return value_of(~(uint32_t)(x >> 32)); }
 
 // Of the tokens in `within`, from the greatest: the one at which the number of tokens (by_mass: the sum of their
@@ -590,7 +605,7 @@ __device__ bool by_bins(Shared &sh, R &row, Weights &wt, Kept &kept, float tempe
 // bits at a time.
 // What bounds it: issue, in passes over a row by one compute unit (two at least: what is kept goes by the greatest, or by
 // what is counted).  256 x 128,000 fp32 without limits 60 us, half of it weights, 512 x 128,000 bf16 with top-p 111 (two
-// rounds, 0.23 ns a token and row), one row of 32,768 fp32 with all limits 25, where every pass waits for its loads and each
+// rounds, 0.23 ns a token and row), one row of 32,768 fp32 with all limits 22, where every pass waits for its loads and each
 // new piece of code for its instructions.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
@@ -651,10 +666,11 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
         int n = kMostListed + 1;
         u64 inside = 0;
         if (by_k && k <= kThreads) {
-            uint32_t bound = 0;              // the k-th greatest of the threads' greatest, two bits at a time
+            // the k-th greatest of the threads' greatest, two bits at a time, or a little less: its first eighteen
+        uint32_t bound = 0;
             const uint32_t mine_key = key_of(mine);
 #pragma unroll 1
-            for (int bit = 30; bit >= (sizeof(T) == 2 ? 12 : 0); bit -= 2) {
+            for (int bit = 30; bit >= 14; bit -= 2) {
                 u64 c = 0;
 #pragma unroll
                 for (int d = 1; d < 4; ++d) c |= (u64)__popcll(__ballot(mine_key >= (bound | (uint32_t)d << bit))) << (16 * d);
