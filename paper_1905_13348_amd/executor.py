@@ -82,7 +82,9 @@ class PagedCache:
 
 
 class Batch:
-    """A step's ragged batch (infaas_sel_batch) with the memory of its plan."""
+    """A step's ragged batch (infaas_sel_batch) with the memory of its plan.  That memory is a torch tensor like the arrays:
+    it is made and cleared on torch's current stream, so calls on another stream have to wait for that one first, and a batch
+    has to be kept until the calls that use it have run."""
 
     def __init__(self, cache: PagedCache, heads: int, *, token_seq, token_pos, seq_start, seq_len, page_table,
                  group_start=None, shared_len=None, max_len: Optional[int] = None):
