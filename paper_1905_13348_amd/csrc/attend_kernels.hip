@@ -549,9 +549,14 @@ __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a)
     vec<float, 4> o = vec<float, 4>{};
     auto join = [&](float m1, float l1, vec<float, 4> o1) {
         if (m1 == -INFINITY && l1 == 0) return;        // nothing seen
+        if (m == -INFINITY && l == 0) {                // nothing so far
+            m = m1; l = l1; o = o1;
+            return;
+        }
+        // (a sum of NaN with a maximum of -infinity, of scores that are all NaN, stays NaN times 0)
         const float m2 = fmaxf(m, m1), f = exp2_fast(m - m2), g = exp2_fast(m1 - m2);
-        o = m == -INFINITY ? o1 * g : o * f + o1 * g;
-        l = m == -INFINITY ? l1 * g : l * f + l1 * g;
+        o = o * f + o1 * g;
+        l = l * f + l1 * g;
         m = m2;
     };
     if (work) {
