@@ -262,6 +262,15 @@ typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) void global_void;
 
 constexpr float kSlack = 8.0f;       // halvings
+constexpr float kFused = 4194304.0f;
+
+// s * scale - ref with the product rounded, as a maximum's is.
+__device__ __forceinline__ float apart(float s, float scale, float ref)
+{
+#pragma clang fp contract(off)
+    const float t = s * scale;
+    return t - ref;
+}
 
 // A workgroup of four waves takes items of up to 128 rows, 32 to a wave.  With K the A operand, S^T = K Q^T leaves a lane
 // with scores of ONE row (its column), so the running maximum and sum are a lane's own, and P^T is in registers where
@@ -335,6 +344,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) o[dt] = vec<float, 16>{};
         float m = -INFINITY, l = 0;
+        bool far = false;                     // a reference of the wave's is beyond kFused
 
         const int32_t *table = a.cache.table + (int64_t)it.seq * a.cache.table_width;
         auto entry = [&](int kt) {
@@ -415,19 +425,30 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
             float top = s[0][0];
 #pragma unroll
             for (int x = 1; x < 16 * NB; ++x) top = fmaxf(top, s[x / 16][x % 16]);
-            top = max_of_halves(top) * a.scale_log2;
+            top = max_of_halves(top);
             // The reference of the weights follows the maximum only when that is kSlack above it: weights up to 2^kSlack
             // lose nothing in either type, and the results are scaled once or twice a row, not whenever one of a wave's
             // rows has a new maximum (in two tiles of five over 8000 keys).
-            if (__any(top > m + kSlack)) {
-                const float m2 = fmaxf(m, top);
+            float scale = a.scale_log2;
+            float ref = m == -INFINITY ? 0.0f : m;      // (a row that has seen nothing yet)
+            if (__any(apart(top, scale, m) > kSlack) || far) {      // (not against m + kSlack, which is rounded)
+                const float m2 = fmaxf(m, top * scale);
                 const float f = m2 == -INFINITY ? 1.0f : exp2_fast(m - m2);
                 m = m2;
                 l *= f;
 #pragma unroll
                 for (int dt = 0; dt < D / 32; ++dt) o[dt] *= f;
+                ref = m == -INFINITY ? 0.0f : m;
+                // Weights are exp2 of one fused operation a score, and the reference is a product that was rounded: by less
+                // than an eighth up to 2^22, by 8 and more from 2^27 on, where a row's weights would all be infinite or 0.
+                far = __any(fabsf(m) > kFused && m > -INFINITY);
+                if (far) {
+#pragma unroll
+                    for (int x = 0; x < 16 * NB; ++x) s[x / 16][x % 16] = apart(s[x / 16][x % 16], scale, ref);
+                    scale = 1.0f;
+                    ref = 0.0f;
+                }
             }
-            const float ref = m == -INFINITY ? 0.0f : m;      // (a row that has seen nothing yet)
 #pragma unroll
             for (int kb = 0; kb < NB; ++kb) {
                 union { vec<short, 4> h[2]; vec<T, 8> v; } vf[D / 32][2];
@@ -442,7 +463,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
                 vec<T, 8> pt[2];
 #pragma unroll
                 for (int x = 0; x < 16; x += 2) {
-                    const vec<float, 2> e = {exp2_fast(s[kb][x] * a.scale_log2 - ref), exp2_fast(s[kb][x + 1] * a.scale_log2 - ref)};
+                    const vec<float, 2> e = {exp2_fast(s[kb][x] * scale - ref), exp2_fast(s[kb][x + 1] * scale - ref)};
                     l += e[0];
                     l += e[1];
                     const vec<T, 2> y = __builtin_convertvector(e, vec<T, 2>);

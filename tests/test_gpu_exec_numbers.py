@@ -52,3 +52,34 @@ def test_keys_that_are_no_numbers_in_one_item():
     k[:30, 0, 0] = torch.nan
     got, want, tol, items = _run(History(k, v), _normal((2, 2, 128), dtype, 6), 0.1, [60, 20])
     assert len(items) == 2 and np.isnan(got).all() and np.isnan(want).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("S", [3, 512])
+def test_scores_beyond_32_bits(S, dim, dtype):
+    """Scores of 2^5 to 2^40 of either sign, further apart than they are rounded: the greatest takes all, at every size.
+    (S = 512: an item has the whole history, so that its maximum moves from tile to tile.)"""
+    rng = np.random.default_rng(dim)
+    keys = 400
+    # every row's scores are its factor times the keys', which are 1% apart, in no order
+    level = np.linspace(0.02, 1, keys) * rng.choice([-1, 1])
+    level = torch.from_numpy(rng.permutation(level) * (60000.0 if dtype == torch.float16 else 3e5)).to(dtype)
+    assert len(set(level.tolist())) > 100
+    k = level.cuda()[:, None, None].expand(keys, 1, dim).contiguous()
+    v = _normal((keys, 1, dim), dtype, 15)
+    q = torch.from_numpy(np.exp(rng.uniform(np.log(1e-3), np.log(6e4), S)) * rng.choice([-1, 1], S)).to(dtype).cuda()
+    q = q[:, None, None].expand(S, 2, dim).contiguous()
+    scale = 0.3
+    got, want, tol, items = _run(History(k, v), q, scale, [keys] * S)
+    # the oracle's own weights are exact at these scores: some rows' greatest is there twice or more (rounded levels)
+    assert np.isfinite(want).all()
+    steps = torch.mm(q[:, 0, :1].double(), level.double().cuda()[None, :]) * dim * scale
+    two = torch.topk(torch.unique(level.double()).cuda()[None, :] * q[:, 0, :1].double() * dim * scale, 2, dim=1).values
+    # 32 bits err by dim * 2^-24 of the score in the sum, and the next score is further away than that and 20 more
+    clear = (two[:, 0] - two[:, 1] > 20 + dim * 2.0 ** -23 * steps.abs().amax(dim=1)).cpu().numpy()
+    assert clear.sum() >= S // 3
+    bad = ~(np.abs(got - want) <= tol)[clear]
+    assert not bad.any(), (bad.sum(), bad.size, got[clear][bad][:4], want[clear][bad][:4])
+    if S == 512:
+        assert (items[:, 3] - items[:, 2]).min() == keys
