@@ -665,6 +665,7 @@ int infaas_sel_exec_append(infaas_sel_exec_t *x, const infaas_sel_cache *cache, 
  *     out[t][h] = sum over the keys j that t sees of softmax_j(scale * q[t][h] . k[j][h']) v[j][h'],
  * h' = h / (heads / kv_heads).  Scores, their running maximum and sum, and the weighted sums are
  * kept in 32 bits; the weights are rounded to the cache's type for the product with the values.
+ * A token whose scores are all minus infinity has NaN (weights of 0 by 0), not the zeros of a token without keys.
  * Keys and values that a token does not see do not reach its result, whatever they are (infinite, NaN).
  * Query and output arrays as in infaas_sel_exec_append; `scale` is finite and positive.
  * The batch has to be planned: under a plan of other sizes every element of d_out becomes NaN.

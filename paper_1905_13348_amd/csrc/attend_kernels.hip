@@ -232,6 +232,17 @@ template <> struct Mfma<fp16_t> {
 template <int CH> __device__ __forceinline__ constexpr int key_turn(int r) { return CH == 8 ? (r >> 1) & 7 : r & 15; }
 template <int CH> __device__ __forceinline__ constexpr int value_turn(int r) { return CH == 8 ? ((r >> 1) & 1) << 2 : (r & 3) << 2; }
 
+// The maximum of a row that has seen keys, and no score but minus infinity: less than any other's, so that beside other parts
+// it counts for nothing, and alone it is told from a row that has seen no key.
+constexpr float kNothing = -3.402823466e38f;
+
+// What the weighted sum is multiplied by.  A row without any key has zeros; one with scores of minus infinity alone has weights
+// of 0 by 0, so NaN; NaN stays.
+__device__ __forceinline__ float one_by(float m, float l)
+{
+    return l > 0 ? 1.0f / l : l == 0 && m == -INFINITY ? 0.0f : NAN;
+}
+
 // exp2 on the hardware's unit: 1 ulp of 32 bits, and 0 for -infinity.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -345,6 +356,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
         for (int dt = 0; dt < D / 32; ++dt) o[dt] = vec<float, 16>{};
         float m = -INFINITY, l = 0;
         bool far = false;                     // a reference of the wave's is beyond kFused
+        int first_there = 0x7fffffff;         // the first key that is there
 
         const int32_t *table = a.cache.table + (int64_t)it.seq * a.cache.table_width;
         auto entry = [&](int kt) {
@@ -377,6 +389,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
             unsigned long long bits = ~0ull;
             __builtin_memcpy(&bits, seen[slot], sizeof(seen[slot]));
             bits = (unsigned long long)__builtin_amdgcn_readfirstlane((int)(bits >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)bits);
+            const unsigned long long any = KB == 64 ? bits : (uint32_t)bits;
+            if (any && first_there == 0x7fffffff) first_there = kt + __builtin_ctzll(any);
             // Values that nothing sees may be no numbers: zeros.  Where some rows see keys that others do not, values that
             // are no numbers are taken out, too, and added at the end where they are seen (a weight of zero would make
             // NaN of them).
@@ -516,8 +530,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
             }
         }
         l += __shfl_xor(l, 32);
+        // A sum of 0 is that of a row that sees no key, or of one whose scores are all minus infinity.
+        if (l == 0 && lim > first_there) m = kNothing;
         if (valid && it.base < 0) {
-            const float f = l > 0 ? 1.0f / l : (l == 0 ? 0.0f : l);     // (no key: zeros; NaN stays)
+            const float f = one_by(m, l);
             T *out = (T *)a.out + token * a.out_token_stride + head * a.out_head_stride;
 #pragma unroll
             for (int dt = 0; dt < D / 32; ++dt)
@@ -608,7 +624,7 @@ __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a)
         if (lane != 0) return;
         for (int s = 1; s < LANES; ++s) join(lm[sub][s], ll[sub][s], lo[sub * LANES + s][d]);
     }
-    const float f = l > 0 ? 1.0f / l : (l == 0 ? 0.0f : l);
+    const float f = one_by(m, l);
     if (work) *(vec<T, 4> *)out = vec<T, 4>{(T)(o[0] * f), (T)(o[1] * f), (T)(o[2] * f), (T)(o[3] * f)};
 }
 

@@ -55,6 +55,52 @@ def test_keys_that_are_no_numbers_in_one_item():
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("shared", [None, 64])
+@pytest.mark.parametrize("which", ["all", "first", "last", "one", "prefix"])
+def test_scores_of_minus_infinity(which, shared, dtype):
+    """Keys that take every score to minus infinity: weights of 0 beside others, NaN (0 by 0) where a row sees nothing else;
+    not the zeros of a row that sees no key."""
+    k, v = _normal((500, 2, 64), dtype, 7), _normal((500, 2, 64), dtype, 8)
+    q = _normal((5, 4, 64), dtype, 9)
+    q[:, :, 0] = 1
+    cut = {"all": slice(0, 500), "first": slice(0, 64), "last": slice(448, 500), "one": slice(0, 1), "prefix": slice(0, 200)}[which]
+    k[cut, :, 0] = -torch.inf
+    length = [500, 300, 64, 1, 200]
+    got, want, tol, _ = _run(History(k, v), q, 0.125, length, shared=shared)
+    for t, n in enumerate(length):
+        only = cut.start == 0 and n <= cut.stop
+        assert np.isnan(want[t]).all() == only
+        assert np.isnan(got[t]).all() == only, t
+    fine = np.isfinite(want)
+    assert (np.abs(got - want)[fine] <= tol[fine]).all()
+
+
+def test_scores_of_minus_infinity_on_pages_that_are_not_there():
+    """Keys on missing pages are not seen: a row that sees none beside them has zeros, a row that sees one of minus infinity
+    has NaN."""
+    k, v = _normal((320, 1, 64), torch.bfloat16, 10), _normal((320, 1, 64), torch.bfloat16, 11)
+    k[:, :, 0] = -torch.inf
+    q = torch.ones((4, 2, 64), dtype=torch.bfloat16, device="cuda")
+    h = History(k, v)
+    got, want, _, _ = _run(h, q, 0.125, [32, 33, 320, 5], missing=(0, 1))
+    assert (got[[0, 3]] == 0).all() and (want[[0, 3]] == 0).all()
+    assert np.isnan(got[[1, 2]]).all() and np.isnan(want[[1, 2]]).all()
+
+
+@pytest.mark.parametrize("new", [3, 100])
+def test_a_prompt_whose_first_key_takes_scores_to_minus_infinity(new):
+    """The first token sees nothing else: NaN; the second has the second value."""
+    k, v = _normal((new, 1, 128), torch.float16, 12), _normal((new, 1, 128), torch.float16, 13)
+    q = _normal((new, 3, 128), torch.float16, 14)
+    q[:, :, 7] = 0.5
+    k[0, 0, 7] = -torch.inf
+    got, want, tol, _ = _run(History(k, v), q, 0.1, [new], new=[new])
+    assert np.isnan(got[0]).all() and np.isnan(want[0]).all()
+    assert np.array_equal(got[1], np.broadcast_to(v[1].double().cpu().numpy(), got[1].shape))
+    assert (np.abs(got - want)[1:] <= tol[1:]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("dim", [64, 128, 256])
 @pytest.mark.parametrize("S", [3, 512])
 def test_scores_beyond_32_bits(S, dim, dtype):
