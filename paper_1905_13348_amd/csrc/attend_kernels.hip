@@ -273,6 +273,10 @@ typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) void global_void;
 
 constexpr float kSlack = 8.0f;       // halvings
+// How far below a row's maximum its reference is taken: weights of fp16 have their full bits down to 2^-14, and 131,072 keys
+// 25.5 halvings below one were counted in the sum but not in the product, 0.28% of the row.  Up to 2^15 there is room, so that
+// border is 2^-21 or less of the greatest weight.
+template <typename T> constexpr float kRaise = std::is_same<T, fp16_t>::value ? 7.0f : 0.0f;
 constexpr float kFused = 4194304.0f;
 
 // s * scale - ref with the product rounded, as a maximum's is.
@@ -354,7 +358,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
         vec<float, 16> o[D / 32];
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) o[dt] = vec<float, 16>{};
-        float m = -INFINITY, l = 0;
+        float m = -INFINITY, l = 0;           // reference and sum
         bool far = false;                     // a reference of the wave's is beyond kFused
         int first_there = 0x7fffffff;         // the first key that is there
 
@@ -440,13 +444,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
 #pragma unroll
             for (int x = 1; x < 16 * NB; ++x) top = fmaxf(top, s[x / 16][x % 16]);
             top = max_of_halves(top);
-            // The reference of the weights follows the maximum only when that is kSlack above it: weights up to 2^kSlack
-            // lose nothing in either type, and the results are scaled once or twice a row, not whenever one of a wave's
+            // The reference of the weights follows the maximum only when that is kSlack further above it than it was: weights up
+            // to 2^(kSlack + kRaise) lose nothing in either type, and the results are scaled once or twice a row, not whenever one of a wave's
             // rows has a new maximum (in two tiles of five over 8000 keys).
             float scale = a.scale_log2;
             float ref = m == -INFINITY ? 0.0f : m;      // (a row that has seen nothing yet)
-            if (__any(apart(top, scale, m) > kSlack) || far) {      // (not against m + kSlack, which is rounded)
-                const float m2 = fmaxf(m, top * scale);
+            if (__any(apart(top, scale, m) > kSlack + kRaise<T>) || far) {      // (not against a sum, which is rounded)
+                const float m2 = fmaxf(m, apart(top, scale, kRaise<T>));
                 const float f = m2 == -INFINITY ? 1.0f : exp2_fast(m - m2);
                 m = m2;
                 l *= f;

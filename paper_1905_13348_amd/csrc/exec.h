@@ -104,7 +104,7 @@ struct AttendArgs {
     int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
     float scale_log2;                // scale * log2(e)
     float *part_o;                   // [rows][head_dim]
-    float2 *part_ml;                 // [rows] running maximum (of scores in units of log 2) and sum
+    float2 *part_ml;                 // [rows] reference of the weights (of scores in units of log 2) and their sum
 };
 
 struct AppendArgs {

@@ -129,3 +129,26 @@ def test_scores_beyond_32_bits(S, dim, dtype):
     assert not bad.any(), (bad.sum(), bad.size, got[clear][bad][:4], want[clear][bad][:4])
     if S == 512:
         assert (items[:, 3] - items[:, 2]).min() == keys
+
+
+def test_small_weights_in_fp16():
+    """One key 25.5 halvings above 131,071 others: together these have 0.28% of the weight, each of them 2^-25.5.  (512
+    sequences of one history: an item has all of it.)"""
+    keys, S = 131_072, 512
+    k = torch.zeros((keys, 1, 64), dtype=torch.float16, device="cuda")
+    v = torch.ones((keys, 1, 64), dtype=torch.float16, device="cuda")
+    k[0, 0, 0], v[0] = 1, 0
+    q = torch.zeros((S, 1, 64), dtype=torch.float16, device="cuda")
+    q[:, 0, 0] = 1
+    ex = pkg.Executor()
+    h = History(k, v, page=1024)
+    cache = ex.cache(*h.pools)
+    batch, _ = h.batch(ex, cache, 1, [keys] * S)
+    got = exec_history.attend(ex, cache, batch, q, 25.5 * float(np.log(2)))
+    items = exec_history.plan_of(batch)[1]
+    ex.destroy()
+    assert (items[:, 3] - items[:, 2]).min() > keys // 2
+    rest = (keys - 1) * 2.0 ** -25.5
+    want = np.full(got.shape, rest / (1 + rest))
+    tol = tolerance(want, want, torch.float16, keys, 1.0, raised=7)
+    assert (np.abs(got - want) <= tol).all(), (got.min(), got.max(), want[0, 0, 0])
