@@ -1,4 +1,5 @@
-"""Attention where numbers end."""
+"""Attention where numbers end: keys that are no numbers and are seen, scores of minus infinity, scores beyond what 32 bits
+tell apart, weights below the normal range of fp16, rows that see nothing beside rows that do."""
 import numpy as np
 import pytest
 import torch
@@ -42,7 +43,7 @@ def test_keys_that_are_no_numbers_and_are_seen(keys, shared):
         assert np.isnan(want[t, 2:]).all() == seen[t]
         assert np.isnan(got[t, 2:]).all() == seen[t], t
     fine = np.isfinite(want)
-    assert (np.abs(got - want)[fine] <= tol[fine]).all() and (items[:, 3] - items[:, 2]).max() == 64
+    assert (np.abs(got[fine] - want[fine]) <= tol[fine]).all() and (items[:, 3] - items[:, 2]).max() == 64
 
 
 def test_keys_that_are_no_numbers_in_one_item():
@@ -72,7 +73,7 @@ def test_scores_of_minus_infinity(which, shared, dtype):
         assert np.isnan(want[t]).all() == only
         assert np.isnan(got[t]).all() == only, t
     fine = np.isfinite(want)
-    assert (np.abs(got - want)[fine] <= tol[fine]).all()
+    assert (np.abs(got[fine] - want[fine]) <= tol[fine]).all()
 
 
 def test_scores_of_minus_infinity_on_pages_that_are_not_there():
@@ -152,3 +153,79 @@ def test_small_weights_in_fp16():
     want = np.full(got.shape, rest / (1 + rest))
     tol = tolerance(want, want, torch.float16, keys, 1.0, raised=7)
     assert (np.abs(got - want) <= tol).all(), (got.min(), got.max(), want[0, 0, 0])
+
+
+def _time(f, n=5):
+    """Least of some calls, us."""
+    f()
+    best = 1e30
+    for _ in range(n):
+        a, b = torch.cuda.Event(True), torch.cuda.Event(True)
+        a.record()
+        f()
+        b.record()
+        b.synchronize()
+        best = min(best, a.elapsed_time(b) * 1e3)
+    return best
+
+
+@pytest.mark.parametrize("odd", [False, True])
+def test_padding_beside_rows_that_see_a_prefix(odd):
+    """A token of padding in a group: its own result is zeros, also where what the others see is no number, and the others'
+    tiles take the time that they take without it (within twice)."""
+    S, keys = 64, 16_384
+    k, v = _normal((keys, 2, 128), torch.bfloat16, 16), _normal((keys, 2, 128), torch.bfloat16, 17)
+    if odd:
+        v[11, 0, 3], v[5_000, 1, 4] = torch.inf, torch.nan
+    q = _normal((S, 8, 128), torch.bfloat16, 18)
+    h = History(k, v)
+    ex = pkg.Executor()
+    cache = ex.cache(*h.pools)
+    length = [keys] * S
+    pos = np.full(S, keys - 1)
+    batch, limit = h.batch(ex, cache, 8, length, shared=keys - 100, pos=pos)
+    pos[9] = -1
+    padded, padded_limit = h.batch(ex, cache, 8, length, shared=keys - 100, pos=pos)
+    for b, lim in ((batch, limit), (padded, padded_limit)):
+        got = exec_history.attend(ex, cache, b, q, 0.1)
+        want, weighted = h.reference(q, lim, 0.1)
+        fine = np.isfinite(want)
+        assert np.array_equal(got[~fine], want[~fine], equal_nan=True)
+        tol = tolerance(np.nan_to_num(want), weighted, torch.bfloat16, keys, 8.0)
+        assert (np.abs(got[fine] - want[fine]) <= tol[fine]).all()
+    assert (got[9] == 0).all()
+    out = torch.empty_like(q)
+    times = []
+    for b in (batch, padded):
+        ex.plan(b)
+        times.append(_time(lambda: ex.attend(cache, b, q, out, 0.1)))
+    ex.destroy()
+    print(times)
+    assert times[1] <= 2 * times[0], times
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_rows_that_see_nothing_of_an_item(dim):
+    """Sequences that end inside their group's prefix, and padding, beside others, with values that are no numbers behind
+    the end: each row has what it has alone."""
+    keys = 700
+    k, v = _normal((keys, 1, dim), torch.float16, 19), _normal((keys, 1, dim), torch.float16, 20)
+    k[600, 0, 1], v[300, 0, 2], v[650, 0, 3] = torch.nan, torch.inf, torch.nan
+    q = _normal((9, 2, dim), torch.float16, 21)
+    length = [700, 64, 1, 300, 301, 128, 129, 599, 600]
+    pos = [699, 63, 0, 299, 300, -1, 128, 598, 599]
+    got, want, tol, _ = _run(History(k, v), q, 0.1, length, pos=pos, shared=650)
+    ex = pkg.Executor()
+    h = History(k, v)
+    cache = ex.cache(*h.pools)
+    for t, n in enumerate(length):
+        if pos[t] < 0:
+            assert (got[t] == 0).all()
+            continue
+        one, _ = h.batch(ex, cache, 2, [n])
+        alone = exec_history.attend(ex, cache, one, q[t:t + 1], 0.1)[0]
+        fine = np.isfinite(want[t])
+        for x in (got[t], alone):
+            assert np.array_equal(x[~fine], want[t][~fine], equal_nan=True), t
+            assert (np.abs(x[fine] - want[t][fine]) <= tol[t][fine]).all(), t
+    ex.destroy()
