@@ -595,8 +595,8 @@ typedef struct {
  *
  * The arrays are DEVICE memory and may change from step to step (in a replayed graph, too) as long
  * as infaas_sel_exec_plan runs behind the change.  What cannot be is skipped: a page outside
- * 0..num_pages-1, or a key at or beyond max_len or the table's width, is not seen by any token
- * (and not written by infaas_sel_exec_append); a token that its d_token_seq and d_seq_start do not
+ * 0..num_pages-1, or a key at or beyond max_len, the table's width or 2^31 - 256, is not seen by any
+ * token (and not written by infaas_sel_exec_append); a token that its d_token_seq and d_seq_start do not
  * both place in a sequence sees nothing.  A token that sees no key gets zeros.
  */
 typedef struct {

@@ -29,6 +29,9 @@ constexpr int kFewRows = kTileRows / 2;
 constexpr int kMinChunk = 64;
 constexpr int kChunkStep = 64;
 
+// Keys of a sequence, at most: the loops over tiles count in 32 bits, and look the rows of two tiles and 112 keys more up ahead.
+constexpr int64_t kMostKeys = INT32_MAX - 255;
+
 constexpr int kDies = 8;             // workgroups go to the dies in turn, each with an L2 of its own
 // What an item costs besides its keys (queries, first loads, results), in keys.
 constexpr int kItemCost = 128;

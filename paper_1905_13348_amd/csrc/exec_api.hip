@@ -165,8 +165,8 @@ CacheArgs cache_args(const infaas_sel_cache *c, const infaas_sel_batch *b)
     a.page_stride = c->page_stride; a.slot_stride = c->slot_stride; a.head_stride = c->head_stride;
     a.table_width = b->table_width;
     a.page_shift = __builtin_ctz((unsigned)c->page_size);
-    // (what the table can hold)
-    a.max_len = (int32_t)std::min<int64_t>(b->max_len, (int64_t)b->table_width * c->page_size);
+    // (what the table can hold, and what the kernels can count a few tiles beyond)
+    a.max_len = (int32_t)std::min<int64_t>({b->max_len, (int64_t)b->table_width * c->page_size, kMostKeys});
     return a;
 }
 
