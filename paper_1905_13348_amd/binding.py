@@ -208,14 +208,17 @@ def _dev_ptr(t, n: int, name: str) -> int:
     return t.data_ptr()
 
 
-def _stream_ptr(stream) -> int:
+def _stream_ptr(stream, device: Optional[int] = None) -> int:
+    """Raw handle of a stream; None: the current one of `device`, or of the current device."""
     torch = _torch or _use_torch()
     if stream is None:
         if _raw_stream is not None:   # (what current_stream() wraps in an object: 0.2 us instead of 1)
             if not torch.cuda.is_initialized():   # (never behind a device tensor)
                 torch.cuda.init()
-            return _raw_stream(_current_device())
-        stream = torch.cuda.current_stream()
+            return _raw_stream(_current_device() if device is None else device)
+        stream = torch.cuda.current_stream(device)
+    elif device is not None and getattr(stream, "device_index", device) != device:
+        raise ValueError(f"a stream of device {stream.device_index} with a handle of device {device}")
     return int(stream.cuda_stream)
 
 

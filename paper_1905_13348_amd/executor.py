@@ -48,11 +48,11 @@ def _check(status: int) -> None:
         raise InfaasSelError(status, text)
 
 
-def _vector(t, dtype, name: str, size: Optional[int] = None) -> int:
-    """Raw pointer of a contiguous device tensor of one dimension."""
-    if not isinstance(t, _tensor()) or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous() or t.dim() != 1 \
+def _vector(t, dtype, name: str, device: int, size: Optional[int] = None) -> int:
+    """Raw pointer of a contiguous tensor of one dimension on a device."""
+    if not isinstance(t, _tensor()) or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous() or t.dim() != 1 \
             or (size is not None and t.numel() != size):
-        raise TypeError(f"{name}: contiguous {dtype} device tensor [{'any' if size is None else size}] expected")
+        raise TypeError(f"{name}: contiguous {dtype} tensor [{'any' if size is None else size}] on device {device} expected")
     return t.data_ptr()
 
 
@@ -69,9 +69,12 @@ class PagedCache:
         if k_pool.dtype not in (torch.bfloat16, torch.float16) or v_pool.dtype != k_pool.dtype \
                 or v_pool.shape != k_pool.shape or v_pool.stride() != k_pool.stride() or k_pool.stride(3) != 1:
             raise TypeError("pools of one type (bfloat16 or float16), shape and strides expected, the last one 1")
+        if k_pool.get_device() != v_pool.get_device():
+            raise TypeError("pools on one device expected")
         slot, head = (1, 2) if layout == "token" else (2, 1)
         st = k_pool.stride()
         self.k_pool, self.v_pool, self.layout, self.dtype = k_pool, v_pool, layout, k_pool.dtype
+        self.device = k_pool.get_device()
         self.kv_heads, self.head_dim = k_pool.shape[head], k_pool.shape[3]
         self.page_size, self.num_pages = k_pool.shape[slot], k_pool.shape[0]
         self._c = _Cache(d_k=k_pool.data_ptr(), d_v=v_pool.data_ptr(), type=_types()[k_pool.dtype], kv_heads=self.kv_heads,
@@ -95,19 +98,20 @@ class Batch:
             raise TypeError("group_start and shared_len belong together")
         groups = 0 if shared_len is None else shared_len.numel()
         if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2 or page_table.shape[0] != S \
-                or page_table.dtype != i32 or not page_table.is_cuda or not page_table.is_contiguous():
-            raise TypeError(f"page_table: contiguous int32 device tensor [{S}, pages] expected")
+                or page_table.dtype != i32 or page_table.get_device() != cache.device or not page_table.is_contiguous():
+            raise TypeError(f"page_table: contiguous int32 tensor [{S}, pages] on the cache's device {cache.device} expected")
+        vector = lambda t, name, size=None: _vector(t, i32, name, cache.device, size)
         width = page_table.shape[1]
         self.num_tokens, self.heads = n, heads
         self._keep = (token_seq, token_pos, seq_start, seq_len, page_table, group_start, shared_len)
         self._c = _Batch(
             num_tokens=n, num_seqs=S, num_groups=groups, heads=heads,
             max_len=min(width * cache.page_size, 0x7fffffff) if max_len is None else max_len, table_width=width,
-            d_token_seq=_vector(token_seq, i32, "token_seq"), d_token_pos=_vector(token_pos, i32, "token_pos", n),
-            d_seq_start=_vector(seq_start, i32, "seq_start", S + 1), d_seq_len=_vector(seq_len, i32, "seq_len"),
+            d_token_seq=vector(token_seq, "token_seq"), d_token_pos=vector(token_pos, "token_pos", n),
+            d_seq_start=vector(seq_start, "seq_start", S + 1), d_seq_len=vector(seq_len, "seq_len"),
             d_page_table=page_table.data_ptr(),
-            d_group_start=None if not groups else _vector(group_start, i32, "group_start", groups + 1),
-            d_shared_len=None if not groups else _vector(shared_len, i32, "shared_len"))
+            d_group_start=None if not groups else vector(group_start, "group_start", groups + 1),
+            d_shared_len=None if not groups else vector(shared_len, "shared_len"))
         self._ref = ctypes.byref(self._c)
         self._q_shape, self._kv_shape = (n, heads, cache.head_dim), (n, cache.kv_heads, cache.head_dim)
         self._cache = cache      # what the plan's sizes go by
@@ -139,18 +143,20 @@ class Executor:
         _check(self._lib.infaas_sel_exec_reserve(self._h, cache._ref, batch._ref))
 
     def plan(self, batch: Batch, stream=None) -> None:
-        _check(self._lib.infaas_sel_exec_plan(self._h, batch._cache._ref, batch._ref, _stream_ptr(stream)))
+        self._agree(batch._cache, batch)
+        _check(self._lib.infaas_sel_exec_plan(self._h, batch._cache._ref, batch._ref, _stream_ptr(stream, self.device)))
 
-    @staticmethod
-    def _agree(cache: PagedCache, batch: Batch) -> None:
-        if cache._sizes != batch._sizes:
+    def _agree(self, cache: PagedCache, batch: Batch) -> None:
+        if cache is not batch._cache and cache._sizes != batch._sizes:
             raise ValueError(f"a cache of (KV heads, head dimension, page size) {cache._sizes} with a batch made for {batch._sizes}")
+        if cache.device != self.device or batch._cache.device != self.device:
+            raise ValueError(f"an executor of device {self.device} with a cache on {cache.device} and a batch on {batch._cache.device}")
 
     @staticmethod
     def _rows(t, cache: PagedCache, batch: Batch, shape, name: str):
         """Pointer and strides of a [tokens][heads][head_dim] tensor."""
-        if t.dtype is not cache.dtype or not t.is_cuda or t.shape != shape:
-            raise TypeError(f"{name}: {cache.dtype} device tensor {list(shape)} expected")
+        if t.dtype is not cache.dtype or t.get_device() != cache.device or t.shape != shape:
+            raise TypeError(f"{name}: {cache.dtype} tensor {list(shape)} on device {cache.device} expected")
         a, b, c = t.stride()
         if c != 1:
             raise TypeError(f"{name}: the last dimension is not consecutive")
@@ -161,28 +167,28 @@ class Executor:
                stream=None) -> None:
         """Keys and values into the cache, rotated by the positions; ``freq`` (float64, a frequency per rotated pair) None:
         not rotated; ``q`` and ``q_out`` both None: no queries."""
-        if cache is not batch._cache:
+        if cache is not batch._cache or cache.device != self.device:
             self._agree(cache, batch)
         rows, q_shape, kv_shape = self._rows, batch._q_shape, batch._kv_shape
         qp, qt, qh = (None, 0, 0) if q is None else rows(q, cache, batch, q_shape, "q")
         op, ot, oh = (None, 0, 0) if q_out is None else rows(q_out, cache, batch, q_shape, "q_out")
         kp, kt, kh = rows(k, cache, batch, kv_shape, "k")
         vp, vt, vh = rows(v, cache, batch, kv_shape, "v")
-        fp, rot = (None, 0) if freq is None else (_vector(freq, _use_torch().float64, "freq"), 2 * freq.numel())
+        fp, rot = (None, 0) if freq is None else (_vector(freq, _use_torch().float64, "freq", self.device), 2 * freq.numel())
         a = _AppendArgs(qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, fp, rot, 1 if interleaved else 0)
-        status = self._lib.infaas_sel_exec_append(self._h, cache._ref, batch._ref, a, _stream_ptr(stream))
+        status = self._lib.infaas_sel_exec_append(self._h, cache._ref, batch._ref, a, _stream_ptr(stream, self.device))
         if status:
             _check(status)
 
     def attend(self, cache: PagedCache, batch: Batch, q, out, scale: Optional[float] = None, stream=None) -> None:
         """Attention of the planned batch's tokens over the cache; ``scale`` None: head_dim ** -0.5."""
-        if cache is not batch._cache:
+        if cache is not batch._cache or cache.device != self.device:
             self._agree(cache, batch)
         shape = batch._q_shape
         status = self._lib.infaas_sel_exec_attend(
             self._h, cache._ref, batch._ref, *self._rows(q, cache, batch, shape, "q"),
             *self._rows(out, cache, batch, shape, "out"), cache.head_dim ** -0.5 if scale is None else scale,
-            _stream_ptr(stream))
+            _stream_ptr(stream, self.device))
         if status:
             _check(status)
 
@@ -190,19 +196,20 @@ class Executor:
                stream=None) -> None:
         """A token of every row of logits [rows, vocab]; limits are tensors [rows] or None."""
         torch = _use_torch()
-        if not isinstance(logits, torch.Tensor) or not logits.is_cuda or logits.dim() != 2 or logits.dtype not in _types() \
+        dev = self.device
+        if not isinstance(logits, torch.Tensor) or logits.get_device() != dev or logits.dim() != 2 or logits.dtype not in _types() \
                 or (logits.shape[1] > 1 and logits.stride(1) != 1):
-            raise TypeError("logits: device tensor [rows, vocab] expected, the last dimension consecutive")
+            raise TypeError(f"logits: tensor [rows, vocab] on device {dev} expected, the last dimension consecutive")
         rows, vocab = logits.shape
         f32, i32 = torch.float32, torch.int32
         status = self._lib.infaas_sel_exec_sample(
             self._h, rows, vocab, _types()[logits.dtype], logits.data_ptr(), logits.stride(0),
-            temperature if temperature is None else _vector(temperature, f32, "temperature", rows),
-            top_k if top_k is None else _vector(top_k, i32, "top_k", rows),
-            top_p if top_p is None else _vector(top_p, f32, "top_p", rows),
-            min_p if min_p is None else _vector(min_p, f32, "min_p", rows),
-            _vector(draws, f32, "draws", rows), _vector(token, i32, "token", rows),
-            prob if prob is None else _vector(prob, f32, "prob", rows), _stream_ptr(stream))
+            temperature if temperature is None else _vector(temperature, f32, "temperature", dev, rows),
+            top_k if top_k is None else _vector(top_k, i32, "top_k", dev, rows),
+            top_p if top_p is None else _vector(top_p, f32, "top_p", dev, rows),
+            min_p if min_p is None else _vector(min_p, f32, "min_p", dev, rows),
+            _vector(draws, f32, "draws", dev, rows), _vector(token, i32, "token", dev, rows),
+            prob if prob is None else _vector(prob, f32, "prob", dev, rows), _stream_ptr(stream, self.device))
         if status:
             _check(status)
 
