@@ -48,6 +48,13 @@ def _check(status: int) -> None:
         raise InfaasSelError(status, text)
 
 
+def _i32(value: int, name: str) -> int:
+    """A size as the library takes it (ctypes would cut it to 32 bits without a word)."""
+    if not -2 ** 31 <= value < 2 ** 31:
+        raise ValueError(f"{name}: {value} is beyond 32 bits")
+    return value
+
+
 def _vector(t, dtype, name: str, device: int, size: Optional[int] = None) -> int:
     """Raw pointer of a contiguous tensor of one dimension on a device."""
     if not isinstance(t, _tensor()) or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous() or t.dim() != 1 \
@@ -77,8 +84,8 @@ class PagedCache:
         self.device = k_pool.get_device()
         self.kv_heads, self.head_dim = k_pool.shape[head], k_pool.shape[3]
         self.page_size, self.num_pages = k_pool.shape[slot], k_pool.shape[0]
-        self._c = _Cache(d_k=k_pool.data_ptr(), d_v=v_pool.data_ptr(), type=_types()[k_pool.dtype], kv_heads=self.kv_heads,
-                         head_dim=self.head_dim, page_size=self.page_size, num_pages=self.num_pages,
+        self._c = _Cache(d_k=k_pool.data_ptr(), d_v=v_pool.data_ptr(), type=_types()[k_pool.dtype], kv_heads=_i32(self.kv_heads, "KV heads"),
+                         head_dim=_i32(self.head_dim, "head dimension"), page_size=_i32(self.page_size, "page size"), num_pages=self.num_pages,
                          page_stride=st[0], slot_stride=st[slot], head_stride=st[head])
         self._ref = ctypes.byref(self._c)
         self._sizes = (self.kv_heads, self.head_dim, self.page_size)      # what a batch's caches have in common
@@ -105,8 +112,9 @@ class Batch:
         self.num_tokens, self.heads = n, heads
         self._keep = (token_seq, token_pos, seq_start, seq_len, page_table, group_start, shared_len)
         self._c = _Batch(
-            num_tokens=n, num_seqs=S, num_groups=groups, heads=heads,
-            max_len=min(width * cache.page_size, 0x7fffffff) if max_len is None else max_len, table_width=width,
+            num_tokens=_i32(n, "token_seq"), num_seqs=_i32(S, "seq_len"), num_groups=groups, heads=_i32(heads, "heads"),
+            max_len=min(width * cache.page_size, 0x7fffffff) if max_len is None else _i32(max_len, "max_len"),
+            table_width=_i32(width, "page_table"),
             d_token_seq=vector(token_seq, "token_seq"), d_token_pos=vector(token_pos, "token_pos", n),
             d_seq_start=vector(seq_start, "seq_start", S + 1), d_seq_len=vector(seq_len, "seq_len"),
             d_page_table=page_table.data_ptr(),
@@ -129,7 +137,7 @@ class Executor:
     def __init__(self, device: int = 0):
         self._h = ctypes.c_void_p()
         self._lib = load_library()
-        _check(self._lib.infaas_sel_exec_create(device, ctypes.byref(self._h)))
+        _check(self._lib.infaas_sel_exec_create(_i32(device, "device"), ctypes.byref(self._h)))
         self.device = device
 
     def cache(self, k_pool, v_pool, layout: str = "token") -> PagedCache:
@@ -174,7 +182,7 @@ class Executor:
         op, ot, oh = (None, 0, 0) if q_out is None else rows(q_out, cache, batch, q_shape, "q_out")
         kp, kt, kh = rows(k, cache, batch, kv_shape, "k")
         vp, vt, vh = rows(v, cache, batch, kv_shape, "v")
-        fp, rot = (None, 0) if freq is None else (_vector(freq, _use_torch().float64, "freq", self.device), 2 * freq.numel())
+        fp, rot = (None, 0) if freq is None else (_vector(freq, _use_torch().float64, "freq", self.device), _i32(2 * freq.numel(), "freq"))
         a = _AppendArgs(qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, fp, rot, 1 if interleaved else 0)
         status = self._lib.infaas_sel_exec_append(self._h, cache._ref, batch._ref, a, _stream_ptr(stream, self.device))
         if status:
@@ -203,7 +211,7 @@ class Executor:
         rows, vocab = logits.shape
         f32, i32 = torch.float32, torch.int32
         status = self._lib.infaas_sel_exec_sample(
-            self._h, rows, vocab, _types()[logits.dtype], logits.data_ptr(), logits.stride(0),
+            self._h, _i32(rows, "rows"), _i32(vocab, "vocab"), _types()[logits.dtype], logits.data_ptr(), logits.stride(0),
             temperature if temperature is None else _vector(temperature, f32, "temperature", dev, rows),
             top_k if top_k is None else _vector(top_k, i32, "top_k", dev, rows),
             top_p if top_p is None else _vector(top_p, f32, "top_p", dev, rows),

@@ -143,3 +143,30 @@ def test_streams(monkeypatch):
     with pytest.raises(ValueError, match="stream of device 1"):
         ex.plan(batch, stream=SimpleNamespace(cuda_stream=5, device_index=1))
     assert len(calls) == 2
+
+
+@pytest.mark.parametrize("value", [2 ** 32 + 8, 2 ** 31, -2 ** 31 - 8, 2 ** 40])
+def test_sizes_beyond_32_bits(monkeypatch, value):
+    """They would reach the library cut to 32 bits: 2^32 + 8 query heads as 8."""
+    with pytest.raises(ValueError, match="heads"):
+        pkg.Batch(_cache(), value, **_arrays())
+    with pytest.raises(ValueError, match="max_len"):
+        pkg.Batch(_cache(), 4, max_len=value, **_arrays())
+    with pytest.raises(ValueError, match="device"):
+        pkg.Executor(value)
+
+
+@pytest.mark.parametrize("size", [2 ** 32 + 8, 2 ** 31])
+def test_tensors_of_more_elements_than_32_bits(monkeypatch, size):
+    """(Of no memory: what they are refused for is looked at first.)"""
+    wide = lambda *shape, dtype=torch.int32: torch.empty(shape, dtype=dtype, device="meta")
+    ex, calls = _executor(monkeypatch)
+    with pytest.raises(ValueError, match="vocab"):
+        _sample(ex, logits=wide(2, size, dtype=torch.float32))
+    with pytest.raises(ValueError, match="rows"):
+        _sample(ex, logits=wide(size, 50, dtype=torch.float32))
+    with pytest.raises(ValueError, match="page_table"):
+        pkg.Batch(_cache(), 4, **_arrays(page_table=wide(2, size)))
+    with pytest.raises(ValueError, match="token_seq"):
+        pkg.Batch(_cache(), 4, **_arrays(token_seq=wide(size)))
+    assert calls == []
