@@ -9,7 +9,8 @@
     ex.sample(logits, draws, token, prob, top_p=...)     # behind the last layer
 
 Argument marshalling only, like ``Selector``: shapes and types are checked here, values in the library.  A cache and a
-batch keep references to their tensors; the tensors' contents may change from step to step.
+batch keep references to their tensors; the tensors' contents may change from step to step.  There is no backward pass:
+inputs that require a gradient are refused where gradients are recorded.
 """
 from __future__ import annotations
 
@@ -63,6 +64,13 @@ def _vector(t, dtype, name: str, device: int, size: Optional[int] = None) -> int
     return t.data_ptr()
 
 
+def _no_gradient(t, name: str) -> None:
+    """The calls write to tensors that they are given, and what they compute has no backward: as with torch's own outputs that
+    are given, an input that needs a gradient would lose it without a word."""
+    if t.requires_grad and _use_torch().is_grad_enabled():
+        raise RuntimeError(f"{name} requires a gradient and the executor's calls have none: call them under torch.no_grad()")
+
+
 class PagedCache:
     """One layer's pools of pages (infaas_sel_cache): ``layout`` "token" for [page][slot][head][dim], "head" for
     [page][head][slot][dim]; both pools have the same shape and strides, the last dimension consecutive."""
@@ -78,6 +86,8 @@ class PagedCache:
             raise TypeError("pools of one type (bfloat16 or float16), shape and strides expected, the last one 1")
         if k_pool.get_device() != v_pool.get_device():
             raise TypeError("pools on one device expected")
+        _no_gradient(k_pool, "k_pool")
+        _no_gradient(v_pool, "v_pool")
         slot, head = (1, 2) if layout == "token" else (2, 1)
         st = k_pool.stride()
         self.k_pool, self.v_pool, self.layout, self.dtype = k_pool, v_pool, layout, k_pool.dtype
@@ -165,6 +175,8 @@ class Executor:
         """Pointer and strides of a [tokens][heads][head_dim] tensor."""
         if t.dtype is not cache.dtype or t.get_device() != cache.device or t.shape != shape:
             raise TypeError(f"{name}: {cache.dtype} tensor {list(shape)} on device {cache.device} expected")
+        if t.requires_grad:
+            _no_gradient(t, name)
         a, b, c = t.stride()
         if c != 1:
             raise TypeError(f"{name}: the last dimension is not consecutive")
@@ -182,6 +194,8 @@ class Executor:
         op, ot, oh = (None, 0, 0) if q_out is None else rows(q_out, cache, batch, q_shape, "q_out")
         kp, kt, kh = rows(k, cache, batch, kv_shape, "k")
         vp, vt, vh = rows(v, cache, batch, kv_shape, "v")
+        if freq is not None:
+            _no_gradient(freq, "freq")
         fp, rot = (None, 0) if freq is None else (_vector(freq, _use_torch().float64, "freq", self.device), _i32(2 * freq.numel(), "freq"))
         a = _AppendArgs(qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, fp, rot, 1 if interleaved else 0)
         status = self._lib.infaas_sel_exec_append(self._h, cache._ref, batch._ref, a, _stream_ptr(stream, self.device))
@@ -208,6 +222,7 @@ class Executor:
         if not isinstance(logits, torch.Tensor) or logits.get_device() != dev or logits.dim() != 2 or logits.dtype not in _types() \
                 or (logits.shape[1] > 1 and logits.stride(1) != 1):
             raise TypeError(f"logits: tensor [rows, vocab] on device {dev} expected, the last dimension consecutive")
+        _no_gradient(logits, "logits")
         rows, vocab = logits.shape
         f32, i32 = torch.float32, torch.int32
         status = self._lib.infaas_sel_exec_sample(

@@ -170,3 +170,26 @@ def test_tensors_of_more_elements_than_32_bits(monkeypatch, size):
     with pytest.raises(ValueError, match="token_seq"):
         pkg.Batch(_cache(), 4, **_arrays(token_seq=wide(size)))
     assert calls == []
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v", "q_out", "out", "freq", "logits", "pool"])
+def test_inputs_that_require_a_gradient(monkeypatch, name):
+    """Refused where gradients are recorded, by name; taken where they are not."""
+    ex, calls = _executor(monkeypatch)
+    cache = _cache()
+    batch = pkg.Batch(cache, 4, **_arrays())
+    if name == "logits":
+        t = torch.zeros(2, 50, requires_grad=True)
+        call = lambda: _sample(ex, logits=t)
+    elif name == "pool":
+        t = _elsewhere(torch.zeros(2, 16, 2, 64, dtype=torch.bfloat16)).requires_grad_()
+        call = lambda: pkg.PagedCache(t.detach(), t)
+    else:
+        t = torch.zeros((32,) if name == "freq" else (3, 2 if name in "kv" else 4, 64),
+                        dtype=torch.float64 if name == "freq" else torch.bfloat16, requires_grad=True)
+        call = lambda: _step(ex, cache, batch, **{name: t})
+    with pytest.raises(RuntimeError, match=f"{name}.* requires a gradient"):
+        call()
+    assert len(calls) == (1 if name == "out" else 0)
+    with torch.no_grad():
+        call()
