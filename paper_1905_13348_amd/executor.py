@@ -110,6 +110,9 @@ class Batch:
                  group_start=None, shared_len=None, max_len: Optional[int] = None):
         torch = _use_torch()
         i32 = torch.int32
+        for name, t in (("token_seq", token_seq), ("seq_len", seq_len)) + ((("shared_len", shared_len),) if shared_len is not None else ()):
+            if not isinstance(t, torch.Tensor):
+                raise TypeError(f"{name}: a tensor expected, not {type(t).__name__}")
         n, S = token_seq.numel(), seq_len.numel()
         if (group_start is None) != (shared_len is None):
             raise TypeError("group_start and shared_len belong together")
@@ -173,7 +176,7 @@ class Executor:
     @staticmethod
     def _rows(t, cache: PagedCache, batch: Batch, shape, name: str):
         """Pointer and strides of a [tokens][heads][head_dim] tensor."""
-        if t.dtype is not cache.dtype or t.get_device() != cache.device or t.shape != shape:
+        if not isinstance(t, _tensor_class or _tensor()) or t.dtype is not cache.dtype or t.get_device() != cache.device or t.shape != shape:
             raise TypeError(f"{name}: {cache.dtype} tensor {list(shape)} on device {cache.device} expected")
         if t.requires_grad:
             _no_gradient(t, name)
@@ -194,9 +197,10 @@ class Executor:
         op, ot, oh = (None, 0, 0) if q_out is None else rows(q_out, cache, batch, q_shape, "q_out")
         kp, kt, kh = rows(k, cache, batch, kv_shape, "k")
         vp, vt, vh = rows(v, cache, batch, kv_shape, "v")
+        fp, rot = None, 0
         if freq is not None:
+            fp, rot = _vector(freq, _use_torch().float64, "freq", self.device), _i32(2 * freq.numel(), "freq")
             _no_gradient(freq, "freq")
-        fp, rot = (None, 0) if freq is None else (_vector(freq, _use_torch().float64, "freq", self.device), _i32(2 * freq.numel(), "freq"))
         a = _AppendArgs(qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, fp, rot, 1 if interleaved else 0)
         status = self._lib.infaas_sel_exec_append(self._h, cache._ref, batch._ref, a, _stream_ptr(stream, self.device))
         if status:

@@ -193,3 +193,27 @@ def test_inputs_that_require_a_gradient(monkeypatch, name):
     assert len(calls) == (1 if name == "out" else 0)
     with torch.no_grad():
         call()
+
+
+@pytest.mark.parametrize("what", [None, [0, 1], 3.0])
+def test_what_is_no_tensor(monkeypatch, what):
+    """Named, as a wrong type is."""
+    ex, calls = _executor(monkeypatch)
+    cache = _cache()
+    batch = pkg.Batch(cache, 4, **_arrays())
+    for name in ("token_seq", "token_pos", "seq_start", "seq_len", "page_table"):
+        with pytest.raises(TypeError, match=name):
+            pkg.Batch(cache, 4, **_arrays(**{name: what}))
+    for name in ("k", "v", "out") + (("q", "q_out", "freq") if what is not None else ()):      # (None: without queries, not rotated)
+        calls.clear()
+        with pytest.raises(TypeError, match=name):
+            _step(ex, cache, batch, **{name: what})
+        assert len(calls) == (1 if name == "out" else 0)
+    for name in ("logits", "draws", "token"):
+        with pytest.raises(TypeError, match=name):
+            _sample(ex, **{name: what})
+    with pytest.raises(TypeError):
+        pkg.PagedCache(what, torch.zeros(2, 16, 2, 64, dtype=torch.bfloat16))
+    if what is not None:
+        with pytest.raises(TypeError, match="shared_len"):
+            pkg.Batch(cache, 4, **_arrays(shared_len=what))
