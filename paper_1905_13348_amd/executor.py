@@ -81,15 +81,16 @@ class PagedCache:
             raise ValueError(f"layout {layout!r}: 'token' or 'head'")
         if not all(isinstance(p, torch.Tensor) and p.is_cuda and p.dim() == 4 for p in (k_pool, v_pool)):
             raise TypeError("device tensors of four dimensions expected")
+        # (a dimension of one element has a stride of no meaning)
+        st, vst = ([0 if n == 1 else x for n, x in zip(p.shape, p.stride())] for p in (k_pool, v_pool))
         if k_pool.dtype not in (torch.bfloat16, torch.float16) or v_pool.dtype != k_pool.dtype \
-                or v_pool.shape != k_pool.shape or v_pool.stride() != k_pool.stride() or k_pool.stride(3) != 1:
+                or v_pool.shape != k_pool.shape or st != vst or k_pool.stride(3) != 1:
             raise TypeError("pools of one type (bfloat16 or float16), shape and strides expected, the last one 1")
         if k_pool.get_device() != v_pool.get_device():
             raise TypeError("pools on one device expected")
         _no_gradient(k_pool, "k_pool")
         _no_gradient(v_pool, "v_pool")
         slot, head = (1, 2) if layout == "token" else (2, 1)
-        st = k_pool.stride()
         self.k_pool, self.v_pool, self.layout, self.dtype = k_pool, v_pool, layout, k_pool.dtype
         self.device = k_pool.get_device()
         self.kv_heads, self.head_dim = k_pool.shape[head], k_pool.shape[3]

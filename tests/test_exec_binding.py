@@ -217,3 +217,15 @@ def test_what_is_no_tensor(monkeypatch, what):
     if what is not None:
         with pytest.raises(TypeError, match="shared_len"):
             pkg.Batch(cache, 4, **_arrays(shared_len=what))
+
+
+def test_pools_with_dimensions_of_one_element():
+    """Their strides mean nothing: neither compared nor asked to be multiples of 8."""
+    k = _elsewhere(torch.zeros(1, 16, 1, 64, dtype=torch.bfloat16))
+    v = _elsewhere(torch.zeros(16 * 64, dtype=torch.bfloat16).as_strided((1, 16, 1, 64), (5, 64, 3, 1)))
+    c = pkg.PagedCache(k, v)._c
+    assert (c.page_stride, c.slot_stride, c.head_stride) == (0, 64, 0)
+    c = pkg.PagedCache(v, k, layout="head")._c
+    assert (c.page_stride, c.slot_stride, c.head_stride) == (0, 0, 64)
+    with pytest.raises(TypeError, match="strides"):
+        pkg.PagedCache(k, _elsewhere(torch.zeros(2048, dtype=torch.bfloat16).as_strided((1, 16, 1, 64), (5, 72, 3, 1))))
