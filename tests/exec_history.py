@@ -28,9 +28,9 @@ class History:
             self.pools.append(mixed)
         self.row = order
 
-    def batch(self, ex, cache, heads, length, new=None, pos=None, missing=(), shared=None, max_len=None):
+    def batch(self, ex, cache, heads, length, new=None, pos=None, missing=(), shared=None, groups=None, max_len=None):
         """A token to every sequence (or `new` of them), the last of its keys; `missing`: pages (of the history) that are not
-        there; `shared`: keys that all of them share as a group."""
+        there; `shared`: keys that all of them share as a group, or with `groups` (first sequences and the end) each group."""
         S = len(length)
         length = np.asarray(length, dtype=np.int64)
         new = np.ones(S, dtype=np.int64) if new is None else np.asarray(new)
@@ -40,7 +40,9 @@ class History:
             pos = (length - new)[seq] + np.arange(len(seq)) - start[seq]
         row = self.row.copy()
         row[list(missing)] = -1
-        groups = {} if shared is None else dict(group_start=i32([0, S]), shared_len=i32([shared]))
+        if shared is not None and groups is None:
+            groups, shared = [0, S], [shared]
+        groups = {} if shared is None else dict(group_start=i32(groups), shared_len=i32(shared))
         batch = ex.batch(cache, heads, token_seq=i32(seq), token_pos=i32(pos), seq_start=i32(start), seq_len=i32(length),
                          page_table=i32(np.tile(row, (S, 1))), max_len=int(length.max()) if max_len is None else max_len, **groups)
         return batch, np.minimum(np.asarray(pos) + 1, length[seq])
