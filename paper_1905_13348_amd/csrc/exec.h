@@ -127,6 +127,9 @@ struct SampleArgs {
     float *prob;
 };
 
+// Workgroups of a launch, at most: a grid of 2^32 threads and more is cut to its low 32 bits without an error.
+constexpr int64_t kMostGroups = 1 << 16;
+
 hipError_t launch_plan(const BatchArgs &b, const CacheArgs &c, const PlanView &p, const PlanSizes &z, hipStream_t s);
 hipError_t launch_attend(const AttendArgs &a, int32_t type, int64_t max_items, hipStream_t s);
 hipError_t launch_append(const AppendArgs &a, int32_t type, hipStream_t s);

@@ -1,6 +1,7 @@
 // Drawing a token of every row of logits (infaas_sel_exec_sample).
 #include "exec.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace infaas {
@@ -608,10 +609,10 @@ __device__ bool by_bins(Shared &sh, R &row, Weights &wt, Kept &kept, float tempe
 // rounds, 0.23 ns a token and row), one row of 32,768 fp32 with all limits 22, where every pass waits for its loads and each
 // new piece of code for its instructions.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
+__global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a, int first)
 {
     __shared__ Shared sh;
-    const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), V = a.vocab;
+    const int r = first + blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), V = a.vocab;
     Row<T> row;
     row.init((const T *)a.logits + r * a.row_stride, V);
     const int segs = row.segments;
@@ -762,10 +763,14 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a)
 
 hipError_t launch_sample(const SampleArgs &a, int32_t type, hipStream_t s)
 {
-    if (type == INFAAS_SEL_TYPE_FP32) k_sample<float><<<a.rows, kThreads, 0, s>>>(a);
-    else if (type == INFAAS_SEL_TYPE_BF16) k_sample<bf16_t><<<a.rows, kThreads, 0, s>>>(a);
-    else k_sample<fp16_t><<<a.rows, kThreads, 0, s>>>(a);
-    return hipGetLastError();
+    for (int64_t first = 0; first < a.rows; first += kMostGroups) {
+        const dim3 grid((unsigned)std::min(kMostGroups, a.rows - first));
+        if (type == INFAAS_SEL_TYPE_FP32) k_sample<float><<<grid, kThreads, 0, s>>>(a, (int)first);
+        else if (type == INFAAS_SEL_TYPE_BF16) k_sample<bf16_t><<<grid, kThreads, 0, s>>>(a, (int)first);
+        else k_sample<fp16_t><<<grid, kThreads, 0, s>>>(a, (int)first);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace infaas
