@@ -2,6 +2,7 @@
 // the plan, the items and the merge of their results.
 #include "exec.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace infaas {
@@ -578,13 +579,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
 // L2 and memory: 80,000 rows of three splits 26 us.  One row to a workgroup for few rows
 // (which may have a hundred splits each), as many as fit for many: those 80,000 rows took 145 us with one row each.
 template <typename T, int D, int ROWS>
-__global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a)
+__global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a, int64_t first_item)
 {
     constexpr int W = D / 4, LANES = 256 / W / ROWS;
     __shared__ float lm[ROWS][LANES], ll[ROWS][LANES];
     __shared__ vec<float, 4> lo[LANES > 1 ? ROWS * LANES : 1][W];
     const int sub = threadIdx.x / (W * LANES), d = threadIdx.x % W, lane = threadIdx.x / W % LANES;
-    const int64_t item = (int64_t)blockIdx.x * ROWS + sub;
+    const int64_t item = first_item + (int64_t)blockIdx.x * ROWS + sub;
     const bool there = item < (int64_t)a.batch.num_tokens * a.batch.heads;
     const int token = there ? (int)(item / a.batch.heads) : 0, head = there ? (int)(item % a.batch.heads) : 0;
     T *out = (T *)a.out + token * a.out_token_stride + head * a.out_head_stride + d * 4;
@@ -649,11 +650,18 @@ hipError_t attend(const AttendArgs &a, int64_t max_items, hipStream_t s)
     const int grid = ((int)(max_items < 1024 ? 2 * max_items : 2048) / kDies + 1) * kDies;
     k_attend_items<T, D><<<grid, 256, 0, s>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
-    const unsigned rows = (unsigned)a.batch.num_tokens * a.batch.heads;
+    const int64_t rows = (int64_t)a.batch.num_tokens * a.batch.heads;
     constexpr int MANY = 256 / (D / 4);
-    if (rows < 32768) k_attend_merge<T, D, 1><<<rows, 256, 0, s>>>(a);
-    else k_attend_merge<T, D, MANY><<<(rows + MANY - 1) / MANY, 256, 0, s>>>(a);
-    return hipGetLastError();
+    if (rows < 32768) {
+        k_attend_merge<T, D, 1><<<(unsigned)rows, 256, 0, s>>>(a, 0);
+        return hipGetLastError();
+    }
+    for (int64_t first = 0; first < rows; first += kMostGroups * MANY) {
+        const dim3 grid((unsigned)std::min(kMostGroups, (rows - first + MANY - 1) / MANY));
+        k_attend_merge<T, D, MANY><<<grid, 256, 0, s>>>(a, first);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
 }
 
 template <typename T>

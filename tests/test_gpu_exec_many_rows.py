@@ -1,7 +1,9 @@
 """Batches whose rows are more than a launch's grid can hold."""
+import numpy as np
 import pytest
 import torch
 
+import exec_history
 import paper_1905_13348_amd as pkg
 
 pytestmark = pytest.mark.gpu
@@ -21,3 +23,19 @@ def test_draws_of_many_rows(rows):
     torch.cuda.synchronize()
     ex.destroy()
     assert torch.equal(token.long(), which) and bool((prob == 1).all())
+
+
+def test_attention_of_many_rows():
+    """8200 tokens of 128 heads behind a short prefix: 1,049,600 rows to merge, more than 65,536 workgroups of 16."""
+    tokens, heads, dim, dtype = 8_200, 128, 64, torch.bfloat16
+    normal = lambda shape, seed: torch.randn(shape, generator=torch.Generator().manual_seed(seed)).to(dtype).cuda()
+    h = exec_history.History(normal((40, 1, dim), 1), normal((40, 1, dim), 2))
+    q = normal((tokens, heads, dim), 3)
+    length = 1 + np.arange(tokens) % 40
+    ex = pkg.Executor()
+    cache = ex.cache(*h.pools)
+    batch, limit = h.batch(ex, cache, heads, length, shared=7)
+    got = exec_history.attend(ex, cache, batch, q, 0.125)
+    ex.destroy()
+    want, weighted = h.reference(q, limit, 0.125)
+    assert (np.abs(got - want) <= exec_history.tolerance(want, weighted, dtype, 40, 6.0)).all()
