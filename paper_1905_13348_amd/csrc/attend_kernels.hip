@@ -59,9 +59,13 @@ __device__ __forceinline__ UnitRange unit_range(const BatchArgs &b, const CacheA
     return r;
 }
 
-// One workgroup.  The cost of a tile is its keys; chunks are as long as makes so many items of all tiles, and the same for
-// all, so that items are of one length but for the last of each tile.  How many depends on the rows of the tiles (their
-// mean by cost): see kFewItems.  10 us for few sequences, 18 for 256 behind prefixes: once a step, for all layers.
+// One workgroup.  The cost of a tile is its keys; chunks are as long as would make so many items if tiles could be cut
+// anywhere, and the same for all, so that items are of one length but for the last of each tile (and there are more of them:
+// one at least to every tile).  How many depends on the rows of the tiles (their mean by cost): see kFewItems.
+// 9 to 11 us for few sequences, 16 to 20 for 256 behind prefixes or four prompts of 2048: once a step, for all layers.
+// The cost counts all keys of a sequence, also those behind a tile's tokens.  Behind a long prefix that is nothing; of a prompt
+// alone the dies' work is uneven (1024 tokens of 32 heads on 8: from 2.1 to 0.02 of the mean, 45 us), below 4096
+// tokens, from which on a tile is one item.
 __global__ __launch_bounds__(kPlanThreads) void k_plan(BatchArgs b, CacheArgs c, PlanView p, int max_items, int max_rows)
 {
     __shared__ unsigned long long cost, row_cost;
@@ -296,10 +300,12 @@ __device__ __forceinline__ float apart(float s, float scale, float ref)
 // two trips to memory in a row take longer than a tile.
 // What bounds it (bf16, 32 query heads on 8 KV heads of 128 dimensions; both kernels together): memory where few rows see
 // many keys, one token behind 131,072 keys 107 us, 5.0 TB/s, 256 tokens behind four prefixes of up to 32,768 and own parts of
-// up to 2048 370 us, 4.8 TB/s (a large copy: 4.9); issue where tiles are full, prompts of up to 512 tokens behind 16,000 keys
-// (fp16, on 4 KV heads) 853 us, 730 TFLOP/s: the matrix units work half of the time, 7.5 other vector instructions come
-// to a product, and two waves on a SIMD do not hide all of them.  Few short sequences wait for the chain of loads from the
-// plan to the first tile: four of up to 700 keys 11.9 us, 4.4 of them the merge's.
+// up to 2048 370 to 380 us, 4.7 TB/s (a large copy: 4.9); issue where tiles are full, prompts of up to 512 tokens behind 16,000
+// keys (fp16, on 4 KV heads) 830 to 880 us from card to card, 710 to 750 TFLOP/s: 6.5 other vector instructions come to a
+// product, the matrix units work 47% of the time and the vector units 50%, so hardly anything of one is hidden behind the
+// other.  Few short sequences wait for the chain of loads from the plan to the first tile: four of up to 700 keys 11.1 us, of
+// kernels 7.5 and the merge's 4.4.  64 dimensions: 131,072 keys 50 us, prompts 500; 256 (255 + 166 registers, one wave to a
+// SIMD): 232 and 2470.
 template <typename T, int D>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendArgs a)
 {
@@ -324,9 +330,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
 
     // Workgroups go to the dies in turn; each die takes a stretch of the groups' items, and behind them one of the
     // sequences', so that neighbouring items (the tiles that read the same keys) meet in one L2 and are there at the same
-    // time.  Stretches are of equal cost.  Of 256 sequences behind 32k prefixes: one stretch of both kinds to a die 458 us
+    // time.  Stretches are of equal cost as the plan counts it.  Of 256 sequences behind 32k prefixes: one stretch of both kinds to a die 458 us
     // (some dies wait for their products, the others for an eighth of the memory's rate each), the kinds in turns 511 (tiles
-    // of the same keys drift apart), this 443.
+    // of the same keys drift apart), this 443.  (All three before other changes.)
     const int die = blockIdx.x & (kDies - 1), step = gridDim.x / kDies;
     const int first0 = a.plan.head->die_start[0][die], first1 = a.plan.head->die_start[1][die];
     const int n0 = a.plan.head->die_start[0][die + 1] - first0, n = n0 + a.plan.head->die_start[1][die + 1] - first1;
@@ -487,6 +493,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
                     const vec<float, 2> e = {exp2_fast(s[kb][x] * scale - ref), exp2_fast(s[kb][x + 1] * scale - ref)};
                     l += e[0];
                     l += e[1];
+                    // Rounded to 16 bits, half a step each, because the matrix instruction takes both sides in one type; the sum
+                    // takes them before.  Against 64 bits results are then off by 2.3e-3 of their norm in bf16 and 2.9e-4
+                    // in fp16, where weights of 32 bits give 1.7e-3 and 2.1e-4 (the rounding of the result alone).  What is
+                    // left of each weight in a second product would double the products with the values.
                     const vec<T, 2> y = __builtin_convertvector(e, vec<T, 2>);
                     pt[x / 8][x % 8] = y[0];
                     pt[x / 8][x % 8 + 1] = y[1];
@@ -576,7 +586,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
 
 // D/4 threads side by side take four dimensions of a (token, query head) each.  A workgroup takes ROWS of those; the
 // threads that are left over take further splits, merged through LDS at the end.  Bound by the reads of the results, from
-// L2 and memory: 80,000 rows of three splits 26 us.  One row to a workgroup for few rows
+// L2 and memory: 80,000 rows of three splits 25 us.  One row to a workgroup for few rows
 // (which may have a hundred splits each), as many as fit for many: those 80,000 rows took 145 us with one row each.
 template <typename T, int D, int ROWS>
 __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a, int64_t first_item)

@@ -597,17 +597,21 @@ __device__ bool by_bins(Shared &sh, R &row, Weights &wt, Kept &kept, float tempe
 
 // A workgroup per row: the greatest logit, then what is kept, by whichever way is short for the row's limits, with the
 // sums of its weights by segments, then the segment that the draw falls into.
-//   top-k up to kThreads: the k-th of the threads' greatest logits is a bound that k tokens at least reach, and few more;
-//     those are listed, put in order, and cut by all limits there.
+//   top-k up to kThreads: the k-th of the threads' greatest logits is a bound that k tokens at least reach; those are
+//     listed, put in order, and cut by all limits there.  For small k they are few more than k.  From some 85% of the threads
+//     that hold tokens on (64 for each 1024 tokens, up to 1024) the list is too short, and what follows comes on top:
+//     one row of 128,000 with a top-k of 200 31 us, 832 53, 896 to 1024 212 in bf16 (1025, by value, 52).
 //   top-p alone: of bf16 by value (by_bins); else weights summed into buckets of logits; the bucket that the border is in is
 //     listed and put in order.
 //   neither: nothing to find.
-// Where the lists are too short (top-k above kThreads, thousands of equal logits at a border) the border is found eight
-// bits at a time.
-// What bounds it: issue, in passes over a row by one compute unit (two at least: what is kept goes by the greatest, or by
-// what is counted).  256 x 128,000 fp32 without limits 60 us, half of it weights, 512 x 128,000 bf16 with top-p 111 (two
-// rounds, 0.23 ns a token and row), one row of 32,768 fp32 with all limits 22, where every pass waits for its loads and each
-// new piece of code for its instructions.
+// Where the lists are too short (top-k near and above kThreads, thousands of equal logits at a border) the border is found eight
+// bits at a time (one row of 128,000 fp32 or fp16 with a top-k of 1025: 170 us).
+// What bounds it: passes over a row by one compute unit (two at least: what is kept goes by the greatest, or by what is
+// counted), which holds one workgroup (94 to 106 registers) and so has nothing else to do at a row's barriers and ends.
+// 256 x 128,000 fp32 without limits 60 us: vector instructions take 61% of the busy compute units' time, the waves wait for
+// 43% of theirs.  512 x 128,000 bf16 with top-p 110 (two rounds, 0.23 ns a token and row): 69%, and LDS 40%, half of that
+// conflicts; fp16 200 and fp32 218, by buckets.  One row of 32,768 fp32 with all limits 22, where every pass waits for its
+// loads and each new piece of code for its instructions.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a, int first)
 {
@@ -668,7 +672,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(SampleArgs a, int first)
         u64 inside = 0;
         if (by_k && k <= kThreads) {
             // the k-th greatest of the threads' greatest, two bits at a time, or a little less: its first eighteen
-        uint32_t bound = 0;
+            uint32_t bound = 0;
             const uint32_t mine_key = key_of(mine);
 #pragma unroll 1
             for (int bit = 30; bit >= 14; bit -= 2) {
