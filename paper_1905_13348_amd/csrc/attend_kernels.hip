@@ -282,7 +282,7 @@ constexpr float kSlack = 8.0f;       // halvings
 // 25.5 halvings below one were counted in the sum but not in the product, 0.28% of the row.  Up to 2^15 there is room, so that
 // border is 2^-21 or less of the greatest weight.
 template <typename T> constexpr float kRaise = std::is_same<T, fp16_t>::value ? 7.0f : 0.0f;
-constexpr float kFused = 4194304.0f;
+constexpr float kFused = 4194304.0f; // 2^22: references beyond it and products that are not rounded do not go together
 
 // s * scale - ref with the product rounded, as a maximum's is.
 __device__ __forceinline__ float apart(float s, float scale, float ref)
@@ -453,9 +453,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
 #pragma unroll
             for (int x = 1; x < 16 * NB; ++x) top = fmaxf(top, s[x / 16][x % 16]);
             top = max_of_halves(top);
-            // The reference of the weights follows the maximum only when that is kSlack further above it than it was: weights up
-            // to 2^(kSlack + kRaise) lose nothing in either type, and the results are scaled once or twice a row, not whenever one of a wave's
-            // rows has a new maximum (in two tiles of five over 8000 keys).
+            // The reference of the weights follows the maximum only when that is kSlack further above it than it was: weights
+            // up to 2^(kSlack + kRaise) lose nothing in either type, and the results are scaled once or twice a row, not
+            // whenever one of a wave's rows has a new maximum (in two tiles of five over 8000 keys).
             float scale = a.scale_log2;
             float ref = m == -INFINITY ? 0.0f : m;      // (a row that has seen nothing yet)
             if (__any(apart(top, scale, m) > kSlack + kRaise<T>) || far) {      // (not against a sum, which is rounded)
