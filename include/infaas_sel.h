@@ -677,6 +677,54 @@ int infaas_sel_exec_attend(infaas_sel_exec_t *x, const infaas_sel_cache *cache, 
                            float scale, void *hip_stream);
 
 /*
+ * A layer's cache in 8 bits: the pools of an infaas_sel_cache hold codes of e4m3 (sign, 4 bits of exponent with a bias of 7,
+ * 3 of fraction; up to 448; 0x7f and 0xff are NaN), a byte each, and every `block` keys of a page have one scale to each head,
+ * for keys and for values: a byte e that stands for 2^(e - 127), 255 for NaN.  Key i of head j on page p is
+ *     code * 2^(d_k_scale[p * page_stride + i / block * block_stride + j * head_stride] - 127),
+ * as a number of the cache's `type`, which is that of the queries: exact but where that type ends (fp16: infinite from
+ * 65520 on, rounded below 2^-14).  The cache's strides are multiples of 16 (bytes).  A power of two costs e4m3 nothing but
+ * range at its lower end, and makes products with it exact.
+ */
+typedef struct {
+    void *d_k_scale, *d_v_scale;    /* DEVICE, bytes */
+    int32_t block;                  /* keys to a scale: a power of two, at most the page size */
+    int32_t pad;
+    int64_t page_stride;            /* strides in bytes, not negative */
+    int64_t block_stride;
+    int64_t head_stride;
+} infaas_sel_scales;
+
+/*
+ * infaas_sel_exec_append into a cache of 8 bits.  A block's scale becomes the least that holds every finite number of
+ * the step's tokens in it (|x| <= 448 * 2^(e - 127); at least 1), or stays the one that it has if that is greater and the step
+ * does not begin the block; where it rises, the codes of the block's earlier keys are rounded again to the new one.
+ * Numbers are rounded once, from 32 bits, to the nearest code (ties to even); infinities and NaN become NaN.  What the block
+ * holds behind the step's last token is left as it is.
+ * The tokens of a sequence stand one behind the other: token t of sequence s is at position
+ * d_token_pos[d_seq_start[s]] + t - d_seq_start[s].  One whose d_token_pos is another (padding at the end, say) is not written, nor
+ * are those of a sequence whose first token has none.  A block belongs to one sequence of the batch (a page that several
+ * share is full, or copied first: infaas_sel_exec_advance).  Needs d_seq_start as well.  Errors: INVALID_ARG, HIP.
+ */
+int infaas_sel_exec_append_scaled(infaas_sel_exec_t *x, const infaas_sel_cache *cache, const infaas_sel_scales *scales,
+                                  const infaas_sel_batch *batch, const infaas_sel_append_args *args, void *hip_stream);
+
+/* infaas_sel_exec_attend over a cache of 8 bits: the same plan, the same result as over a cache that holds those numbers in
+ * the queries' type, up to the order of its sums.  Errors: INVALID_ARG, HIP, OOM. */
+int infaas_sel_exec_attend_scaled(infaas_sel_exec_t *x, const infaas_sel_cache *cache, const infaas_sel_scales *scales,
+                                  const infaas_sel_batch *batch, const void *d_q, int64_t q_token_stride, int64_t q_head_stride,
+                                  void *d_out, int64_t out_token_stride, int64_t out_head_stride, float scale, void *hip_stream);
+
+/*
+ * Take keys and values out of a cache again (to move a sequence to another worker or into a cache of another width): those at
+ * the batch's tokens' positions, [n][kv_heads][head_dim] of the cache's type, strided and aligned as in infaas_sel_exec_append.
+ * A token without a place (as there) gets zeros.  `scales` is null for a cache of 16 bits.
+ * Needs d_token_seq, d_token_pos and d_page_table of the batch, and no plan.  Errors: INVALID_ARG, HIP.
+ */
+int infaas_sel_exec_read(infaas_sel_exec_t *x, const infaas_sel_cache *cache, const infaas_sel_scales *scales,
+                         const infaas_sel_batch *batch, void *d_k, int64_t k_token_stride, int64_t k_head_stride,
+                         void *d_v, int64_t v_token_stride, int64_t v_head_stride, void *hip_stream);
+
+/*
  * Draw a token of every row of logits.  In row r the tokens are ordered by logit, the greatest
  * first, equal ones by number; weight w_i = exp((x_i - max x) / temperature).  Kept are, in this order,
  *     the first top_k,                                                    (0 or less: all)

@@ -64,6 +64,11 @@ class _Cache(ctypes.Structure):
                 ("page_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
+class _Scales(ctypes.Structure):
+    _fields_ = [("d_k_scale", ctypes.c_void_p), ("d_v_scale", ctypes.c_void_p), ("block", ctypes.c_int32), ("pad", ctypes.c_int32),
+                ("page_stride", ctypes.c_int64), ("block_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
 class _Batch(ctypes.Structure):
     _fields_ = [("num_tokens", ctypes.c_int32), ("num_seqs", ctypes.c_int32), ("num_groups", ctypes.c_int32),
                 ("heads", ctypes.c_int32), ("max_len", ctypes.c_int32), ("table_width", ctypes.c_int32),
@@ -91,7 +96,8 @@ EXPORTED = ("infaas_sel_create", "infaas_sel_load_variants", "infaas_sel_update_
             "infaas_sel_read_load", "infaas_sel_set_timing", "infaas_sel_get_timings",
             "infaas_sel_get_info", "infaas_sel_strerror", "infaas_sel_last_error",
             "infaas_sel_exec_create", "infaas_sel_exec_destroy", "infaas_sel_exec_plan_bytes", "infaas_sel_exec_reserve",
-            "infaas_sel_exec_plan", "infaas_sel_exec_append", "infaas_sel_exec_attend", "infaas_sel_exec_sample")
+            "infaas_sel_exec_plan", "infaas_sel_exec_append", "infaas_sel_exec_attend", "infaas_sel_exec_sample",
+            "infaas_sel_exec_append_scaled", "infaas_sel_exec_attend_scaled", "infaas_sel_exec_read")
 
 
 def library_path() -> str:
@@ -156,6 +162,10 @@ def load_library() -> ctypes.CDLL:
     lib.infaas_sel_exec_append.argtypes = [vp, cp, bp, ctypes.POINTER(_AppendArgs), vp]
     lib.infaas_sel_exec_attend.argtypes = [vp, cp, bp, vp, i64, i64, vp, i64, i64, ctypes.c_float, vp]
     lib.infaas_sel_exec_sample.argtypes = [vp, i32, i32, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]
+    sp = ctypes.POINTER(_Scales)
+    lib.infaas_sel_exec_append_scaled.argtypes = [vp, cp, sp, bp, ctypes.POINTER(_AppendArgs), vp]
+    lib.infaas_sel_exec_attend_scaled.argtypes = [vp, cp, sp, bp, vp, i64, i64, vp, i64, i64, ctypes.c_float, vp]
+    lib.infaas_sel_exec_read.argtypes = [vp, cp, sp, bp, vp, i64, i64, vp, i64, i64, vp]
     for name in EXPORTED:
         if name not in ("infaas_sel_destroy", "infaas_sel_strerror", "infaas_sel_last_error", "infaas_sel_exec_destroy",
                         "infaas_sel_exec_plan_bytes"):

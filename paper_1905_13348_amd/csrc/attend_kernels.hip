@@ -306,12 +306,17 @@ __device__ __forceinline__ float apart(float s, float scale, float ref)
 // other.  Few short sequences wait for the chain of loads from the plan to the first tile: four of up to 700 keys 11.1 us, of
 // kernels 7.5 and the merge's 4.4.  64 dimensions: 131,072 keys 50 us, prompts 500; 256 (255 + 166 registers, one wave to a
 // SIMD): 232 and 2470.
-template <typename T, int D>
+// CODED: the cache has codes of 8 bits and scales.  A tile's codes then come into registers, and are written to LDS as numbers
+// of T when the tile's turn comes: half the bytes from memory, and a conversion of two numbers to an instruction, which the
+// waves share.
+template <typename T, int D, bool CODED>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendArgs a)
 {
     constexpr int KB = D == 256 ? 32 : 64, CH = D / 8, LOADS = KB * CH / 256, ROW = D * 2;
+    constexpr int PIECE = CODED ? 16 : 8, CODE_LOADS = LOADS / 2 < 1 ? 1 : LOADS / 2;      // elements of 16 bytes in the cache
     __shared__ uint4 lk0[KB * CH], lv0[KB * CH], lk1[KB * CH], lv1[KB * CH];
     __shared__ int64_t where[4][KB];      // of the next tiles' rows, in pieces (of what is not there: any that is)
+    __shared__ int64_t scale_at[CODED ? 4 : 1][CODED ? KB : 1];      // and of their scales
     constexpr int MINE = KB / 4;          // rows of a tile that each wave looks up
     typedef std::conditional_t<MINE == 16, uint16_t, uint8_t> Seen;
     __shared__ __align__(8) Seen seen[4][4];      // which of them are there
@@ -382,9 +387,38 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
             const bool there = lane < MINE && page >= 0 && page < a.cache.num_pages;
             if (lane < MINE)
                 where[slot][wave * MINE + lane] = there
-                    ? (page * a.cache.page_stride + (int64_t)(key & page_mask) * a.cache.slot_stride + it.head * a.cache.head_stride) / 8 : 0;
+                    ? (page * a.cache.page_stride + (int64_t)(key & page_mask) * a.cache.slot_stride + it.head * a.cache.head_stride) / PIECE : 0;
+            if (CODED && lane < MINE)
+                scale_at[slot][wave * MINE + lane] = there
+                    ? page * a.cache.scale_page_stride + (int64_t)((key & page_mask) >> a.cache.block_shift) * a.cache.scale_block_stride +
+                          it.head * a.cache.scale_head_stride : 0;
             const unsigned long long bits = __ballot(there);
             if (lane == 0) seen[slot][wave] = (Seen)bits;
+        };
+        vec<uint32_t, 4> ck[CODE_LOADS], cv[CODE_LOADS];      // a tile's codes and scales
+        uint32_t ek[CODE_LOADS], ev[CODE_LOADS];
+        auto load_codes = [&](int slot) {
+#pragma unroll
+            for (int x = 0; x < CODE_LOADS; ++x) {
+                const int row = (x * 256 + tid) / (CH / 2), c = tid % (CH / 2);
+                const int64_t at = where[slot][row] + c, s = scale_at[slot][row];
+                ck[x] = ((const vec<uint32_t, 4> *)kp)[at];
+                ek[x] = a.cache.k_scale[s];
+                cv[x] = ((const vec<uint32_t, 4> *)vp)[at];
+                ev[x] = a.cache.v_scale[s];
+            }
+        };
+        auto store_codes = [&](auto buf) {
+            vec<T, 8> *const lk = (vec<T, 8> *)(buf.value ? lk1 : lk0), *const lv = (vec<T, 8> *)(buf.value ? lv1 : lv0);
+#pragma unroll
+            for (int x = 0; x < CODE_LOADS; ++x) {
+                const int row = (x * 256 + tid) / (CH / 2), c = tid % (CH / 2) * 2;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    lk[row * CH + ((c + h) ^ key_turn<CH>(row))] = decode8<T>(vec<uint32_t, 2>{ck[x][2 * h], ck[x][2 * h + 1]}, ek[x]);
+                    lv[row * CH + ((c + h) ^ value_turn<CH>(row))] = decode8<T>(vec<uint32_t, 2>{cv[x][2 * h], cv[x][2 * h + 1]}, ev[x]);
+                }
+            }
         };
         auto load = [&](auto buf, int slot) {
             uint4 *const lk = buf.value ? lk1 : lk0, *const lv = buf.value ? lv1 : lv0;
@@ -511,14 +545,17 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
             note(it.k0, entry(it.k0), 0);
             note(it.k0 + KB, entry(it.k0 + KB), 1);
             __syncthreads();
-            load(std::integral_constant<int, 0>(), 0);
+            if constexpr (CODED) load_codes(0);
+            else load(std::integral_constant<int, 0>(), 0);
         }
         for (int kt = it.k0, t = 0; kt < end; kt += KB, ++t) {
             auto tile = [&](auto buf) {
-                __builtin_amdgcn_s_waitcnt(0x0f70);       // this tile is there
+                if constexpr (CODED) store_codes(buf);      // (all are done with the tile before the last)
+                else __builtin_amdgcn_s_waitcnt(0x0f70);       // this tile is there
                 __syncthreads();
                 const int e = entry(kt + 2 * KB);
-                load(std::integral_constant<int, 1 - buf.value>(), (t + 1) & 3);      // (behind the last tile: any row)
+                if constexpr (CODED) load_codes((t + 1) & 3);
+                else load(std::integral_constant<int, 1 - buf.value>(), (t + 1) & 3);      // (behind the last tile: any row)
                 compute(buf, kt, t & 3);
                 note(kt + 2 * KB, e, (t + 2) & 3);
             };
@@ -535,11 +572,17 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
             for (int key = it.k0 + max(0, odd_from + KB - it.k0) / KB * KB; key < lim; ++key) {
                 const int64_t page = table[key >> a.cache.page_shift];
                 if (page < 0 || page >= a.cache.num_pages) continue;
-                const T *v = (const T *)a.cache.v + page * a.cache.page_stride + (key & page_mask) * a.cache.slot_stride +
-                             it.head * a.cache.head_stride + 4 * half;
+                const int64_t at = page * a.cache.page_stride + (key & page_mask) * a.cache.slot_stride + it.head * a.cache.head_stride + 4 * half;
+                const T *v = (const T *)a.cache.v + at;
+                uint32_t e8 = 0;
+                if constexpr (CODED)
+                    e8 = a.cache.v_scale[page * a.cache.scale_page_stride +
+                                         (int64_t)((key & page_mask) >> a.cache.block_shift) * a.cache.scale_block_stride + it.head * a.cache.scale_head_stride];
 #pragma unroll
                 for (int x = 0; x < D / 8; ++x) {
-                    const vec<T, 4> y = *(const vec<T, 4> *)(v + 8 * x);
+                    vec<T, 4> y;
+                    if constexpr (CODED) y = decode4<T>(*(const uint32_t *)((const uint8_t *)a.cache.v + at + 8 * x), e8);
+                    else y = *(const vec<T, 4> *)(v + 8 * x);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         if (!(fabsf((float)y[e]) < INFINITY)) o[x / 4][x % 4 * 4 + e] += (float)y[e];
@@ -653,12 +696,12 @@ __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a, int64_t firs
     if (work) *(vec<T, 4> *)out = vec<T, 4>{(T)(o[0] * f), (T)(o[1] * f), (T)(o[2] * f), (T)(o[3] * f)};
 }
 
-template <typename T, int D>
+template <typename T, int D, bool CODED>
 hipError_t attend(const AttendArgs &a, int64_t max_items, hipStream_t s)
 {
     // (twice the items, because dies with shorter ones have more of them)
     const int grid = ((int)(max_items < 1024 ? 2 * max_items : 2048) / kDies + 1) * kDies;
-    k_attend_items<T, D><<<grid, 256, 0, s>>>(a);
+    k_attend_items<T, D, CODED><<<grid, 256, 0, s>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
     const int64_t rows = (int64_t)a.batch.num_tokens * a.batch.heads;
     constexpr int MANY = 256 / (D / 4);
@@ -674,13 +717,13 @@ hipError_t attend(const AttendArgs &a, int64_t max_items, hipStream_t s)
     return hipSuccess;
 }
 
-template <typename T>
+template <typename T, bool CODED>
 hipError_t attend(const AttendArgs &a, int64_t max_items, hipStream_t s)
 {
     switch (a.batch.head_dim) {
-    case 64: return attend<T, 64>(a, max_items, s);
-    case 128: return attend<T, 128>(a, max_items, s);
-    default: return attend<T, 256>(a, max_items, s);
+    case 64: return attend<T, 64, CODED>(a, max_items, s);
+    case 128: return attend<T, 128, CODED>(a, max_items, s);
+    default: return attend<T, 256, CODED>(a, max_items, s);
     }
 }
 
@@ -694,7 +737,8 @@ hipError_t launch_plan(const BatchArgs &b, const CacheArgs &c, const PlanView &p
 
 hipError_t launch_attend(const AttendArgs &a, int32_t type, int64_t max_items, hipStream_t s)
 {
-    return type == INFAAS_SEL_TYPE_BF16 ? attend<bf16_t>(a, max_items, s) : attend<fp16_t>(a, max_items, s);
+    if (a.cache.k_scale) return type == INFAAS_SEL_TYPE_BF16 ? attend<bf16_t, true>(a, max_items, s) : attend<fp16_t, true>(a, max_items, s);
+    return type == INFAAS_SEL_TYPE_BF16 ? attend<bf16_t, false>(a, max_items, s) : attend<fp16_t, false>(a, max_items, s);
 }
 
 }  // namespace infaas

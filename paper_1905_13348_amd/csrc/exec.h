@@ -91,6 +91,10 @@ struct CacheArgs {
     const int32_t *table;
     int64_t num_pages, page_stride, slot_stride, head_stride;
     int32_t table_width, page_shift, max_len;
+    // of a cache of 8 bits (null: of 16)
+    int32_t block_shift;
+    uint8_t *k_scale, *v_scale;
+    int64_t scale_page_stride, scale_block_stride, scale_head_stride;
 };
 
 struct BatchArgs {
@@ -117,6 +121,20 @@ struct AppendArgs {
     int32_t num_tokens, num_seqs, heads, kv_heads, head_dim;
 };
 
+struct AppendScaledArgs {
+    AppendArgs append;
+    const int32_t *seq_start;
+    int32_t q_groups, chunk;         // workgroups for the queries; tokens that one of the others looks through
+};
+
+struct ReadArgs {
+    CacheArgs cache;
+    const int32_t *token_seq, *token_pos;
+    int32_t num_tokens, num_seqs, kv_heads, head_dim;
+    void *k, *v;
+    int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+};
+
 struct SampleArgs {
     const void *logits;
     int64_t row_stride;
@@ -127,12 +145,51 @@ struct SampleArgs {
     float *prob;
 };
 
+// ---- codes of 8 bits --------------------------------------------------------------------------
+
+// Two of a word's four codes times 2^(e - 127), as numbers of T: one instruction, exact where T has the number (all codes with
+// all scales compared with the products in 64 bits; 0 stands for 2^-127, 255 gives NaN).
+template <typename T, bool UPPER> __device__ __forceinline__ vec<T, 2> decode2(uint32_t word, uint32_t e)
+{
+    const float scale = __uint_as_float(e << 23);
+    if constexpr (sizeof(T) == 2 && __is_same(T, bf16_t)) return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(word, scale, UPPER);
+    else return __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(word, scale, UPPER);
+}
+template <typename T> __device__ __forceinline__ vec<T, 4> decode4(uint32_t word, uint32_t e)
+{
+    const vec<T, 2> a = decode2<T, false>(word, e), b = decode2<T, true>(word, e);
+    return vec<T, 4>{a[0], a[1], b[0], b[1]};
+}
+template <typename T> __device__ __forceinline__ vec<T, 8> decode8(vec<uint32_t, 2> w, uint32_t e)
+{
+    const vec<T, 4> a = decode4<T>(w[0], e), b = decode4<T>(w[1], e);
+    return vec<T, 8>{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+}
+
+// Four numbers as codes, rounded to the nearest, ties to even (the instruction's rounding, compared with torch's over 2^20 numbers;
+// beyond 464 and for what is no number it gives NaN).
+__device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d)
+{
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
+}
+
+// The page of a key, or -1.
+__device__ __forceinline__ int64_t page_of(const CacheArgs &c, int seq, int num_seqs, int64_t pos)
+{
+    if (pos < 0 || pos >= c.max_len || (uint32_t)seq >= (uint32_t)num_seqs) return -1;
+    const int64_t page = c.table[(int64_t)seq * c.table_width + (pos >> c.page_shift)];
+    return page >= 0 && page < c.num_pages ? page : -1;
+}
+
 // Workgroups of a launch, at most: a grid of 2^32 threads and more is cut to its low 32 bits without an error.
 constexpr int64_t kMostGroups = 1 << 16;
 
 hipError_t launch_plan(const BatchArgs &b, const CacheArgs &c, const PlanView &p, const PlanSizes &z, hipStream_t s);
 hipError_t launch_attend(const AttendArgs &a, int32_t type, int64_t max_items, hipStream_t s);
 hipError_t launch_append(const AppendArgs &a, int32_t type, hipStream_t s);
+hipError_t launch_append_scaled(const AppendScaledArgs &a, int32_t type, hipStream_t s);
+hipError_t launch_read(const ReadArgs &a, int32_t type, hipStream_t s);
 hipError_t launch_sample(const SampleArgs &a, int32_t type, hipStream_t s);
 
 }  // namespace infaas

@@ -76,6 +76,18 @@ int check_pools(const infaas_sel_cache *c)
     return INFAAS_SEL_OK;
 }
 
+int check_scales(const infaas_sel_cache *c, const infaas_sel_scales *s)
+{
+    if (!s) return refuse("scales: null");
+    if (!s->d_k_scale || !s->d_v_scale) return refuse("scales: null arrays");
+    if (s->block < 1 || s->block > c->page_size || (s->block & (s->block - 1)))
+        return refuse("scales: a block of %d keys is not a power of two up to the page size %d", s->block, c->page_size);
+    if (s->page_stride < 0 || s->block_stride < 0 || s->head_stride < 0) return refuse("scales: a negative stride");
+    if (c->page_stride % 16 || c->slot_stride % 16 || c->head_stride % 16)
+        return refuse("cache: strides of codes are not multiples of 16");
+    return INFAAS_SEL_OK;
+}
+
 // Sizes that the batch and the cache have to agree on; looks at no pointer.
 int check_sizes(const infaas_sel_cache *c, const infaas_sel_batch *b)
 {
@@ -156,7 +168,7 @@ int ensure(infaas_sel_exec *x, int64_t bytes, hipStream_t s, bool in_call)
     return INFAAS_SEL_OK;
 }
 
-CacheArgs cache_args(const infaas_sel_cache *c, const infaas_sel_batch *b)
+CacheArgs cache_args(const infaas_sel_cache *c, const infaas_sel_batch *b, const infaas_sel_scales *s = nullptr)
 {
     CacheArgs a{};
     a.k = c->d_k; a.v = c->d_v;
@@ -167,6 +179,11 @@ CacheArgs cache_args(const infaas_sel_cache *c, const infaas_sel_batch *b)
     a.page_shift = __builtin_ctz((unsigned)c->page_size);
     // (what the table can hold, and what the kernels can count a few tiles beyond)
     a.max_len = (int32_t)std::min<int64_t>({b->max_len, (int64_t)b->table_width * c->page_size, kMostKeys});
+    if (s) {
+        a.k_scale = (uint8_t *)s->d_k_scale; a.v_scale = (uint8_t *)s->d_v_scale;
+        a.block_shift = __builtin_ctz((unsigned)s->block);
+        a.scale_page_stride = s->page_stride; a.scale_block_stride = s->block_stride; a.scale_head_stride = s->head_stride;
+    }
     return a;
 }
 
@@ -180,6 +197,77 @@ PlanView plan_view(const infaas_sel_batch *b, const PlanSizes &z)
 {
     char *p = (char *)b->d_plan;
     return PlanView{(PlanHeader *)p, (PlanToken *)(p + z.tokens_at), (PlanUnit *)(p + z.units_at), (PlanItem *)(p + z.items_at)};
+}
+
+// infaas_sel_exec_append, and _append_scaled where `coded`.
+int append(infaas_sel_exec *x, const infaas_sel_cache *cache, const infaas_sel_scales *scales, bool coded, const infaas_sel_batch *batch,
+           const infaas_sel_append_args *args, void *hip_stream)
+{
+    if (!x) return refuse("executor: null");
+    if (int rc = check_sizes(cache, batch)) return rc;
+    if (int rc = check_pools(cache)) return rc;
+    if (coded)
+        if (int rc = check_scales(cache, scales)) return rc;
+    if (int rc = check_arrays(batch)) return rc;
+    if (coded && batch->num_seqs > 0 && !batch->d_seq_start) return refuse("batch: null sequence arrays");
+    if (!args) return refuse("append: null");
+    if (args->rot_dim < 0 || args->rot_dim > cache->head_dim || args->rot_dim % 16)
+        return refuse("append: %d rotated dimensions (a multiple of 16 up to %d)", args->rot_dim, cache->head_dim);
+    if (args->rot_dim > 0 && !args->d_freq) return refuse("append: null frequencies");
+    if ((args->d_q == nullptr) != (args->d_q_out == nullptr)) return refuse("append: queries without an output, or the reverse");
+    if (batch->num_tokens == 0) return INFAAS_SEL_OK;
+    if (!args->d_k || !args->d_v || !aligned(args->d_k) || !aligned(args->d_v) || !aligned(args->d_q) || !aligned(args->d_q_out))
+        return refuse("append: arrays are null or not aligned to 16 bytes");
+    for (int64_t s : {args->q_token_stride, args->q_head_stride, args->k_token_stride, args->k_head_stride, args->v_token_stride,
+                      args->v_head_stride, args->out_token_stride, args->out_head_stride})
+        if (!vector_stride(s)) return refuse("append: strides are not multiples of 8 elements");
+    OnDevice on(x->device);
+    if (on.err != hipSuccess) return hip_failed(on.err, "hipSetDevice");
+    AppendArgs a{*args, cache_args(cache, batch, scales), batch->d_token_seq, batch->d_token_pos, batch->num_tokens, batch->num_seqs,
+                 batch->heads, cache->kv_heads, cache->head_dim};
+    if (coded) {
+        const AppendScaledArgs sa{a, batch->d_seq_start, 0, 0};
+        if (hipError_t e = launch_append_scaled(sa, cache->type, (hipStream_t)hip_stream)) return hip_failed(e, "infaas_sel_exec_append_scaled");
+        return INFAAS_SEL_OK;
+    }
+    if (hipError_t e = launch_append(a, cache->type, (hipStream_t)hip_stream)) return hip_failed(e, "infaas_sel_exec_append");
+    return INFAAS_SEL_OK;
+}
+
+// infaas_sel_exec_attend, and _attend_scaled where `coded`.
+int attend(infaas_sel_exec *x, const infaas_sel_cache *cache, const infaas_sel_scales *scales, bool coded, const infaas_sel_batch *batch,
+           const void *d_q, int64_t q_token_stride, int64_t q_head_stride,
+           void *d_out, int64_t out_token_stride, int64_t out_head_stride, float scale, void *hip_stream)
+{
+    if (!x) return refuse("executor: null");
+    if (int rc = check_sizes(cache, batch)) return rc;
+    if (int rc = check_pools(cache)) return rc;
+    if (coded)
+        if (int rc = check_scales(cache, scales)) return rc;
+    if (int rc = check_arrays(batch)) return rc;
+    PlanSizes z;
+    if (!plan_sizes(cache, batch, &z)) return refuse("batch: too many tokens");
+    if (int rc = check_plan_arrays(batch, z)) return rc;
+    if (!(scale > 0) || !std::isfinite(scale)) return refuse("attend: the scale is not finite and positive");
+    if (batch->num_tokens == 0) return INFAAS_SEL_OK;
+    if (!d_q || !d_out || !aligned(d_q) || !aligned(d_out)) return refuse("attend: arrays are null or not aligned to 16 bytes");
+    for (int64_t s : {q_token_stride, q_head_stride, out_token_stride, out_head_stride})
+        if (!vector_stride(s)) return refuse("attend: strides are not multiples of 8 elements");
+    OnDevice on(x->device);
+    if (on.err != hipSuccess) return hip_failed(on.err, "hipSetDevice");
+    if (int rc = ensure(x, scratch_for(cache, z), (hipStream_t)hip_stream, true)) return rc;
+    AttendArgs a{};
+    a.batch = batch_args(cache, batch);
+    a.cache = cache_args(cache, batch, scales);
+    a.plan = plan_view(batch, z);
+    a.q = d_q; a.out = d_out;
+    a.q_token_stride = q_token_stride; a.q_head_stride = q_head_stride;
+    a.out_token_stride = out_token_stride; a.out_head_stride = out_head_stride;
+    a.scale_log2 = scale * 1.44269504088896f;
+    a.part_o = (float *)x->scratch;
+    a.part_ml = (float2 *)((char *)x->scratch + z.max_rows * cache->kv_heads * cache->head_dim * (int64_t)sizeof(float));
+    if (hipError_t e = launch_attend(a, cache->type, z.max_items, (hipStream_t)hip_stream)) return hip_failed(e, coded ? "infaas_sel_exec_attend_scaled" : "infaas_sel_exec_attend");
+    return INFAAS_SEL_OK;
 }
 
 }  // namespace
@@ -248,59 +336,50 @@ int infaas_sel_exec_plan(infaas_sel_exec_t *x, const infaas_sel_cache *cache, co
 int infaas_sel_exec_append(infaas_sel_exec_t *x, const infaas_sel_cache *cache, const infaas_sel_batch *batch,
                            const infaas_sel_append_args *args, void *hip_stream)
 {
-    if (!x) return refuse("executor: null");
-    if (int rc = check_sizes(cache, batch)) return rc;
-    if (int rc = check_pools(cache)) return rc;
-    if (int rc = check_arrays(batch)) return rc;
-    if (!args) return refuse("append: null");
-    if (args->rot_dim < 0 || args->rot_dim > cache->head_dim || args->rot_dim % 16)
-        return refuse("append: %d rotated dimensions (a multiple of 16 up to %d)", args->rot_dim, cache->head_dim);
-    if (args->rot_dim > 0 && !args->d_freq) return refuse("append: null frequencies");
-    if ((args->d_q == nullptr) != (args->d_q_out == nullptr)) return refuse("append: queries without an output, or the reverse");
-    if (batch->num_tokens == 0) return INFAAS_SEL_OK;
-    if (!args->d_k || !args->d_v || !aligned(args->d_k) || !aligned(args->d_v) || !aligned(args->d_q) || !aligned(args->d_q_out))
-        return refuse("append: arrays are null or not aligned to 16 bytes");
-    for (int64_t s : {args->q_token_stride, args->q_head_stride, args->k_token_stride, args->k_head_stride, args->v_token_stride,
-                      args->v_head_stride, args->out_token_stride, args->out_head_stride})
-        if (!vector_stride(s)) return refuse("append: strides are not multiples of 8 elements");
-    OnDevice on(x->device);
-    if (on.err != hipSuccess) return hip_failed(on.err, "hipSetDevice");
-    AppendArgs a{*args, cache_args(cache, batch), batch->d_token_seq, batch->d_token_pos, batch->num_tokens, batch->num_seqs,
-                 batch->heads, cache->kv_heads, cache->head_dim};
-    if (hipError_t e = launch_append(a, cache->type, (hipStream_t)hip_stream)) return hip_failed(e, "infaas_sel_exec_append");
-    return INFAAS_SEL_OK;
+    return append(x, cache, nullptr, false, batch, args, hip_stream);
+}
+
+int infaas_sel_exec_append_scaled(infaas_sel_exec_t *x, const infaas_sel_cache *cache, const infaas_sel_scales *scales,
+                                  const infaas_sel_batch *batch, const infaas_sel_append_args *args, void *hip_stream)
+{
+    return append(x, cache, scales, true, batch, args, hip_stream);
 }
 
 int infaas_sel_exec_attend(infaas_sel_exec_t *x, const infaas_sel_cache *cache, const infaas_sel_batch *batch,
                            const void *d_q, int64_t q_token_stride, int64_t q_head_stride,
                            void *d_out, int64_t out_token_stride, int64_t out_head_stride, float scale, void *hip_stream)
 {
+    return attend(x, cache, nullptr, false, batch, d_q, q_token_stride, q_head_stride, d_out, out_token_stride, out_head_stride, scale,
+                  hip_stream);
+}
+
+int infaas_sel_exec_attend_scaled(infaas_sel_exec_t *x, const infaas_sel_cache *cache, const infaas_sel_scales *scales,
+                                  const infaas_sel_batch *batch, const void *d_q, int64_t q_token_stride, int64_t q_head_stride,
+                                  void *d_out, int64_t out_token_stride, int64_t out_head_stride, float scale, void *hip_stream)
+{
+    return attend(x, cache, scales, true, batch, d_q, q_token_stride, q_head_stride, d_out, out_token_stride, out_head_stride, scale,
+                  hip_stream);
+}
+
+int infaas_sel_exec_read(infaas_sel_exec_t *x, const infaas_sel_cache *cache, const infaas_sel_scales *scales,
+                         const infaas_sel_batch *batch, void *d_k, int64_t k_token_stride, int64_t k_head_stride,
+                         void *d_v, int64_t v_token_stride, int64_t v_head_stride, void *hip_stream)
+{
     if (!x) return refuse("executor: null");
     if (int rc = check_sizes(cache, batch)) return rc;
     if (int rc = check_pools(cache)) return rc;
+    if (scales)
+        if (int rc = check_scales(cache, scales)) return rc;
     if (int rc = check_arrays(batch)) return rc;
-    PlanSizes z;
-    if (!plan_sizes(cache, batch, &z)) return refuse("batch: too many tokens");
-    if (int rc = check_plan_arrays(batch, z)) return rc;
-    if (!(scale > 0) || !std::isfinite(scale)) return refuse("attend: the scale is not finite and positive");
     if (batch->num_tokens == 0) return INFAAS_SEL_OK;
-    if (!d_q || !d_out || !aligned(d_q) || !aligned(d_out)) return refuse("attend: arrays are null or not aligned to 16 bytes");
-    for (int64_t s : {q_token_stride, q_head_stride, out_token_stride, out_head_stride})
-        if (!vector_stride(s)) return refuse("attend: strides are not multiples of 8 elements");
+    if (!d_k || !d_v || !aligned(d_k) || !aligned(d_v)) return refuse("read: arrays are null or not aligned to 16 bytes");
+    for (int64_t s : {k_token_stride, k_head_stride, v_token_stride, v_head_stride})
+        if (!vector_stride(s)) return refuse("read: strides are not multiples of 8 elements");
     OnDevice on(x->device);
     if (on.err != hipSuccess) return hip_failed(on.err, "hipSetDevice");
-    if (int rc = ensure(x, scratch_for(cache, z), (hipStream_t)hip_stream, true)) return rc;
-    AttendArgs a{};
-    a.batch = batch_args(cache, batch);
-    a.cache = cache_args(cache, batch);
-    a.plan = plan_view(batch, z);
-    a.q = d_q; a.out = d_out;
-    a.q_token_stride = q_token_stride; a.q_head_stride = q_head_stride;
-    a.out_token_stride = out_token_stride; a.out_head_stride = out_head_stride;
-    a.scale_log2 = scale * 1.44269504088896f;
-    a.part_o = (float *)x->scratch;
-    a.part_ml = (float2 *)((char *)x->scratch + z.max_rows * cache->kv_heads * cache->head_dim * (int64_t)sizeof(float));
-    if (hipError_t e = launch_attend(a, cache->type, z.max_items, (hipStream_t)hip_stream)) return hip_failed(e, "infaas_sel_exec_attend");
+    const ReadArgs a{cache_args(cache, batch, scales), batch->d_token_seq, batch->d_token_pos, batch->num_tokens, batch->num_seqs,
+                     cache->kv_heads, cache->head_dim, d_k, d_v, k_token_stride, k_head_stride, v_token_stride, v_head_stride};
+    if (hipError_t e = launch_read(a, cache->type, (hipStream_t)hip_stream)) return hip_failed(e, "infaas_sel_exec_read");
     return INFAAS_SEL_OK;
 }
 

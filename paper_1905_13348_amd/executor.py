@@ -17,7 +17,7 @@ from __future__ import annotations
 import ctypes
 from typing import Optional
 
-from .binding import InfaasSelError, _AppendArgs, _Batch, _Cache, _stream_ptr, _use_torch, load_library
+from .binding import InfaasSelError, _AppendArgs, _Batch, _Cache, _Scales, _stream_ptr, _use_torch, load_library
 
 _TYPES = None        # torch type -> INFAAS_SEL_TYPE_*
 
@@ -73,33 +73,63 @@ def _no_gradient(t, name: str) -> None:
 
 class PagedCache:
     """One layer's pools of pages (infaas_sel_cache): ``layout`` "token" for [page][slot][head][dim], "head" for
-    [page][head][slot][dim]; both pools have the same shape and strides, the last dimension consecutive."""
+    [page][head][slot][dim]; both pools have the same shape and strides, the last dimension consecutive.
 
-    def __init__(self, k_pool, v_pool, layout: str = "token"):
+    With ``k_scale`` and ``v_scale`` a cache of 8 bits (infaas_sel_scales): pools of float8_e4m3fn, scales of float8_e8m0fnu
+    [page][block][head] or [page][head][block], page size / blocks keys to a scale; ``dtype`` is then the type of what is
+    appended and of queries and results (bfloat16 if not given)."""
+
+    def __init__(self, k_pool, v_pool, layout: str = "token", k_scale=None, v_scale=None, dtype=None):
         torch = _use_torch()
+        coded = k_scale is not None or v_scale is not None
         if layout not in ("token", "head"):
             raise ValueError(f"layout {layout!r}: 'token' or 'head'")
         if not all(isinstance(p, torch.Tensor) and p.is_cuda and p.dim() == 4 for p in (k_pool, v_pool)):
             raise TypeError("device tensors of four dimensions expected")
         # (a dimension of one element has a stride of no meaning)
         st, vst = ([0 if n == 1 else x for n, x in zip(p.shape, p.stride())] for p in (k_pool, v_pool))
-        if k_pool.dtype not in (torch.bfloat16, torch.float16) or v_pool.dtype != k_pool.dtype \
-                or v_pool.shape != k_pool.shape or st != vst or k_pool.stride(3) != 1:
-            raise TypeError("pools of one type (bfloat16 or float16), shape and strides expected, the last one 1")
+        types = (torch.float8_e4m3fn,) if coded else (torch.bfloat16, torch.float16)
+        if k_pool.dtype not in types or v_pool.dtype != k_pool.dtype or v_pool.shape != k_pool.shape or st != vst or k_pool.stride(3) != 1:
+            raise TypeError(f"pools of one type ({'float8_e4m3fn' if coded else 'bfloat16 or float16'}), shape and strides expected, "
+                            "the last one 1")
         if k_pool.get_device() != v_pool.get_device():
             raise TypeError("pools on one device expected")
         _no_gradient(k_pool, "k_pool")
         _no_gradient(v_pool, "v_pool")
         slot, head = (1, 2) if layout == "token" else (2, 1)
-        self.k_pool, self.v_pool, self.layout, self.dtype = k_pool, v_pool, layout, k_pool.dtype
+        if dtype is None:
+            dtype = torch.bfloat16 if coded else k_pool.dtype
+        if dtype not in (torch.bfloat16, torch.float16) or (not coded and dtype != k_pool.dtype):
+            raise TypeError(f"dtype {dtype}: that of the pools, or with scales bfloat16 or float16")
+        self.k_pool, self.v_pool, self.layout, self.dtype = k_pool, v_pool, layout, dtype
         self.device = k_pool.get_device()
         self.kv_heads, self.head_dim = k_pool.shape[head], k_pool.shape[3]
         self.page_size, self.num_pages = k_pool.shape[slot], k_pool.shape[0]
-        self._c = _Cache(d_k=k_pool.data_ptr(), d_v=v_pool.data_ptr(), type=_types()[k_pool.dtype], kv_heads=_i32(self.kv_heads, "KV heads"),
+        self._c = _Cache(d_k=k_pool.data_ptr(), d_v=v_pool.data_ptr(), type=_types()[dtype], kv_heads=_i32(self.kv_heads, "KV heads"),
                          head_dim=_i32(self.head_dim, "head dimension"), page_size=_i32(self.page_size, "page size"), num_pages=self.num_pages,
                          page_stride=st[0], slot_stride=st[slot], head_stride=st[head])
         self._ref = ctypes.byref(self._c)
         self._sizes = (self.kv_heads, self.head_dim, self.page_size)      # what a batch's caches have in common
+        self.k_scale, self.v_scale, self._scales = k_scale, v_scale, None
+        if coded:
+            self._scales_of(torch, slot, head)
+
+    def _scales_of(self, torch, slot: int, head: int) -> None:
+        """The scales' part of the arguments."""
+        for name, s in (("k_scale", self.k_scale), ("v_scale", self.v_scale)):
+            if not isinstance(s, torch.Tensor) or s.dtype != torch.float8_e8m0fnu or s.dim() != 3 or s.get_device() != self.device:
+                raise TypeError(f"{name}: float8_e8m0fnu tensor of three dimensions on device {self.device} expected")
+        ks, vs = self.k_scale, self.v_scale
+        blocks = ks.shape[slot]
+        want = [self.num_pages] * 3
+        want[slot], want[head] = blocks, self.kv_heads
+        st, vst = ([0 if n == 1 else x for n, x in zip(s.shape, s.stride())] for s in (ks, vs))
+        if list(ks.shape) != want or ks.shape != vs.shape or st != vst or blocks < 1 or self.page_size % blocks:
+            raise TypeError(f"scales of one shape and strides expected: the pools' without the last dimension, with blocks of keys in the "
+                            f"place of {self.page_size} slots, not {list(ks.shape)} and {list(vs.shape)}")
+        self._scales = _Scales(d_k_scale=ks.data_ptr(), d_v_scale=vs.data_ptr(), block=self.page_size // blocks,
+                               page_stride=st[0], block_stride=st[slot], head_stride=st[head])
+        self._scales_ref = ctypes.byref(self._scales)
 
 
 class Batch:
@@ -154,8 +184,8 @@ class Executor:
         _check(self._lib.infaas_sel_exec_create(_i32(device, "device"), ctypes.byref(self._h)))
         self.device = device
 
-    def cache(self, k_pool, v_pool, layout: str = "token") -> PagedCache:
-        return PagedCache(k_pool, v_pool, layout)
+    def cache(self, k_pool, v_pool, layout: str = "token", k_scale=None, v_scale=None, dtype=None) -> PagedCache:
+        return PagedCache(k_pool, v_pool, layout, k_scale, v_scale, dtype)
 
     def batch(self, cache: PagedCache, heads: int, **arrays) -> Batch:
         return Batch(cache, heads, **arrays)
@@ -203,7 +233,23 @@ class Executor:
             fp, rot = _vector(freq, _use_torch().float64, "freq", self.device), _i32(2 * freq.numel(), "freq")
             _no_gradient(freq, "freq")
         a = _AppendArgs(qp, kp, vp, op, qt, qh, kt, kh, vt, vh, ot, oh, fp, rot, 1 if interleaved else 0)
-        status = self._lib.infaas_sel_exec_append(self._h, cache._ref, batch._ref, a, _stream_ptr(stream, self.device))
+        if getattr(cache, "_scales", None) is None:
+            status = self._lib.infaas_sel_exec_append(self._h, cache._ref, batch._ref, a, _stream_ptr(stream, self.device))
+        else:
+            status = self._lib.infaas_sel_exec_append_scaled(self._h, cache._ref, cache._scales_ref, batch._ref, a,
+                                                             _stream_ptr(stream, self.device))
+        if status:
+            _check(status)
+
+    def read(self, cache: PagedCache, batch: Batch, k, v, stream=None) -> None:
+        """The cache's keys and values at the batch's tokens' positions into ``k`` and ``v`` [tokens][KV heads][dim]."""
+        if cache is not batch._cache or cache.device != self.device:
+            self._agree(cache, batch)
+        scales = getattr(cache, "_scales", None)
+        status = self._lib.infaas_sel_exec_read(
+            self._h, cache._ref, None if scales is None else cache._scales_ref, batch._ref,
+            *self._rows(k, cache, batch, batch._kv_shape, "k"), *self._rows(v, cache, batch, batch._kv_shape, "v"),
+            _stream_ptr(stream, self.device))
         if status:
             _check(status)
 
@@ -212,10 +258,12 @@ class Executor:
         if cache is not batch._cache or cache.device != self.device:
             self._agree(cache, batch)
         shape = batch._q_shape
-        status = self._lib.infaas_sel_exec_attend(
-            self._h, cache._ref, batch._ref, *self._rows(q, cache, batch, shape, "q"),
-            *self._rows(out, cache, batch, shape, "out"), cache.head_dim ** -0.5 if scale is None else scale,
-            _stream_ptr(stream, self.device))
+        rest = (*self._rows(q, cache, batch, shape, "q"), *self._rows(out, cache, batch, shape, "out"),
+                cache.head_dim ** -0.5 if scale is None else scale, _stream_ptr(stream, self.device))
+        if getattr(cache, "_scales", None) is None:
+            status = self._lib.infaas_sel_exec_attend(self._h, cache._ref, batch._ref, *rest)
+        else:
+            status = self._lib.infaas_sel_exec_attend_scaled(self._h, cache._ref, cache._scales_ref, batch._ref, *rest)
         if status:
             _check(status)
 
