@@ -725,6 +725,56 @@ int infaas_sel_exec_read(infaas_sel_exec_t *x, const infaas_sel_cache *cache, co
                          void *d_v, int64_t v_token_stride, int64_t v_head_stride, void *hip_stream);
 
 /*
+ * The pages of a worker's sequences, kept on the device: which page each key is on (a batch's d_page_table and d_seq_len), how
+ * many rows of the table name each page, and the arrays of the step's batch, which infaas_sel_exec_advance writes.  A page
+ * that no row names is free.  The caller may hold pages beside the table (a prompt that is kept for queries to come): it
+ * adds to their counts.  All arrays are the caller's DEVICE memory; before the first call the lengths and counts are 0.
+ */
+typedef struct {
+    int32_t num_seqs;       /* S, 1 .. 4096 */
+    int32_t table_width;    /* pages per row of d_page_table, >= 1 */
+    int32_t page_size;      /* keys to a page, a power of two from 1 to 65536 */
+    int32_t num_pages;      /* >= 1 */
+    int32_t max_tokens;     /* n of the step's batch, >= 1 */
+    int32_t pad;
+    int32_t *d_page_table;  /* [S * table_width] the first pages of a row, as many as its length needs, are the sequence's */
+    int32_t *d_seq_len;     /* [S]  keys of every sequence */
+    int32_t *d_page_refs;   /* [num_pages] rows that name the page; 16-byte aligned */
+    int32_t *d_seq_start;   /* [S + 1] written: first token of every sequence, and their number */
+    int32_t *d_token_seq;   /* [max_tokens] written: sequence of every token, -1 behind the last */
+    int32_t *d_token_pos;   /* [max_tokens] written: its position, -1 behind the last */
+    int32_t *d_taken;       /* [S] written: tokens that the sequence got */
+    int32_t *d_copies;      /* [S][3] written: page that the sequence's last one is copied from, page it is copied to, keys on it; or -1s */
+} infaas_sel_table;
+
+/*
+ * Take all sequences a step further.  In this order:
+ *   d_parent [S] (may be null: every sequence goes on by itself)  sequence s goes on from what sequence d_parent[s] had before
+ *       the call: its length, and its pages, which are then shared.  Another number than 0..S-1: it is empty.
+ *   d_new [S] below 0: as many of its last keys are dropped (all, if it has fewer).
+ *       Pages that no row names any more are free from here on; their entries become -1.
+ *   d_new [S] above 0: so many tokens come.  The sequence takes them if its length then fits the table's width; the tokens of it
+ *       and of those in front of it that come too are max_tokens at most; and it needs no page, or the pages that it and
+ *       those in front of it need are as many as are free, at most.  Otherwise it gets none of them and stays as it is.  (So who waits
+ *       for pages is not overtaken by who needs some, too.)
+ *       Pages are handed out the lowest-numbered first, to the sequences in their order.  If its last page is not full, and
+ *       other rows name it as well, the sequence gets a page for a copy of it first (d_copies): infaas_sel_exec_copy has to run,
+ *       for every layer's cache, before the step's keys are appended.
+ * A step's arrays are then those of a batch of max_tokens tokens (in a replayed graph, too).  Lengths that are out of range count as the
+ * nearest that is not, pages in the table that are not there as none.  Errors: INVALID_ARG, HIP.
+ */
+int infaas_sel_exec_advance(infaas_sel_exec_t *x, const infaas_sel_table *table, const int32_t *d_new, const int32_t *d_parent,
+                            void *hip_stream);
+
+/*
+ * Copy the keys and values that the latest infaas_sel_exec_advance put down in d_copies from page to page of a layer's cache, and their
+ * scales (`scales`: null for a cache of 16 bits).  Page sizes have to agree; pages beyond the cache are left out.
+ * Errors: INVALID_ARG, HIP.
+ */
+int infaas_sel_exec_copy(infaas_sel_exec_t *x, const infaas_sel_cache *cache, const infaas_sel_scales *scales,
+                         const infaas_sel_table *table, void *hip_stream);
+
+/*
  * Draw a token of every row of logits.  In row r the tokens are ordered by logit, the greatest
  * first, equal ones by number; weight w_i = exp((x_i - max x) / temperature).  Kept are, in this order,
  *     the first top_k,                                                    (0 or less: all)

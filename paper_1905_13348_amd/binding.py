@@ -69,6 +69,12 @@ class _Scales(ctypes.Structure):
                 ("page_stride", ctypes.c_int64), ("block_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
+class _Table(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("num_seqs", "table_width", "page_size", "num_pages", "max_tokens", "pad")] + \
+        [(n, ctypes.c_void_p) for n in ("d_page_table", "d_seq_len", "d_page_refs", "d_seq_start", "d_token_seq", "d_token_pos", "d_taken",
+                                        "d_copies")]
+
+
 class _Batch(ctypes.Structure):
     _fields_ = [("num_tokens", ctypes.c_int32), ("num_seqs", ctypes.c_int32), ("num_groups", ctypes.c_int32),
                 ("heads", ctypes.c_int32), ("max_len", ctypes.c_int32), ("table_width", ctypes.c_int32),
@@ -97,7 +103,8 @@ EXPORTED = ("infaas_sel_create", "infaas_sel_load_variants", "infaas_sel_update_
             "infaas_sel_get_info", "infaas_sel_strerror", "infaas_sel_last_error",
             "infaas_sel_exec_create", "infaas_sel_exec_destroy", "infaas_sel_exec_plan_bytes", "infaas_sel_exec_reserve",
             "infaas_sel_exec_plan", "infaas_sel_exec_append", "infaas_sel_exec_attend", "infaas_sel_exec_sample",
-            "infaas_sel_exec_append_scaled", "infaas_sel_exec_attend_scaled", "infaas_sel_exec_read")
+            "infaas_sel_exec_append_scaled", "infaas_sel_exec_attend_scaled", "infaas_sel_exec_read",
+            "infaas_sel_exec_advance", "infaas_sel_exec_copy")
 
 
 def library_path() -> str:
@@ -166,6 +173,9 @@ def load_library() -> ctypes.CDLL:
     lib.infaas_sel_exec_append_scaled.argtypes = [vp, cp, sp, bp, ctypes.POINTER(_AppendArgs), vp]
     lib.infaas_sel_exec_attend_scaled.argtypes = [vp, cp, sp, bp, vp, i64, i64, vp, i64, i64, ctypes.c_float, vp]
     lib.infaas_sel_exec_read.argtypes = [vp, cp, sp, bp, vp, i64, i64, vp, i64, i64, vp]
+    tp = ctypes.POINTER(_Table)
+    lib.infaas_sel_exec_advance.argtypes = [vp, tp, vp, vp, vp]
+    lib.infaas_sel_exec_copy.argtypes = [vp, cp, sp, tp, vp]
     for name in EXPORTED:
         if name not in ("infaas_sel_destroy", "infaas_sel_strerror", "infaas_sel_last_error", "infaas_sel_exec_destroy",
                         "infaas_sel_exec_plan_bytes"):

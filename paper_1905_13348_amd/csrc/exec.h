@@ -135,6 +135,22 @@ struct ReadArgs {
     int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
 };
 
+struct AdvanceArgs {
+    infaas_sel_table t;
+    const int32_t *more, *parent;    // d_new, d_parent
+    int32_t page_shift;
+    int32_t most;                    // keys that a row has room for
+};
+
+struct CopyArgs {
+    CacheArgs cache;
+    int32_t kv_heads, bytes;         // of a head's key
+    int32_t num_seqs;
+    const int32_t *copies;
+};
+
+constexpr int kMostSeqs = 4096;      // of a table
+
 struct SampleArgs {
     const void *logits;
     int64_t row_stride;
@@ -190,6 +206,8 @@ hipError_t launch_attend(const AttendArgs &a, int32_t type, int64_t max_items, h
 hipError_t launch_append(const AppendArgs &a, int32_t type, hipStream_t s);
 hipError_t launch_append_scaled(const AppendScaledArgs &a, int32_t type, hipStream_t s);
 hipError_t launch_read(const ReadArgs &a, int32_t type, hipStream_t s);
+hipError_t launch_advance(const AdvanceArgs &a, hipStream_t s);
+hipError_t launch_copy(const CopyArgs &a, hipStream_t s);
 hipError_t launch_sample(const SampleArgs &a, int32_t type, hipStream_t s);
 
 }  // namespace infaas

@@ -199,6 +199,21 @@ PlanView plan_view(const infaas_sel_batch *b, const PlanSizes &z)
     return PlanView{(PlanHeader *)p, (PlanToken *)(p + z.tokens_at), (PlanUnit *)(p + z.units_at), (PlanItem *)(p + z.items_at)};
 }
 
+int check_table(const infaas_sel_table *t)
+{
+    if (!t) return refuse("table: null");
+    if (t->num_seqs < 1 || t->num_seqs > kMostSeqs) return refuse("table: %d sequences (1 .. %d)", t->num_seqs, kMostSeqs);
+    if (t->table_width < 1 || t->num_pages < 1 || t->max_tokens < 1)
+        return refuse("table: %d pages to a row, %d pages, %d tokens (1 at least)", t->table_width, t->num_pages, t->max_tokens);
+    if (t->page_size < 1 || t->page_size > 65536 || (t->page_size & (t->page_size - 1)))
+        return refuse("table: page size %d is not a power of two up to 65536", t->page_size);
+    if (!t->d_page_table || !t->d_seq_len || !t->d_page_refs || !t->d_seq_start || !t->d_token_seq || !t->d_token_pos || !t->d_taken ||
+        !t->d_copies)
+        return refuse("table: null arrays");
+    if (!aligned(t->d_page_refs)) return refuse("table: the pages' counts are not aligned to 16 bytes");
+    return INFAAS_SEL_OK;
+}
+
 // infaas_sel_exec_append, and _append_scaled where `coded`.
 int append(infaas_sel_exec *x, const infaas_sel_cache *cache, const infaas_sel_scales *scales, bool coded, const infaas_sel_batch *batch,
            const infaas_sel_append_args *args, void *hip_stream)
@@ -380,6 +395,39 @@ int infaas_sel_exec_read(infaas_sel_exec_t *x, const infaas_sel_cache *cache, co
     const ReadArgs a{cache_args(cache, batch, scales), batch->d_token_seq, batch->d_token_pos, batch->num_tokens, batch->num_seqs,
                      cache->kv_heads, cache->head_dim, d_k, d_v, k_token_stride, k_head_stride, v_token_stride, v_head_stride};
     if (hipError_t e = launch_read(a, cache->type, (hipStream_t)hip_stream)) return hip_failed(e, "infaas_sel_exec_read");
+    return INFAAS_SEL_OK;
+}
+
+int infaas_sel_exec_advance(infaas_sel_exec_t *x, const infaas_sel_table *table, const int32_t *d_new, const int32_t *d_parent,
+                            void *hip_stream)
+{
+    if (!x) return refuse("executor: null");
+    if (int rc = check_table(table)) return rc;
+    if (!d_new) return refuse("advance: null arrays");
+    OnDevice on(x->device);
+    if (on.err != hipSuccess) return hip_failed(on.err, "hipSetDevice");
+    const AdvanceArgs a{*table, d_new, d_parent, __builtin_ctz((unsigned)table->page_size),
+                        (int32_t)std::min<int64_t>((int64_t)table->table_width * table->page_size, kMostKeys)};
+    if (hipError_t e = launch_advance(a, (hipStream_t)hip_stream)) return hip_failed(e, "infaas_sel_exec_advance");
+    return INFAAS_SEL_OK;
+}
+
+int infaas_sel_exec_copy(infaas_sel_exec_t *x, const infaas_sel_cache *cache, const infaas_sel_scales *scales,
+                         const infaas_sel_table *table, void *hip_stream)
+{
+    if (!x) return refuse("executor: null");
+    if (int rc = check_cache(cache)) return rc;
+    if (int rc = check_pools(cache)) return rc;
+    if (scales)
+        if (int rc = check_scales(cache, scales)) return rc;
+    if (int rc = check_table(table)) return rc;
+    if (table->page_size != cache->page_size)
+        return refuse("copy: a table for pages of %d keys with a cache's of %d", table->page_size, cache->page_size);
+    OnDevice on(x->device);
+    if (on.err != hipSuccess) return hip_failed(on.err, "hipSetDevice");
+    infaas_sel_batch none{};
+    const CopyArgs a{cache_args(cache, &none, scales), cache->kv_heads, cache->head_dim * (scales ? 1 : 2), table->num_seqs, table->d_copies};
+    if (hipError_t e = launch_copy(a, (hipStream_t)hip_stream)) return hip_failed(e, "infaas_sel_exec_copy");
     return INFAAS_SEL_OK;
 }
 

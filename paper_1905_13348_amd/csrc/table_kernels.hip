@@ -1,0 +1,315 @@
+// The pages of a worker's sequences (infaas_sel_exec_advance) and copies of pages (infaas_sel_exec_copy).
+#include "exec.h"
+
+#include <algorithm>
+
+namespace infaas {
+
+namespace {
+
+constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kRows = kMostSeqs / kThreads;      // sequences of a thread
+typedef long long i64;
+
+__device__ __forceinline__ int pages_of(const AdvanceArgs &a, int keys) { return (int)(((i64)keys + a.t.page_size - 1) >> a.page_shift); }
+__device__ __forceinline__ int length_of(const AdvanceArgs &a, int s) { return min(max(a.t.d_seq_len[s], 0), a.most); }
+__device__ __forceinline__ bool is_page(const AdvanceArgs &a, int page) { return (uint32_t)page < (uint32_t)a.t.num_pages; }
+// The sequence whose state a sequence goes on from, or -1.
+__device__ __forceinline__ int parent_of(const AdvanceArgs &a, int s)
+{
+    if (!a.parent) return s;
+    const int p = a.parent[s];
+    return (uint32_t)p < (uint32_t)a.t.num_seqs ? p : -1;
+}
+
+// ---- rows that go on from others ----------------------------------------------------------------
+
+// A workgroup takes some columns of the table, of all rows: what the rows are to be is read before any is written.  Counts
+// change by atomics, whose order does not matter.
+constexpr int kCells = 8192;
+__global__ __launch_bounds__(kThreads) void k_reparent(AdvanceArgs a, int columns)
+{
+    __shared__ int cell[kCells];
+    const int S = a.t.num_seqs;
+    for (i64 c0 = (i64)blockIdx.x * columns; c0 < a.t.table_width; c0 += (i64)gridDim.x * columns) {
+        for (int i = threadIdx.x; i < S * columns; i += kThreads) {
+            const int s = i / columns, p = parent_of(a, s);
+            const i64 c = c0 + i % columns;
+            cell[i] = p >= 0 && p != s && c < pages_of(a, length_of(a, p)) ? a.t.d_page_table[(i64)p * a.t.table_width + c] : -1;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < S * columns; i += kThreads) {
+            const int s = i / columns, p = parent_of(a, s);
+            const i64 c = c0 + i % columns;
+            if (p == s) continue;
+            const int had = pages_of(a, length_of(a, s)), has = p < 0 ? 0 : pages_of(a, length_of(a, p));
+            if (c >= max(had, has)) continue;
+            int32_t *const at = a.t.d_page_table + (i64)s * a.t.table_width + c;
+            const int before = c < had ? *at : -1, now = cell[i];
+            *at = now;
+            if (before == now) continue;
+            if (is_page(a, before)) atomicSub(&a.t.d_page_refs[before], 1);
+            if (is_page(a, now)) atomicAdd(&a.t.d_page_refs[now], 1);
+        }
+        __syncthreads();
+    }
+}
+
+// ---- lengths, pages, the batch's arrays ---------------------------------------------------------
+
+// Sum of v over the threads in front of this one; `all` becomes the sum over all threads.  (Two barriers.)
+__device__ __forceinline__ i64 before_me(i64 v, i64 *waves, i64 &all)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    i64 inc = v;
+    for (int d = 1; d < 64; d <<= 1) {
+        const i64 o = __shfl_up(inc, d);
+        if (lane >= d) inc += o;
+    }
+    __syncthreads();
+    if (lane == 63) waves[wave] = inc;
+    __syncthreads();
+    i64 sum = inc - v;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) sum += waves[w];
+        all += waves[w];
+    }
+    return sum;
+}
+
+// The last of n entries, which do not fall, that is at most x (the first is).
+__device__ __forceinline__ int last_upto(const int *v, int n, int x)
+{
+    int lo = 0, hi = n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (v[mid] <= x) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+// Sequence and position of tokens first, first + step, ...; `start` are the sequences' first tokens.
+__device__ __forceinline__ void fill_tokens(const AdvanceArgs &a, const int *start, int total, int first, int step)
+{
+    for (i64 i = first; i < a.t.max_tokens; i += step) {
+        int seq = -1, pos = -1;
+        if (i < total) {
+            seq = last_upto(start, a.t.num_seqs, (int)i);
+            pos = a.t.d_seq_len[seq] - a.t.d_taken[seq] + (int)i - start[seq];
+        }
+        a.t.d_token_seq[i] = seq;
+        a.t.d_token_pos[i] = pos;
+    }
+}
+
+// Batches of more tokens are written by a launch of their own.
+constexpr int kFewTokens = 4096;
+
+// One workgroup; thread t has sequences t, t + 1024, ...
+__global__ __launch_bounds__(kThreads) void k_advance(AdvanceArgs a)
+{
+    __shared__ int base[kMostSeqs];      // pages that those in front of a sequence need; at the end its first token
+    __shared__ int column[kMostSeqs];    // where its first new page goes; as ~column, where that is for a copy
+    __shared__ i64 waves[kWaves];
+    const int S = a.t.num_seqs, W = a.t.table_width, P = a.t.page_size, tid = threadIdx.x, lane = tid & 63;
+    int32_t *const refs = a.t.d_page_refs;
+    int len[kRows], more[kRows], need[kRows], last[kRows];      // last: the page to copy, or -1
+
+    // what goes
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        const int s = r * kThreads + tid;
+        len[r] = more[r] = 0;
+        int had = 0, has = 0;
+        if (s < S) {
+            const int p = parent_of(a, s);
+            const int before = p < 0 ? 0 : length_of(a, p);
+            more[r] = a.more[s];
+            len[r] = (int)max((i64)before + min(more[r], 0), (i64)0);
+            had = pages_of(a, before);
+            has = pages_of(a, len[r]);
+        }
+        unsigned long long rows = __ballot(had > has);      // (a wave to a row)
+        while (rows) {
+            const int l = __builtin_ctzll(rows);
+            rows &= rows - 1;
+            const int from = __shfl(has, l), to = __shfl(had, l);
+            int32_t *const row = a.t.d_page_table + (i64)(r * kThreads + (tid & ~63) + l) * W;
+            for (int c = from + lane; c < to; c += 64) {
+                const int page = row[c];
+                if (is_page(a, page)) atomicSub(&refs[page], 1);
+                row[c] = -1;
+            }
+        }
+    }
+    __threadfence();
+    __syncthreads();
+
+    // who asks for what
+    i64 tokens = 0, pages = 0;
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        const int s = r * kThreads + tid;
+        if (r * kThreads >= S) break;
+        bool wants = s < S && more[r] > 0 && (i64)len[r] + more[r] <= a.most;
+        i64 all;
+        const i64 upto = tokens + before_me(wants ? more[r] : 0, waves, all) + (wants ? more[r] : 0);
+        tokens += all;
+        wants = wants && upto <= a.t.max_tokens;
+        last[r] = -1;
+        need[r] = 0;
+        if (wants) {
+            if (len[r] & (P - 1)) {
+                const int page = a.t.d_page_table[(i64)s * W + (len[r] >> a.page_shift)];
+                if (is_page(a, page) && __hip_atomic_load(&refs[page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) > 1) last[r] = page;
+            }
+            need[r] = pages_of(a, len[r] + more[r]) - pages_of(a, len[r]) + (last[r] >= 0);
+        } else {
+            more[r] = 0;
+        }
+        const i64 at = pages + before_me(need[r], waves, all);
+        pages += all;
+        if (s < S) {
+            base[s] = (int)min(at, (i64)INT32_MAX);
+            const int c = pages_of(a, len[r]) - (last[r] >= 0);
+            column[s] = last[r] >= 0 ? ~c : c;
+        }
+    }
+    __syncthreads();
+
+    // free pages, in order, to who needs them
+    i64 found = 0;
+    constexpr int EACH = 16;      // pages of a thread at a time
+    for (i64 p0 = 0; p0 < a.t.num_pages && found < pages; p0 += kThreads * EACH) {
+        const i64 mine = p0 + tid * EACH;
+        uint32_t free = 0;
+        if (mine + EACH <= a.t.num_pages) {
+#pragma unroll
+            for (int q = 0; q < EACH / 4; ++q) {
+                const int4 v = *(const int4 *)(refs + mine + 4 * q);
+                free |= ((v.x == 0) | (v.y == 0) << 1 | (v.z == 0) << 2 | (v.w == 0) << 3) << 4 * q;
+            }
+        } else {
+            for (int q = 0; q < EACH; ++q)
+                if (mine + q < a.t.num_pages && refs[mine + q] == 0) free |= 1u << q;
+        }
+        i64 all;
+        i64 rank = found + before_me(__popc(free), waves, all);
+        found += all;
+        for (; free && rank < pages; ++rank, free &= free - 1) {
+            const int page = (int)mine + __builtin_ctz(free);
+            const int s = last_upto(base, S, (int)rank), j = (int)rank - base[s], c = column[s];
+            a.t.d_page_table[(i64)s * W + (c < 0 ? ~c : c) + j] = page;
+            refs[page] = 1;
+        }
+    }
+    __threadfence();
+    __syncthreads();
+
+    // who got it
+    i64 total = 0;
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        const int s = r * kThreads + tid;
+        if (r * kThreads >= S) break;
+        const bool served = s < S && more[r] > 0 && (need[r] == 0 || (i64)base[s] + need[r] <= found);
+        if (s < S && need[r] > 0) {
+            int32_t *const at = a.t.d_page_table + (i64)s * W + (column[s] < 0 ? ~column[s] : column[s]);
+            if (served) {
+                if (last[r] >= 0) {
+                    a.t.d_copies[3 * s] = last[r];
+                    a.t.d_copies[3 * s + 1] = at[0];
+                    a.t.d_copies[3 * s + 2] = len[r] & (P - 1);
+                    atomicSub(&refs[last[r]], 1);
+                }
+            } else {
+                for (int j = 0; j < found - base[s]; ++j) {      // (one sequence at most: the pages ended within what it needs)
+                    refs[at[j]] = 0;
+                    at[j] = j == 0 && last[r] >= 0 ? last[r] : -1;
+                }
+            }
+        }
+        if (s < S && !(served && last[r] >= 0)) a.t.d_copies[3 * s] = a.t.d_copies[3 * s + 1] = a.t.d_copies[3 * s + 2] = -1;
+        const int taken = served ? more[r] : 0;
+        i64 all;
+        const int start = (int)(total + before_me(taken, waves, all));
+        total += all;
+        if (s < S) {
+            a.t.d_seq_len[s] = len[r] + taken;
+            a.t.d_taken[s] = taken;
+            a.t.d_seq_start[s] = start;
+            base[s] = start;      // (its own entry alone is looked at in this loop)
+        }
+    }
+    if (tid == 0) a.t.d_seq_start[S] = (int)total;
+    if (a.t.max_tokens > kFewTokens) return;
+    __threadfence();
+    __syncthreads();
+    fill_tokens(a, base, (int)total, tid, kThreads);
+}
+
+__global__ __launch_bounds__(256) void k_tokens(AdvanceArgs a)
+{
+    __shared__ int start[kMostSeqs + 1];
+    for (int i = threadIdx.x; i <= a.t.num_seqs; i += 256) start[i] = a.t.d_seq_start[i];
+    __syncthreads();
+    fill_tokens(a, start, start[a.t.num_seqs], blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
+}
+
+// ---- copies of pages ----------------------------------------------------------------------------
+
+// Workgroups (sequence, keys or values, part): a thread takes 16 bytes at a time.
+__global__ __launch_bounds__(256) void k_copy(CopyArgs a)
+{
+    const int s = blockIdx.x, parts = gridDim.z;
+    const int64_t from = a.copies[3 * s], to = a.copies[3 * s + 1];
+    const int slots = min(a.copies[3 * s + 2], 1 << a.cache.page_shift);
+    if (from < 0 || from >= a.cache.num_pages || to < 0 || to >= a.cache.num_pages || slots <= 0) return;
+    const int size = a.cache.k_scale ? 1 : 2, pieces = a.bytes / 16;
+    uint8_t *const pool = (uint8_t *)(blockIdx.y ? a.cache.v : a.cache.k);
+    const int64_t all = (int64_t)slots * a.kv_heads * pieces;
+    for (int64_t i = blockIdx.z * 256 + threadIdx.x; i < all; i += parts * 256) {
+        const int64_t at = i / pieces / a.kv_heads * a.cache.slot_stride + i / pieces % a.kv_heads * a.cache.head_stride;
+        const int64_t byte = at * size + i % pieces * 16;
+        *(uint4 *)(pool + to * a.cache.page_stride * size + byte) = *(const uint4 *)(pool + from * a.cache.page_stride * size + byte);
+    }
+    if (a.cache.k_scale) {
+        uint8_t *const scale = blockIdx.y ? a.cache.v_scale : a.cache.k_scale;
+        const int64_t blocks = (int64_t)(((slots - 1) >> a.cache.block_shift) + 1) * a.kv_heads;
+        for (int64_t i = blockIdx.z * 256 + threadIdx.x; i < blocks; i += parts * 256) {
+            const int64_t at = i / a.kv_heads * a.cache.scale_block_stride + i % a.kv_heads * a.cache.scale_head_stride;
+            scale[to * a.cache.scale_page_stride + at] = scale[from * a.cache.scale_page_stride + at];
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_advance(const AdvanceArgs &a, hipStream_t s)
+{
+    if (a.parent) {
+        const int columns = std::max(1, std::min(16, kCells / a.t.num_seqs));
+        k_reparent<<<std::min(4096, (a.t.table_width - 1) / columns + 1), kThreads, 0, s>>>(a, columns);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    k_advance<<<1, kThreads, 0, s>>>(a);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (a.t.max_tokens > kFewTokens) {
+        k_tokens<<<std::min(1024, (a.t.max_tokens - 1) / 256 + 1), 256, 0, s>>>(a);
+        return hipGetLastError();
+    }
+    return hipSuccess;
+}
+
+hipError_t launch_copy(const CopyArgs &a, hipStream_t s)
+{
+    const int64_t most = ((int64_t)1 << a.cache.page_shift) * a.kv_heads * (a.bytes / 16);
+    const dim3 grid((unsigned)a.num_seqs, 2, (unsigned)std::max<int64_t>(1, std::min<int64_t>(16, most / 2048)));
+    k_copy<<<grid, 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace infaas

@@ -17,7 +17,7 @@ from __future__ import annotations
 import ctypes
 from typing import Optional
 
-from .binding import InfaasSelError, _AppendArgs, _Batch, _Cache, _Scales, _stream_ptr, _use_torch, load_library
+from .binding import InfaasSelError, _AppendArgs, _Batch, _Cache, _Scales, _stream_ptr, _Table, _use_torch, load_library
 
 _TYPES = None        # torch type -> INFAAS_SEL_TYPE_*
 
@@ -175,6 +175,37 @@ class Batch:
         self._c.d_plan, self._c.plan_bytes = self.plan_memory.data_ptr(), size
 
 
+class Table:
+    """The pages of a worker's sequences (infaas_sel_table), with all of its arrays: int32 tensors that are made here, empty, on
+    torch's current stream.
+
+    State, which ``Executor.advance`` takes a step further: ``page_table`` [sequences, width], ``seq_len`` [sequences],
+    ``page_refs`` [pages].  What it writes beside that: ``seq_start``, ``token_seq`` and ``token_pos``, which with the state are the arrays
+    of a batch of ``max_tokens`` tokens (``arrays()``), ``taken`` [sequences] and ``copies`` [sequences, 3]."""
+
+    def __init__(self, num_seqs: int, table_width: int, page_size: int, num_pages: int, max_tokens: int, device: int = 0):
+        torch = _use_torch()
+        for name, n, most in (("num_seqs", num_seqs, 4096), ("table_width", table_width, 2 ** 31 - 1), ("page_size", page_size, 65536),
+                              ("num_pages", num_pages, 2 ** 31 - 1), ("max_tokens", max_tokens, 2 ** 31 - 1)):
+            if not 1 <= n <= most:
+                raise ValueError(f"{name}: {n} is not within 1 .. {most}")
+        if page_size & (page_size - 1):
+            raise ValueError(f"page_size: {page_size} is not a power of two")
+        full = lambda value, *shape: torch.full(shape, value, dtype=torch.int32, device=torch.device("cuda", device))
+        self.num_seqs, self.table_width, self.page_size, self.num_pages, self.max_tokens = num_seqs, table_width, page_size, num_pages, max_tokens
+        self.device = device
+        self.page_table, self.seq_len, self.page_refs = full(-1, num_seqs, table_width), full(0, num_seqs), full(0, num_pages)
+        self.seq_start, self.token_seq, self.token_pos = full(0, num_seqs + 1), full(-1, max_tokens), full(-1, max_tokens)
+        self.taken, self.copies = full(0, num_seqs), full(-1, num_seqs, 3)
+        self._keep = (self.page_table, self.seq_len, self.page_refs, self.seq_start, self.token_seq, self.token_pos, self.taken, self.copies)
+        self._c = _Table(num_seqs, table_width, page_size, num_pages, max_tokens, 0, *(t.data_ptr() for t in self._keep))
+        self._ref = ctypes.byref(self._c)
+
+    def arrays(self) -> dict:
+        """What ``Executor.batch`` takes."""
+        return dict(token_seq=self.token_seq, token_pos=self.token_pos, seq_start=self.seq_start, seq_len=self.seq_len, page_table=self.page_table)
+
+
 class Executor:
     """One executor handle of the library (infaas_sel_exec_create ... infaas_sel_exec_destroy)."""
 
@@ -189,6 +220,31 @@ class Executor:
 
     def batch(self, cache: PagedCache, heads: int, **arrays) -> Batch:
         return Batch(cache, heads, **arrays)
+
+    def table(self, num_seqs: int, table_width: int, page_size: int, num_pages: int, max_tokens: int) -> Table:
+        return Table(num_seqs, table_width, page_size, num_pages, max_tokens, self.device)
+
+    def advance(self, table: Table, new, parent=None, stream=None) -> None:
+        """All sequences a step further: ``new`` tokens of each (below 0: keys that are dropped), going on from ``parent`` (None:
+        from itself; a number that is no sequence's: from nothing)."""
+        if table.device != self.device:
+            raise ValueError(f"an executor of device {self.device} with a table on {table.device}")
+        i32 = _use_torch().int32
+        status = self._lib.infaas_sel_exec_advance(
+            self._h, table._ref, _vector(new, i32, "new", self.device, table.num_seqs),
+            None if parent is None else _vector(parent, i32, "parent", self.device, table.num_seqs), _stream_ptr(stream, self.device))
+        if status:
+            _check(status)
+
+    def copy(self, cache: PagedCache, table: Table, stream=None) -> None:
+        """What the table's latest step copies from page to page, in one layer's cache."""
+        if table.device != self.device or cache.device != self.device:
+            raise ValueError(f"an executor of device {self.device} with a cache on {cache.device} and a table on {table.device}")
+        scales = getattr(cache, "_scales", None)
+        status = self._lib.infaas_sel_exec_copy(self._h, cache._ref, None if scales is None else cache._scales_ref, table._ref,
+                                                _stream_ptr(stream, self.device))
+        if status:
+            _check(status)
 
     def reserve(self, cache: PagedCache, batch: Batch) -> None:
         self._agree(cache, batch)
