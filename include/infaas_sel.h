@@ -797,6 +797,32 @@ int infaas_sel_exec_sample(infaas_sel_exec_t *x, int32_t rows, int32_t vocab, in
                            const float *d_top_p, const float *d_min_p, const float *d_draw,
                            int32_t *d_out_token, float *d_out_prob, void *hip_stream);
 
+/*
+ * A step of beam search: the best continuations of every query's beams.  Beam w of query q has row q * beams + w of the logits and
+ * a score, the sum of the logarithms of its tokens' probabilities so far.  Continuing it with token i has the score
+ *     d_scores[q][w] + x_i - log(sum over j of exp(x_j)),
+ * and they are ranked by score times d_factor[q][w] (a factor of its length, say; positive; null: 1), the greatest first, equal ones
+ * by beam and then by token.  A beam that has ended (d_ended[q][w] not 0) has one continuation, by end_token, at its own
+ * score.  One whose score is not finite, or whose factor is not finite and positive, has none.
+ *   d_logits       [queries * beams][vocab], type INFAAS_SEL_TYPE_*, rows row_stride elements apart
+ *   d_scores, d_ended, d_factor  [queries][beams]; the last two may be null
+ *   d_out_parent   [queries][picks] row of the beam that goes on (a sequence's number, for infaas_sel_exec_advance)
+ *   d_out_token    [queries][picks];  d_out_score [queries][picks] (may be d_scores when picks == beams)
+ * Where there are fewer continuations than picks, the others are -1, -1 and minus infinity.  Logits of -infinity and NaN are never
+ * picked; among logits of +infinity the probabilities are equal, of the others then 0.  Sums and scores are held in 64 bits, and
+ * weights are summed exactly: rows with the same logits have the same scores.
+ * queries >= 0, beams and picks 1..64, vocab 1..1,048,576, end_token 0..vocab-1 where d_ended is given.
+ * The handle's scratch memory grows as needed, but not while the stream is being captured (infaas_sel_exec_reserve_beam).
+ * Errors: INVALID_ARG, HIP, OOM.
+ */
+int infaas_sel_exec_beam(infaas_sel_exec_t *x, int32_t queries, int32_t beams, int32_t vocab, int32_t picks, int32_t type,
+                         const void *d_logits, int64_t row_stride, const float *d_scores, const int32_t *d_ended,
+                         const float *d_factor, int32_t end_token, int32_t *d_out_parent, int32_t *d_out_token,
+                         float *d_out_score, void *hip_stream);
+
+/* Grow the handle's scratch memory for infaas_sel_exec_beam with these sizes.  Errors: INVALID_ARG, HIP, OOM. */
+int infaas_sel_exec_reserve_beam(infaas_sel_exec_t *x, int32_t queries, int32_t beams, int32_t vocab, int32_t picks, int32_t type);
+
 /* Static text for a status code. */
 const char *infaas_sel_strerror(int status);
 

@@ -104,7 +104,7 @@ EXPORTED = ("infaas_sel_create", "infaas_sel_load_variants", "infaas_sel_update_
             "infaas_sel_exec_create", "infaas_sel_exec_destroy", "infaas_sel_exec_plan_bytes", "infaas_sel_exec_reserve",
             "infaas_sel_exec_plan", "infaas_sel_exec_append", "infaas_sel_exec_attend", "infaas_sel_exec_sample",
             "infaas_sel_exec_append_scaled", "infaas_sel_exec_attend_scaled", "infaas_sel_exec_read",
-            "infaas_sel_exec_advance", "infaas_sel_exec_copy")
+            "infaas_sel_exec_advance", "infaas_sel_exec_copy", "infaas_sel_exec_beam", "infaas_sel_exec_reserve_beam")
 
 
 def library_path() -> str:
@@ -176,6 +176,8 @@ def load_library() -> ctypes.CDLL:
     tp = ctypes.POINTER(_Table)
     lib.infaas_sel_exec_advance.argtypes = [vp, tp, vp, vp, vp]
     lib.infaas_sel_exec_copy.argtypes = [vp, cp, sp, tp, vp]
+    lib.infaas_sel_exec_beam.argtypes = [vp, i32, i32, i32, i32, i32, vp, i64, vp, vp, vp, i32, vp, vp, vp, vp]
+    lib.infaas_sel_exec_reserve_beam.argtypes = [vp, i32, i32, i32, i32, i32]
     for name in EXPORTED:
         if name not in ("infaas_sel_destroy", "infaas_sel_strerror", "infaas_sel_last_error", "infaas_sel_exec_destroy",
                         "infaas_sel_exec_plan_bytes"):

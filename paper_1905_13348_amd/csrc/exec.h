@@ -149,6 +149,22 @@ struct CopyArgs {
     const int32_t *copies;
 };
 
+struct BeamArgs {
+    const void *logits;
+    int64_t row_stride;
+    int32_t queries, beams, vocab, picks, end_token, parts;
+    const float *scores, *factor;
+    const int32_t *ended;
+    int32_t *out_parent, *out_token;
+    float *out_score;
+    // of every part of every row: its best (order key of the logit, ~token; 0: none), the sum of its weights, its maximum
+    unsigned long long *best;
+    double *sum;
+    float *top;
+};
+struct BeamSizes { int64_t parts, sum_at, top_at, bytes; };
+constexpr int kMostBeams = 64;       // beams, and picks
+
 constexpr int kMostSeqs = 4096;      // of a table
 
 struct SampleArgs {
@@ -208,6 +224,8 @@ hipError_t launch_append_scaled(const AppendScaledArgs &a, int32_t type, hipStre
 hipError_t launch_read(const ReadArgs &a, int32_t type, hipStream_t s);
 hipError_t launch_advance(const AdvanceArgs &a, hipStream_t s);
 hipError_t launch_copy(const CopyArgs &a, hipStream_t s);
+BeamSizes beam_sizes(int32_t queries, int32_t beams, int32_t vocab, int32_t picks, int32_t type);
+hipError_t launch_beam(const BeamArgs &a, int32_t type, hipStream_t s);
 hipError_t launch_sample(const SampleArgs &a, int32_t type, hipStream_t s);
 
 }  // namespace infaas

@@ -141,14 +141,14 @@ int64_t scratch_for(const infaas_sel_cache *c, const PlanSizes &z)
 }
 
 // At least `bytes` of scratch memory; `s` is the stream of the call, or null outside one.
-int ensure(infaas_sel_exec *x, int64_t bytes, hipStream_t s, bool in_call)
+int ensure(infaas_sel_exec *x, int64_t bytes, hipStream_t s, bool in_call, const char *reserve = "infaas_sel_exec_reserve")
 {
     if (x->scratch_bytes >= bytes) return INFAAS_SEL_OK;
     if (in_call) {
         hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
         if (hipError_t e = hipStreamIsCapturing(s, &st)) return hip_failed(e, "hipStreamIsCapturing");
         if (st != hipStreamCaptureStatusNone)
-            return refuse("scratch memory has to grow while the stream is being captured: call infaas_sel_exec_reserve first");
+            return refuse("scratch memory has to grow while the stream is being captured: call %s first", reserve);
     }
     // (half as much again, so that what is retired stays below twice what is in use)
     const int64_t want = std::max(bytes, x->scratch_bytes + x->scratch_bytes / 2);
@@ -197,6 +197,17 @@ PlanView plan_view(const infaas_sel_batch *b, const PlanSizes &z)
 {
     char *p = (char *)b->d_plan;
     return PlanView{(PlanHeader *)p, (PlanToken *)(p + z.tokens_at), (PlanUnit *)(p + z.units_at), (PlanItem *)(p + z.items_at)};
+}
+
+int check_beam(int32_t queries, int32_t beams, int32_t vocab, int32_t picks, int32_t type)
+{
+    if (queries < 0) return refuse("beam: %d queries", queries);
+    if (beams < 1 || beams > kMostBeams || picks < 1 || picks > kMostBeams)
+        return refuse("beam: %d beams and %d picks (1 .. %d)", beams, picks, kMostBeams);
+    if (vocab < 1 || vocab > 1 << 20) return refuse("beam: a vocabulary of %d (1 .. 1048576)", vocab);
+    if (type != INFAAS_SEL_TYPE_FP32 && type != INFAAS_SEL_TYPE_BF16 && type != INFAAS_SEL_TYPE_FP16) return refuse("beam: type %d", type);
+    if ((int64_t)queries * beams > INT32_MAX) return refuse("beam: %d queries of %d beams", queries, beams);
+    return INFAAS_SEL_OK;
 }
 
 int check_table(const infaas_sel_table *t)
@@ -447,6 +458,37 @@ int infaas_sel_exec_sample(infaas_sel_exec_t *x, int32_t rows, int32_t vocab, in
     SampleArgs a{d_logits, row_stride, rows, vocab, d_temperature, d_top_p, d_min_p, d_draw, d_top_k, d_out_token, d_out_prob};
     if (hipError_t e = launch_sample(a, type, (hipStream_t)hip_stream)) return hip_failed(e, "infaas_sel_exec_sample");
     return INFAAS_SEL_OK;
+}
+
+int infaas_sel_exec_beam(infaas_sel_exec_t *x, int32_t queries, int32_t beams, int32_t vocab, int32_t picks, int32_t type,
+                         const void *d_logits, int64_t row_stride, const float *d_scores, const int32_t *d_ended,
+                         const float *d_factor, int32_t end_token, int32_t *d_out_parent, int32_t *d_out_token,
+                         float *d_out_score, void *hip_stream)
+{
+    if (!x) return refuse("executor: null");
+    if (int rc = check_beam(queries, beams, vocab, picks, type)) return rc;
+    if (d_ended && (end_token < 0 || end_token >= vocab)) return refuse("beam: end token %d of a vocabulary of %d", end_token, vocab);
+    if (queries == 0) return INFAAS_SEL_OK;
+    if (!d_logits || !d_scores || !d_out_parent || !d_out_token || !d_out_score) return refuse("beam: null arrays");
+    if ((uintptr_t)d_logits % (type == INFAAS_SEL_TYPE_FP32 ? 4 : 2)) return refuse("beam: logits are not aligned to their type");
+    OnDevice on(x->device);
+    if (on.err != hipSuccess) return hip_failed(on.err, "hipSetDevice");
+    const BeamSizes z = beam_sizes(queries, beams, vocab, picks, type);
+    if (int rc = ensure(x, z.bytes, (hipStream_t)hip_stream, true, "infaas_sel_exec_reserve_beam")) return rc;
+    char *const p = (char *)x->scratch;
+    const BeamArgs a{d_logits, row_stride, queries, beams, vocab, picks, end_token, (int32_t)z.parts, d_scores, d_factor, d_ended,
+                     d_out_parent, d_out_token, d_out_score, (unsigned long long *)p, (double *)(p + z.sum_at), (float *)(p + z.top_at)};
+    if (hipError_t e = launch_beam(a, type, (hipStream_t)hip_stream)) return hip_failed(e, "infaas_sel_exec_beam");
+    return INFAAS_SEL_OK;
+}
+
+int infaas_sel_exec_reserve_beam(infaas_sel_exec_t *x, int32_t queries, int32_t beams, int32_t vocab, int32_t picks, int32_t type)
+{
+    if (!x) return refuse("executor: null");
+    if (int rc = check_beam(queries, beams, vocab, picks, type)) return rc;
+    OnDevice on(x->device);
+    if (on.err != hipSuccess) return hip_failed(on.err, "hipSetDevice");
+    return ensure(x, beam_sizes(queries, beams, vocab, picks, type).bytes, nullptr, false);
 }
 
 }  // extern "C"

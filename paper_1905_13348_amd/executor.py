@@ -345,6 +345,47 @@ class Executor:
         if status:
             _check(status)
 
+    def beam(self, logits, scores, parent, token, score, *, ended=None, factor=None, end_token: int = -1, stream=None) -> None:
+        """The best continuations of every query's beams: logits [queries * beams, vocab], ``scores`` [queries, beams], into
+        ``parent``, ``token`` and ``score`` [queries, picks].  ``ended`` (int32) and ``factor`` (float32) are [queries, beams] or None."""
+        torch = _use_torch()
+        dev = self.device
+        if not isinstance(logits, torch.Tensor) or logits.get_device() != dev or logits.dim() != 2 or logits.dtype not in _types() \
+                or (logits.shape[1] > 1 and logits.stride(1) != 1):
+            raise TypeError(f"logits: tensor [rows, vocab] on device {dev} expected, the last dimension consecutive")
+        for name, t in (("scores", scores), ("token", token)):
+            if not isinstance(t, torch.Tensor) or t.dim() != 2:
+                raise TypeError(f"{name}: tensor of two dimensions expected")
+        queries, beams = scores.shape
+        picks, vocab = token.shape[1], logits.shape[1]
+        if logits.shape[0] != queries * beams:
+            raise TypeError(f"logits: {queries * beams} rows expected for scores {[queries, beams]}, not {logits.shape[0]}")
+
+        def matrix(t, dtype, name, columns):
+            if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() \
+                    or tuple(t.shape) != (queries, columns):
+                raise TypeError(f"{name}: contiguous {dtype} tensor {[queries, columns]} on device {dev} expected")
+            _no_gradient(t, name)
+            return t.data_ptr()
+
+        _no_gradient(logits, "logits")
+        f32, i32 = torch.float32, torch.int32
+        status = self._lib.infaas_sel_exec_beam(
+            self._h, _i32(queries, "queries"), _i32(beams, "beams"), _i32(vocab, "vocab"), _i32(picks, "picks"), _types()[logits.dtype],
+            logits.data_ptr(), logits.stride(0), matrix(scores, f32, "scores", beams),
+            None if ended is None else matrix(ended, i32, "ended", beams), None if factor is None else matrix(factor, f32, "factor", beams),
+            _i32(end_token, "end_token"), matrix(parent, i32, "parent", picks), matrix(token, i32, "token", picks),
+            matrix(score, f32, "score", picks), _stream_ptr(stream, self.device))
+        if status:
+            _check(status)
+
+    def reserve_beam(self, queries: int, beams: int, vocab: int, picks: int, dtype) -> None:
+        """Scratch memory for ``beam`` with these sizes, for calls that are recorded into a graph."""
+        if dtype not in _types():
+            raise TypeError(f"dtype {dtype}: float32, bfloat16 or float16")
+        _check(self._lib.infaas_sel_exec_reserve_beam(self._h, _i32(queries, "queries"), _i32(beams, "beams"), _i32(vocab, "vocab"),
+                                                      _i32(picks, "picks"), _types()[dtype]))
+
     def destroy(self) -> None:
         if self._h:
             self._lib.infaas_sel_exec_destroy(self._h)
