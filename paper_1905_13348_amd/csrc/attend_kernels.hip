@@ -224,11 +224,19 @@ template <> struct Mfma<bf16_t> {
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
     }
+    static __device__ __forceinline__ vec<float, 4> run(vec<bf16_t, 8> a, vec<bf16_t, 8> b, vec<float, 4> c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
 };
 template <> struct Mfma<fp16_t> {
     static __device__ __forceinline__ vec<float, 16> run(vec<fp16_t, 8> a, vec<fp16_t, 8> b, vec<float, 16> c)
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ vec<float, 4> run(vec<fp16_t, 8> a, vec<fp16_t, 8> b, vec<float, 4> c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
     }
 };
 
@@ -292,6 +300,254 @@ __device__ __forceinline__ float apart(float s, float scale, float ref)
     return t - ref;
 }
 
+// ---- items of few rows over codes -------------------------------------------------------------
+
+// A part of a row's result: reference of the weights, their sum, the weighted sums of four dimensions.
+struct RowPart { float m, l; vec<float, 4> o; };
+
+__device__ __forceinline__ void join(RowPart &a, float m1, float l1, vec<float, 4> o1)
+{
+    if (m1 == -INFINITY && l1 == 0) return;        // nothing seen
+    if (a.m == -INFINITY && a.l == 0) {            // nothing so far
+        a = RowPart{m1, l1, o1};
+        return;
+    }
+    // (a sum of NaN with a maximum of -infinity, of scores that are all NaN, stays NaN times 0)
+    const float m2 = fmaxf(a.m, m1), f = exp2_fast(a.m - m2), g = exp2_fast(m1 - m2);
+    a.o = a.o * f + o1 * g;
+    a.l = a.l * f + l1 * g;
+    a.m = m2;
+}
+
+constexpr int kNarrow = 16;      // rows of an item that its waves go through side by side
+
+// Up to sixteen rows: what bounds them is the cache's bytes, and a wave that computes while three stand by is too slow for
+// these.  So each wave has keys of its own, 32 at a time, nothing waits for another wave until the end, and the waves' parts are
+// joined through LDS.  Lane (key, c) loads the quarter c of a key's and of a value's codes, in one piece; with the dimensions
+// numbered that way for both operands the codes go from memory to the first product through registers alone.  Values are
+// written to the wave's part of LDS as numbers, to be read transposed.
+template <typename T, int D>
+__device__ __forceinline__ void narrow_item(const AttendArgs &a, const PlanItem &it, uint4 *lds0, uint4 *lds1, uint4 *lds2, uint4 *lds3,
+                                            float2 (*ml)[kNarrow])
+{
+    constexpr int KEYS = 32, ROW = D * 2, PIECES = D / 64, CH = D / 8;      // PIECES: of 16 codes, of a lane's quarter
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, c = lane >> 4;
+    const int G = a.batch.heads / a.batch.kv_heads, rows = it.nt * G;
+    const bool valid = col < rows;
+    const int rt = valid ? col / G : 0, token = it.t0 + rt, head = it.head * G + col - rt * G;
+    const int lim = valid ? min(a.plan.tokens[token].limit, it.k1) : 0;
+    vec<T, 8> q[D / 32];
+#pragma unroll
+    for (int kk = 0; kk < D / 32; ++kk) {
+        q[kk] = vec<T, 8>{};
+        if (valid) q[kk] = *(const vec<T, 8> *)((const T *)a.q + token * a.q_token_stride + head * a.q_head_stride + c * (D / 4) + kk * 8);
+    }
+    int end = lim, lo = lim > it.k0 ? lim : 0x7fffffff;      // how far the rows see: one of them, all that see anything
+    for (int d = 1; d < 16; d <<= 1) { end = max(end, __shfl_xor(end, d)); lo = min(lo, __shfl_xor(lo, d)); }
+    end = __builtin_amdgcn_readfirstlane(end);
+    lo = __builtin_amdgcn_readfirstlane(lo);
+
+    char *const lv = (char *)(wave < 2 ? wave == 0 ? lds0 : lds1 : wave == 2 ? lds2 : lds3);      // KEYS * ROW bytes each
+    // pieces of a row change places, so that lanes with neighbouring rows write, and read, other banks
+    auto turn = [](int row) { return CH == 8 ? (row >> 1) & 7 : row & 15; };
+    const int page_mask = (1 << a.cache.page_shift) - 1;
+    const int32_t *const table = a.cache.table + (int64_t)it.seq * a.cache.table_width;
+
+    vec<float, 4> o[D / 16];
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) o[dt] = vec<float, 4>{};
+    float m = -INFINITY, l = 0;
+    bool far = false, odd = false;
+    int first_there = 0x7fffffff;
+
+    int page[2];                                     // of the next tile's keys; -1: not there
+    vec<uint32_t, 4> kc[2][PIECES], vc[2][PIECES];   // this tile's codes
+    uint32_t ke[2], ve[2];
+    bool there[2];
+    auto look_up = [&](int kt) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int key = kt + h * 16 + col, p = table[min(key, end - 1) >> a.cache.page_shift];      // (no branch: it would wait)
+            page[h] = key < end ? p : -1;
+        }
+    };
+    int64_t at[2];
+    auto locate = [&](int kt) {      // and the scales
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            there[h] = page[h] >= 0 && page[h] < a.cache.num_pages;
+            const int64_t p = there[h] ? page[h] : 0;
+            const int slot = there[h] ? (kt + h * 16 + col) & page_mask : 0;
+            at[h] = p * a.cache.page_stride + (int64_t)slot * a.cache.slot_stride + it.head * a.cache.head_stride + c * (D / 4);
+            const int64_t s = p * a.cache.scale_page_stride + (int64_t)(slot >> a.cache.block_shift) * a.cache.scale_block_stride +
+                              it.head * a.cache.scale_head_stride;
+            ke[h] = a.cache.k_scale[s];
+            ve[h] = a.cache.v_scale[s];
+        }
+    };
+    auto load = [&](vec<uint32_t, 4> (&to)[2][PIECES], const void *pool) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int x = 0; x < PIECES; ++x) to[h][x] = *(const vec<uint32_t, 4> *)((const uint8_t *)pool + at[h] + x * 16);
+    };
+    int kt = it.k0 + wave * KEYS;
+    if (kt < end) {
+        look_up(kt);
+        locate(kt);
+        load(kc, a.cache.k);
+        load(vc, a.cache.v);
+        look_up(kt + 4 * KEYS);
+    }
+    for (; kt < end; kt += 4 * KEYS) {
+        const unsigned long long ballots[2] = {__ballot(there[0]), __ballot(there[1])};
+        const uint32_t bits = (uint32_t)(ballots[0] & 0xffff) | (uint32_t)(ballots[1] & 0xffff) << 16;
+        const bool part = kt + KEYS > lo;      // some rows see keys that others do not
+        if (bits && first_there == 0x7fffffff) first_there = kt + __builtin_ctz(bits);
+        // values, as numbers: zeros where nothing is there; where rows differ in what they see, what is no number is taken out
+        // here and added at the end where it is seen (a weight of zero would make NaN of it)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int x = 0; x < PIECES; ++x)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    union { vec<T, 8> v; vec<uint32_t, 4> w; } u;
+                    u.v = decode8<T>(vec<uint32_t, 2>{vc[h][x][2 * y], vc[h][x][2 * y + 1]}, ve[h]);
+                    if (bits != ~0u || part) {
+                        if (!there[h]) u.w = vec<uint32_t, 4>{};
+                        else if (part) odd |= take_out<T>(u.w);
+                    }
+                    const int row = h * 16 + col;
+                    *(vec<T, 8> *)(lv + row * ROW + (((c * PIECES + x) * 2 + y) ^ turn(row)) * 16) = u.v;
+                }
+        vec<float, 4> s[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            s[h] = vec<float, 4>{};
+#pragma unroll
+            for (int kk = 0; kk < D / 32; ++kk)
+                s[h] = Mfma<T>::run(decode8<T>(vec<uint32_t, 2>{kc[h][kk / 2][kk % 2 * 2], kc[h][kk / 2][kk % 2 * 2 + 1]}, ke[h]), q[kk], s[h]);
+        }
+        if (kt + 4 * KEYS < end) {      // the next tile is under way while this one's weights and products are computed
+            locate(kt + 4 * KEYS);
+            load(kc, a.cache.k);
+            load(vc, a.cache.v);
+            look_up(kt + 8 * KEYS);
+        }
+        if (part || bits != ~0u) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int i = h * 16 + c * 4 + x;
+                    s[h][x] = kt + i < lim && (bits >> i & 1) ? s[h][x] : -INFINITY;
+                }
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int x = 1; x < 8; ++x) top = fmaxf(top, s[x / 4][x % 4]);
+        // the weights' reference, as where tiles are full; a row's four lanes agree on it whenever it moves
+        float scale = a.scale_log2;
+        float ref = m == -INFINITY ? 0.0f : m;
+        if (__any(apart(top, scale, m) > kSlack + kRaise<T>) || far) {
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float m2 = fmaxf(m, apart(top, scale, kRaise<T>));
+            const float f = m2 == -INFINITY ? 1.0f : exp2_fast(m - m2);
+            m = m2;
+            l *= f;
+#pragma unroll
+            for (int dt = 0; dt < D / 16; ++dt) o[dt] *= f;
+            ref = m == -INFINITY ? 0.0f : m;
+            far = __any(fabsf(m) > kFused && m > -INFINITY);
+            if (far) {
+#pragma unroll
+                for (int x = 0; x < 8; ++x) s[x / 4][x % 4] = apart(s[x / 4][x % 4], scale, ref);
+                scale = 1.0f;
+                ref = 0.0f;
+            }
+        }
+        vec<T, 8> pt;
+#pragma unroll
+        for (int x = 0; x < 8; x += 2) {
+            const vec<float, 2> e = {exp2_fast(s[x / 4][x % 4] * scale - ref), exp2_fast(s[x / 4][x % 4 + 1] * scale - ref)};
+            l += e[0];
+            l += e[1];
+            const vec<T, 2> y = __builtin_convertvector(e, vec<T, 2>);      // (the rounding of full tiles)
+            pt[x] = y[0];
+            pt[x + 1] = y[1];
+        }
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) {
+            union { vec<short, 4> h[2]; vec<T, 8> v; } vf;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int row = h * 16 + c * 4 + col / 4;
+                vf.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_short4 *)(lv + row * ROW + ((dt * 2 + (col & 3) / 2) ^ turn(row)) * 16 + (col & 1) * 8));
+            }
+            o[dt] = Mfma<T>::run(vf.v, pt, o[dt]);
+        }
+    }
+    if (__any(odd)) {      // the values that were taken out, of the tiles that they were taken out of
+        for (int t = it.k0 + wave * KEYS; t < end; t += 4 * KEYS) {
+            if (t + KEYS <= lo) continue;
+            for (int key = t; key < min(t + KEYS, lim); ++key) {
+                const int64_t page = table[key >> a.cache.page_shift];
+                if (page < 0 || page >= a.cache.num_pages) continue;
+                const int slot = key & page_mask;
+                const uint8_t *v = (const uint8_t *)a.cache.v + page * a.cache.page_stride + (int64_t)slot * a.cache.slot_stride +
+                                   it.head * a.cache.head_stride + 4 * c;
+                const uint32_t e8 = a.cache.v_scale[page * a.cache.scale_page_stride +
+                                                    (int64_t)(slot >> a.cache.block_shift) * a.cache.scale_block_stride + it.head * a.cache.scale_head_stride];
+#pragma unroll
+                for (int dt = 0; dt < D / 16; ++dt) {
+                    const vec<T, 4> y = decode4<T>(*(const uint32_t *)(v + dt * 16), e8);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (!(fabsf((float)y[e]) < INFINITY)) o[dt][e] += (float)y[e];
+                }
+            }
+        }
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (lim <= it.k0) {
+        m = -INFINITY;
+        l = 0;
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) o[dt] = vec<float, 4>{};
+    }
+    if (l == 0 && lim > first_there) m = kNothing;
+
+    // the waves' parts
+    __syncthreads();
+    if (c == 0) ml[wave][col] = float2{m, l};
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) ((vec<float, 4> *)lv)[col * (D / 4) + ((dt * 4 + c) ^ col)] = o[dt];
+    __syncthreads();
+    for (int i = tid; i < rows * (D / 4); i += 256) {
+        const int r = i / (D / 4), d = i % (D / 4), t = r / G;
+        RowPart sum{-INFINITY, 0, vec<float, 4>{}};
+        const int at = r * (D / 4) + (d ^ r);
+        join(sum, ml[0][r].x, ml[0][r].y, ((const vec<float, 4> *)lds0)[at]);
+        join(sum, ml[1][r].x, ml[1][r].y, ((const vec<float, 4> *)lds1)[at]);
+        join(sum, ml[2][r].x, ml[2][r].y, ((const vec<float, 4> *)lds2)[at]);
+        join(sum, ml[3][r].x, ml[3][r].y, ((const vec<float, 4> *)lds3)[at]);
+        if (it.base < 0) {
+            const float f = one_by(sum.m, sum.l);
+            T *out = (T *)a.out + (it.t0 + t) * a.out_token_stride + (it.head * G + r - t * G) * a.out_head_stride + d * 4;
+            *(vec<T, 4> *)out = vec<T, 4>{(T)(sum.o[0] * f), (T)(sum.o[1] * f), (T)(sum.o[2] * f), (T)(sum.o[3] * f)};
+        } else {
+            const int64_t row = (int64_t)it.base + r;
+            if (d == 0) a.part_ml[row] = float2{sum.m, sum.l};
+            *(vec<float, 4> *)(a.part_o + row * D + d * 4) = sum.o;
+        }
+    }
+    __syncthreads();
+}
+
 // A workgroup of four waves takes items of up to 128 rows, 32 to a wave.  With K the A operand, S^T = K Q^T leaves a lane
 // with scores of ONE row (its column), so the running maximum and sum are a lane's own, and P^T is in registers where
 // the B operand of O^T = V^T P^T wants it: key slots of the second product are numbered as the first one leaves them.
@@ -315,6 +571,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
     constexpr int KB = D == 256 ? 32 : 64, CH = D / 8, LOADS = KB * CH / 256, ROW = D * 2;
     constexpr int PIECE = CODED ? 16 : 8, CODE_LOADS = LOADS / 2 < 1 ? 1 : LOADS / 2;      // elements of 16 bytes in the cache
     __shared__ uint4 lk0[KB * CH], lv0[KB * CH], lk1[KB * CH], lv1[KB * CH];
+    __shared__ float2 narrow_ml[CODED ? 4 : 1][kNarrow];
     __shared__ int64_t where[4][KB];      // of the next tiles' rows, in pieces (of what is not there: any that is)
     __shared__ int64_t scale_at[CODED ? 4 : 1][CODED ? KB : 1];      // and of their scales
     constexpr int MINE = KB / 4;          // rows of a tile that each wave looks up
@@ -341,9 +598,16 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
     const int die = blockIdx.x & (kDies - 1), step = gridDim.x / kDies;
     const int first0 = a.plan.head->die_start[0][die], first1 = a.plan.head->die_start[1][die];
     const int n0 = a.plan.head->die_start[0][die + 1] - first0, n = n0 + a.plan.head->die_start[1][die + 1] - first1;
+    if constexpr (CODED) {      // (a loop of its own: within the other one both kinds' registers are too many)
+        for (int i = blockIdx.x / kDies; i < n; i += step) {
+            const PlanItem it = a.plan.items[i < n0 ? first0 + i : first1 + i - n0];
+            if (it.nt * G <= kNarrow) narrow_item<T, D>(a, it, lk0, lv0, lk1, lv1, narrow_ml);
+        }
+    }
     for (int i = blockIdx.x / kDies; i < n; i += step) {
         const PlanItem it = a.plan.items[i < n0 ? first0 + i : first1 + i - n0];
         const int rows = it.nt * G;
+        if (CODED && rows <= kNarrow) continue;
         const int r = wave * 32 + col;
         const bool valid = r < rows;
         const int rt = (int)((uint32_t)r * inv_g >> 16), token = it.t0 + rt, head = it.head * G + r - rt * G;
@@ -650,20 +914,7 @@ __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a, int64_t firs
     const int G = a.batch.heads / a.batch.kv_heads;
     const int64_t first = (int64_t)(head / G) * a.plan.head->rows + head % G;
     const bool work = there && !pt.direct;
-    float m = -INFINITY, l = 0;
-    vec<float, 4> o = vec<float, 4>{};
-    auto join = [&](float m1, float l1, vec<float, 4> o1) {
-        if (m1 == -INFINITY && l1 == 0) return;        // nothing seen
-        if (m == -INFINITY && l == 0) {                // nothing so far
-            m = m1; l = l1; o = o1;
-            return;
-        }
-        // (a sum of NaN with a maximum of -infinity, of scores that are all NaN, stays NaN times 0)
-        const float m2 = fmaxf(m, m1), f = exp2_fast(m - m2), g = exp2_fast(m1 - m2);
-        o = o * f + o1 * g;
-        l = l * f + l1 * g;
-        m = m2;
-    };
+    RowPart sum{-INFINITY, 0, vec<float, 4>{}};
     if (work) {
         const int splits = pt.own_splits + pt.pre_splits;
         auto row_of = [&](int s) {
@@ -682,18 +933,18 @@ __global__ __launch_bounds__(256) void k_attend_merge(AttendArgs a, int64_t firs
                 x[e] = *(const vec<float, 4> *)(a.part_o + row * D + d * 4);
             }
 #pragma unroll
-            for (int e = 0; e < AHEAD; ++e) join(ml[e].x, ml[e].y, x[e]);
+            for (int e = 0; e < AHEAD; ++e) join(sum, ml[e].x, ml[e].y, x[e]);
         }
     }
     if (LANES > 1) {
-        if (d == 0) { lm[sub][lane] = m; ll[sub][lane] = l; }
-        lo[sub * LANES + lane][d] = o;
+        if (d == 0) { lm[sub][lane] = sum.m; ll[sub][lane] = sum.l; }
+        lo[sub * LANES + lane][d] = sum.o;
         __syncthreads();
         if (lane != 0) return;
-        for (int s = 1; s < LANES; ++s) join(lm[sub][s], ll[sub][s], lo[sub * LANES + s][d]);
+        for (int s = 1; s < LANES; ++s) join(sum, lm[sub][s], ll[sub][s], lo[sub * LANES + s][d]);
     }
-    const float f = one_by(m, l);
-    if (work) *(vec<T, 4> *)out = vec<T, 4>{(T)(o[0] * f), (T)(o[1] * f), (T)(o[2] * f), (T)(o[3] * f)};
+    const float f = one_by(sum.m, sum.l);
+    if (work) *(vec<T, 4> *)out = vec<T, 4>{(T)(sum.o[0] * f), (T)(sum.o[1] * f), (T)(sum.o[2] * f), (T)(sum.o[3] * f)};
 }
 
 template <typename T, int D, bool CODED>
