@@ -809,8 +809,8 @@ int infaas_sel_exec_sample(infaas_sel_exec_t *x, int32_t rows, int32_t vocab, in
  *   d_out_parent   [queries][picks] row of the beam that goes on (a sequence's number, for infaas_sel_exec_advance)
  *   d_out_token    [queries][picks];  d_out_score [queries][picks] (may be d_scores when picks == beams)
  * Where there are fewer continuations than picks, the others are -1, -1 and minus infinity.  Logits of -infinity and NaN are never
- * picked; among logits of +infinity the probabilities are equal, of the others then 0.  Sums and scores are held in 64 bits, and
- * weights are summed exactly: rows with the same logits have the same scores.
+ * picked; among logits of +infinity the probabilities are equal, of the others then 0.  Weights exp(x_j - max) are computed in 32
+ * bits, sums of more than 32 of them and the scores in 64; rows with the same logits have the same scores.
  * queries >= 0, beams and picks 1..64, vocab 1..1,048,576, end_token 0..vocab-1 where d_ended is given.
  * The handle's scratch memory grows as needed, but not while the stream is being captured (infaas_sel_exec_reserve_beam).
  * Errors: INVALID_ARG, HIP, OOM.

@@ -2,6 +2,7 @@
 #include "exec.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace infaas {
 
@@ -44,41 +45,32 @@ __device__ __forceinline__ uint32_t reached_by(uint32_t key, int n)
     return t;
 }
 
-// Puts the n entries of a list in order: f(place, entry) for each, from the greatest key.
-template <typename F> __device__ __forceinline__ void in_order(const u64 *list, int n, int want, F f)
-{
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-        const u64 mine = list[i];
-        int before = 0;
-        for (int j = 0; j < n; ++j) before += list[j] > mine;
-        if (before < want) f(before, mine);
-    }
-}
-
 struct PartShared {
     u64 list[kList];
     uint32_t listed, bound[kWaves];
     float top[kWaves];
     double sum[kWaves];
-    u64 counts[kWaves][2];
+    int counts[kWaves];
 };
 
 // ---- parts --------------------------------------------------------------------------------------
 
-// A workgroup takes a part of a row: `kThreads * PIECES` pieces of 16 bytes less one, so that wherever the row begins the part
-// lies within as many pieces at addresses that are multiples of 16.  Its logits stay in registers: one read of memory for the
-// maximum, the sum of weights and the best ones.
-// Weights exp(x - maximum) are rounded to multiples of 2^-40, of which 64 bits sum up 2^13 exactly: the sum does not depend on
-// which thread has which logit, and rows with the same logits have the same, wherever they begin.
+// A workgroup takes a part of a row, whose logits stay in registers: one read of memory for the maximum, the sum of weights and
+// the best ones.  A thread's logits go by their numbers, not by addresses (its loads of 16 bytes are aligned to a logit only), so
+// rows with the same logits have the same sum wherever they begin.
 template <typename T, int PIECES> struct Part {
-    static constexpr int E = 16 / sizeof(T), COUNT = E * PIECES, SIZE = kThreads * COUNT - E;
-    static_assert(kThreads * COUNT <= 8192, "");
+    static constexpr int E = 16 / sizeof(T), COUNT = E * PIECES, SIZE = kThreads * COUNT;
+    static_assert(COUNT <= 32, "");
 };
+typedef vec<uint32_t, 4> Piece;
+typedef Piece PieceAt2 __attribute__((aligned(2)));
+typedef Piece PieceAt4 __attribute__((aligned(4)));
 
 template <typename T, int PIECES>
 __global__ __launch_bounds__(kThreads) void k_beam_parts(BeamArgs a)
 {
     typedef Part<T, PIECES> P;
+    typedef std::conditional_t<sizeof(T) == 2, PieceAt2, PieceAt4> Unaligned;
     constexpr int E = P::E;
     __shared__ PartShared sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -87,71 +79,82 @@ __global__ __launch_bounds__(kThreads) void k_beam_parts(BeamArgs a)
         const int row = (int)(g / a.parts), part = (int)(g % a.parts);
         if (!alive(a, row) || ended(a, row)) continue;
         const T *const logits = (const T *)a.logits + row * a.row_stride;
-        const int first = part * P::SIZE, last = min(a.vocab, first + P::SIZE);      // (of the part)
-        const int shift = (int)((uintptr_t)(logits + first) / sizeof(T) % E);
+        const int first = part * P::SIZE;
+        auto index = [&](int i) { return first + (i / E * kThreads + tid) * E + i % E; };
         float x[P::COUNT];
 #pragma unroll
         for (int j = 0; j < PIECES; ++j) {
-            const int i0 = first - shift + (j * kThreads + tid) * E;
             T y[E];
-            uint4 v = uint4{};
-            // (a piece that the part begins or ends in is read whole: its 16 bytes are on one page with a logit's)
-            if (i0 < last) v = *(const uint4 *)(logits + i0);
-            __builtin_memcpy(y, &v, 16);
+            const int i0 = index(j * E);
+            if (i0 + E <= a.vocab) {
+                const Piece v = *(const Unaligned *)(logits + i0);
+                __builtin_memcpy(y, &v, 16);
+            } else {
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float z = (float)y[e];
-                x[j * E + e] = i0 + e >= first && i0 + e < last && z > -INFINITY ? z : -INFINITY;
+                for (int e = 0; e < E; ++e) y[e] = i0 + e < a.vocab ? logits[i0 + e] : (T)-INFINITY;
             }
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[j * E + e] = (float)y[e];
         }
-        auto index = [&](int i) { return first - shift + (i / E * kThreads + tid) * E + i % E; };
 
-        float mine = x[0];
+        float top;
+        double total;
+        uint32_t least;
+        while (true) {
+            float most[P::COUNT];
 #pragma unroll
-        for (int i = 1; i < P::COUNT; ++i) mine = fmaxf(mine, x[i]);
-        float top = mine;
+            for (int i = 0; i < P::COUNT; ++i) most[i] = x[i];
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-        // of a wave alone so many lanes have one at least as great: the part's best are not below any wave's bound
-        const uint32_t bound = reached_by(mine > -INFINITY ? key_of(mine) : 0, a.picks);
-        __syncthreads();
-        if (lane == 0) { sh.top[wave] = top; sh.bound[wave] = bound; }
-        if (tid == 0) sh.listed = 0;
-        __syncthreads();
-        top = fmaxf(fmaxf(sh.top[0], sh.top[1]), fmaxf(sh.top[2], sh.top[3]));
-        const uint32_t least = max(max(max(sh.bound[0], sh.bound[1]), max(sh.bound[2], sh.bound[3])), kNever + 1);
-
-        double sum = 0;
-        if (top < INFINITY) {
-            constexpr float whole = 1.5f / (1 << 17);      // adding it rounds to multiples of 2^-40, or to a float's own bits
+            for (int n = P::COUNT / 2; n; n /= 2)
+#pragma unroll
+                for (int i = 0; i < n; ++i) most[i] = fmaxf(most[i], most[i + n]);
+            const float mine = most[0];
+            top = mine;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+            // of a wave alone so many lanes have one at least as great: the part's best are not below any wave's bound
+            const uint32_t bound = reached_by(mine > -INFINITY ? key_of(mine) : 0, a.picks);
+            __syncthreads();
+            if (lane == 0) { sh.top[wave] = top; sh.bound[wave] = bound; }
+            if (tid == 0) sh.listed = 0;
+            __syncthreads();
+            top = fmaxf(fmaxf(sh.top[0], sh.top[1]), fmaxf(sh.top[2], sh.top[3]));
+            least = max(max(max(sh.bound[0], sh.bound[1]), max(sh.bound[2], sh.bound[3])), kNever + 1);
+            // Weights in 32 bits, a thread's added in a tree (five roundings at the most), the threads' sums in 64.
+            float w[P::COUNT];
             const float off = top > -INFINITY ? top : 0.0f;
 #pragma unroll
-            for (int i = 0; i < P::COUNT; ++i) {
-                const float w = __builtin_amdgcn_exp2f((x[i] - off) * 1.44269504088896f);
-                sum += (double)((w + whole) - whole);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < P::COUNT; ++i) sum += x[i] == INFINITY ? 1.0 : 0.0;
-        }
-        for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-
-        int above = 0;
-#pragma unroll
-        for (int i = 0; i < P::COUNT; ++i) above += key_of(x[i]) >= least;
-        for (int d = 1; d < 64; d <<= 1) above += __shfl_xor(above, d);
-        if (lane == 0) { sh.sum[wave] = sum; sh.counts[wave][0] = above; }
-        __syncthreads();
-        const u64 total = sh.counts[0][0] + sh.counts[1][0] + sh.counts[2][0] + sh.counts[3][0];
-        auto put = [&](int i) {
-            const uint32_t at = atomicAdd(&sh.listed, 1u);
-            if (at < kList) sh.list[at] = (u64)key_of(x[i]) << 32 | (uint32_t)~index(i);
-        };
-        if (total <= kList) {
-#pragma unroll
             for (int i = 0; i < P::COUNT; ++i)
-                if (key_of(x[i]) >= least) put(i);
-        } else {
+                w[i] = top < INFINITY ? __builtin_amdgcn_exp2f((x[i] - off) * 1.44269504088896f) : x[i] == top ? 1.0f : 0.0f;
+#pragma unroll
+            for (int n = P::COUNT / 2; n; n /= 2)
+#pragma unroll
+                for (int i = 0; i < n; ++i) w[i] += w[i + n];
+            double sum = mine == mine ? w[0] : NAN;
+            for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+            if (lane == 0) sh.sum[wave] = sum;
+            __syncthreads();
+            total = sh.sum[0] + sh.sum[1] + sh.sum[2] + sh.sum[3];
+            if (total == total) break;
+            // There are logits that are no numbers: they are taken out, once.
+#pragma unroll
+            for (int i = 0; i < P::COUNT; ++i) x[i] = x[i] > -INFINITY ? x[i] : -INFINITY;
+        }
+
+        auto put = [&](float z, int i) {
+            const uint32_t at = atomicAdd(&sh.listed, 1u);
+            if (at < kList) sh.list[at] = (u64)key_of(z) << 32 | (uint32_t)~index(i);
+        };
+        const float from = value_of(least);
+        uint32_t mask = 0;
+#pragma unroll
+        for (int i = P::COUNT - 1; i >= 0; --i) mask = mask << 1 | (x[i] >= from);
+        for (; mask; mask &= mask - 1) {      // (read again: a register has no number)
+            const int i = __builtin_ctz(mask);
+            put((float)logits[index(i)], i);
+        }
+        __syncthreads();
+        if (sh.listed > kList) {
             // Too many reach the bound (equal ones, mostly): the value of the last that is wanted, bit by bit over all threads, and of
             // those with that value the ones with the lowest numbers.
             uint32_t t = 0;
@@ -162,14 +165,14 @@ __global__ __launch_bounds__(kThreads) void k_beam_parts(BeamArgs a)
                 for (int i = 0; i < P::COUNT; ++i) n += key_of(x[i]) >= next;
                 for (int d = 1; d < 64; d <<= 1) n += __shfl_xor(n, d);
                 __syncthreads();
-                if (lane == 0) sh.counts[wave][0] = n;
+                if (lane == 0) sh.counts[wave] = n;
+                if (tid == 0) sh.listed = 0;
                 __syncthreads();
-                if (sh.counts[0][0] + sh.counts[1][0] + sh.counts[2][0] + sh.counts[3][0] >= (u64)a.picks) t = next;
+                if (sh.counts[0] + sh.counts[1] + sh.counts[2] + sh.counts[3] >= a.picks) t = next;
             }
-            int mine_at = 0;      // of the pieces of one number, the threads in order
-            uint32_t taken = 0;
+            int taken = 0;      // of the pieces of one number, the threads in order
             for (int j = 0; j < PIECES; ++j) {
-                mine_at = 0;
+                int mine_at = 0;
 #pragma unroll
                 for (int i = 0; i < P::COUNT; ++i) mine_at += i / E == j && key_of(x[i]) == t;
                 int inc = mine_at;
@@ -178,57 +181,69 @@ __global__ __launch_bounds__(kThreads) void k_beam_parts(BeamArgs a)
                     if (lane >= d) inc += o;
                 }
                 __syncthreads();
-                if (lane == 63) sh.counts[wave][0] = inc;
+                if (lane == 63) sh.counts[wave] = inc;
                 __syncthreads();
-                uint32_t at = taken + inc - mine_at;
+                int at = taken + inc - mine_at;
                 for (int w = 0; w < kWaves; ++w) {
-                    if (w < wave) at += (uint32_t)sh.counts[w][0];
-                    taken += (uint32_t)sh.counts[w][0];
+                    if (w < wave) at += sh.counts[w];
+                    taken += sh.counts[w];
                 }
 #pragma unroll
                 for (int i = 0; i < P::COUNT; ++i) {
                     if (i / E != j) continue;
-                    if (key_of(x[i]) > t) put(i);
-                    else if (key_of(x[i]) == t && at++ < (uint32_t)a.picks) put(i);
+                    if (key_of(x[i]) > t) put(x[i], i);
+                    else if (key_of(x[i]) == t && at++ < a.picks) put(x[i], i);
                 }
             }
+            __syncthreads();
         }
-        __syncthreads();
-        const int n = min((int)sh.listed, kList);
+        const int n = (int)sh.listed;
         u64 *const out = a.best + g * a.picks;
-        in_order(sh.list, n, a.picks, [&](int place, u64 entry) { out[place] = entry; });
+        for (int i = tid; i < n; i += kThreads) {      // in order: an entry's place is the number of greater ones
+            const u64 entry = sh.list[i];
+            int before = 0;
+            for (int j = 0; j < n; ++j) before += sh.list[j] > entry;
+            if (before < a.picks) out[before] = entry;
+        }
         for (int i = n + tid; i < a.picks; i += kThreads) out[i] = 0;
         if (tid == 0) {
             a.top[g] = top;
-            a.sum[g] = sh.sum[0] + sh.sum[1] + sh.sum[2] + sh.sum[3];
+            a.sum[g] = total;
         }
     }
 }
 
 // ---- queries ------------------------------------------------------------------------------------
 
-struct Candidate { double rank; u64 number; };      // number: beam * 2^32 + token
+constexpr int kQueryThreads = 1024, kQueryWaves = kQueryThreads / 64;
+constexpr int kHeld = 4;             // entries that a thread holds
 
 struct QueryShared {
     double rank[kList];
-    u64 number[kList];
+    u64 number[kList];       // beam * 2^32 + token
     // of every beam: what its greatest logit scores (NaN: its parts have no candidates), what it scores itself (NaN: it has not
     // ended), its factor, its greatest logit
     double shift[kMostBeams], score[kMostBeams], factor[kMostBeams];
     float top[kMostBeams];
-    uint32_t listed, bound[kWaves];
-    u64 wave_rank[kWaves], wave_number[kWaves];
+    uint32_t listed, bound[kQueryWaves];
+    u64 wave_rank[kQueryWaves], wave_number[kQueryWaves];
 };
 
-// A workgroup takes a query: the sums of its rows' parts, and of all parts' best the best.
-__global__ __launch_bounds__(kThreads) void k_beam_queries(BeamArgs a)
+// A workgroup takes a query: the sums of its rows' parts, and of all parts' best the best.  A row to a wave, some entries to a
+// thread, which come while the sums are computed.  (With 256 threads, and entries looked up again in every pass, 24 queries of 8
+// beams of 13 parts took 25 us.)
+__global__ __launch_bounds__(kQueryThreads) void k_beam_queries(BeamArgs a)
 {
     __shared__ QueryShared sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t per_row = (int64_t)a.parts * a.picks, entries = per_row * a.beams + a.beams;
+    const int64_t per_row = (int64_t)a.parts * a.picks, listed = per_row * a.beams;
     for (int q = blockIdx.x; q < a.queries; q += gridDim.x) {
+        const u64 *const best = a.best + q * listed;
+        u64 held[kHeld];
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u) held[u] = tid + u * kQueryThreads < listed ? best[tid + u * kQueryThreads] : 0;
         __syncthreads();
-        for (int w = wave; w < a.beams; w += kWaves) {
+        for (int w = wave; w < a.beams; w += kQueryWaves) {
             const int row = q * a.beams + w;
             double shift = NAN, score = NAN, factor = 1.0;
             float top = -INFINITY;
@@ -253,55 +268,54 @@ __global__ __launch_bounds__(kThreads) void k_beam_queries(BeamArgs a)
         }
         if (tid == 0) sh.listed = 0;
         __syncthreads();
-        // candidate i: of the parts' lists, then of the beams that have ended; false: there is none
-        auto candidate = [&](int64_t i, Candidate &c, double &score) {
-            if (i < entries - a.beams) {
-                const int w = (int)(i / per_row);
-                const u64 e = a.best[(int64_t)q * a.beams * per_row + i];
-                const double shift = sh.shift[w];
-                if (!(shift == shift) || e == 0) return false;
-                const float x = value_of((uint32_t)(e >> 32)), top = sh.top[w];
-                if (top == INFINITY && x < top) return false;
-                score = x == top ? shift : shift + ((double)x - (double)top);
-                c.rank = score * sh.factor[w];
-                c.number = (u64)w << 32 | (uint32_t)~e;
-                return true;
-            }
-            const int w = (int)(i - (entries - a.beams));      // (the arrays are not looked at again: the result may be one of them)
-            score = sh.score[w];
-            if (!(score == score)) return false;
-            c.rank = score * sh.factor[w];
-            c.number = (u64)w << 32 | (uint32_t)a.end_token;
+        // rank and number of an entry of the parts' lists, if it is a candidate
+        auto from_list = [&](int64_t i, u64 e, double &rank, u64 &number) {
+            if (e == 0) return false;
+            const int w = (int)(i / per_row);
+            const double shift = sh.shift[w];
+            const float x = value_of((uint32_t)(e >> 32)), top = sh.top[w];
+            if (!(shift == shift) || (top == INFINITY && x < top)) return false;
+            rank = (x == top ? shift : shift + ((double)x - (double)top)) * sh.factor[w];
+            number = (u64)w << 32 | (uint32_t)~e;
             return true;
         };
+        // f(rank, number) of all candidates: the held ones, those beyond them, the beams that have ended
+        auto each = [&](auto f) {
+            double rank;
+            u64 number;
+#pragma unroll
+            for (int u = 0; u < kHeld; ++u)
+                if (from_list(tid + u * kQueryThreads, held[u], rank, number)) f(rank, number);
+            for (int64_t i = tid + kHeld * kQueryThreads; i < listed; i += kQueryThreads)
+                if (from_list(i, best[i], rank, number)) f(rank, number);
+            if (tid < a.beams) {      // (the arrays are not looked at again: the result may be one of them)
+                const double score = sh.score[tid];
+                if (score == score) f(score * sh.factor[tid], (u64)tid << 32 | (uint32_t)a.end_token);
+            }
+        };
         uint32_t mine = 0;
-        for (int64_t i = tid; i < entries; i += kThreads) {
-            Candidate c;
-            double s;
-            if (candidate(i, c, s)) mine = max(mine, (uint32_t)(key_of(c.rank) >> 32));
-        }
+        each([&](double rank, u64) { mine = max(mine, (uint32_t)(key_of(rank) >> 32)); });
         const uint32_t bound = reached_by(mine, a.picks);
         if (lane == 0) sh.bound[wave] = bound;
         __syncthreads();
-        const uint32_t least = max(max(sh.bound[0], sh.bound[1]), max(sh.bound[2], sh.bound[3]));
-        for (int64_t i = tid; i < entries; i += kThreads) {
-            Candidate c;
-            double s;
-            if (!candidate(i, c, s) || (uint32_t)(key_of(c.rank) >> 32) < least) continue;
+        uint32_t least = 0;
+        for (int w = 0; w < kQueryWaves; ++w) least = max(least, sh.bound[w]);
+        each([&](double rank, u64 number) {
+            if ((uint32_t)(key_of(rank) >> 32) < least) return;
             const uint32_t at = atomicAdd(&sh.listed, 1u);
-            if (at < kList) { sh.rank[at] = c.rank; sh.number[at] = c.number; }
-        }
+            if (at < kList) { sh.rank[at] = rank; sh.number[at] = number; }
+        });
         __syncthreads();
         const int64_t out = (int64_t)q * a.picks;
         auto write = [&](int place, double rank, u64 number) {
-            const int w = (int)(number >> 32), row = q * a.beams + w;
-            a.out_parent[out + place] = row;
+            const int w = (int)(number >> 32);
+            a.out_parent[out + place] = q * a.beams + w;
             a.out_token[out + place] = (int)(uint32_t)number;
             a.out_score[out + place] = a.factor ? (float)(rank / sh.factor[w]) : (float)rank;
         };
         int found = (int)sh.listed;
         if (found <= kList) {
-            for (int i = tid; i < found; i += kThreads) {
+            for (int i = tid; i < found; i += kQueryThreads) {
                 const double rank = sh.rank[i];
                 const u64 number = sh.number[i];
                 int before = 0;
@@ -310,71 +324,72 @@ __global__ __launch_bounds__(kThreads) void k_beam_queries(BeamArgs a)
             }
         } else {
             // More than the list holds share the bound: one after the other, each the first behind the one before it.
-            double rank = INFINITY;
-            u64 number = 0;
-            found = 0;
-            for (; found < a.picks; ++found) {
-                u64 best = 0, which = ~0ull;
-                for (int64_t i = tid; i < entries; i += kThreads) {
-                    Candidate c;
-                    double s;
-                    if (!candidate(i, c, s) || !(c.rank < rank || (c.rank == rank && found > 0 && c.number > number))) continue;
-                    const u64 k = key_of(c.rank);
-                    if (k > best || (k == best && c.number < which)) { best = k; which = c.number; }
-                }
+            double last = INFINITY;
+            u64 last_number = 0;
+            for (found = 0; found < a.picks; ++found) {
+                u64 most = 0, which = ~0ull;
+                each([&](double rank, u64 number) {
+                    if (!(rank < last || (rank == last && found > 0 && number > last_number))) return;
+                    const u64 k = key_of(rank);
+                    if (k > most || (k == most && number < which)) { most = k; which = number; }
+                });
                 for (int d = 1; d < 64; d <<= 1) {
-                    const u64 k = __shfl_xor(best, d), n = __shfl_xor(which, d);
-                    if (k > best || (k == best && n < which)) { best = k; which = n; }
+                    const u64 k = __shfl_xor(most, d), n = __shfl_xor(which, d);
+                    if (k > most || (k == most && n < which)) { most = k; which = n; }
                 }
                 __syncthreads();
-                if (lane == 0) { sh.wave_rank[wave] = best; sh.wave_number[wave] = which; }
+                if (lane == 0) { sh.wave_rank[wave] = most; sh.wave_number[wave] = which; }
                 __syncthreads();
-                best = 0, which = ~0ull;
-                for (int w = 0; w < kWaves; ++w)
-                    if (sh.wave_rank[w] > best || (sh.wave_rank[w] == best && sh.wave_number[w] < which)) { best = sh.wave_rank[w]; which = sh.wave_number[w]; }
-                if (best == 0) break;
-                rank = __longlong_as_double(best >> 63 ? best & ~(1ull << 63) : ~best);
-                number = which;
-                if (tid == 0) write(found, rank, number);
+                most = 0, which = ~0ull;
+                for (int w = 0; w < kQueryWaves; ++w)
+                    if (sh.wave_rank[w] > most || (sh.wave_rank[w] == most && sh.wave_number[w] < which)) { most = sh.wave_rank[w]; which = sh.wave_number[w]; }
+                if (most == 0) break;
+                last = __longlong_as_double(most >> 63 ? most & ~(1ull << 63) : ~most);
+                last_number = which;
+                if (tid == 0) write(found, last, last_number);
             }
         }
-        for (int i = found + tid; i < a.picks; i += kThreads) {
+        for (int i = found + tid; i < a.picks; i += kQueryThreads) {
             a.out_parent[out + i] = a.out_token[out + i] = -1;
             a.out_score[out + i] = -INFINITY;
         }
     }
 }
 
-template <typename T, int PIECES> hipError_t beam(BeamArgs a, hipStream_t s)
+template <typename T, int PIECES> hipError_t beam(const BeamArgs &a, hipStream_t s)
 {
     const int64_t groups = (int64_t)a.queries * a.beams * a.parts;
     k_beam_parts<T, PIECES><<<(unsigned)std::min<int64_t>(groups, 1 << 20), kThreads, 0, s>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
-    k_beam_queries<<<std::min(a.queries, 1 << 16), kThreads, 0, s>>>(a);
+    k_beam_queries<<<std::min(a.queries, 1 << 16), kQueryThreads, 0, s>>>(a);
     return hipGetLastError();
 }
 
-template <typename T> int64_t parts_of(int32_t vocab) { return (vocab + Part<T, 8192 / kThreads / (16 / sizeof(T))>::SIZE - 1) / Part<T, 8192 / kThreads / (16 / sizeof(T))>::SIZE; }
+// Logits of a part: 8192, or 2048 where those would make too few workgroups.
+constexpr int kLarge = 8192, kSmall = 2048, kFewParts = 512;
 
 }  // namespace
 
-BeamSizes beam_sizes(int32_t queries, int32_t beams, int32_t vocab, int32_t picks, int32_t type)
+BeamSizes beam_sizes(int32_t queries, int32_t beams, int32_t vocab, int32_t picks)
 {
     BeamSizes z{};
-    z.parts = type == INFAAS_SEL_TYPE_FP32 ? parts_of<float>(vocab) : parts_of<bf16_t>(vocab);
-    const int64_t groups = (int64_t)queries * beams * z.parts;
+    const int64_t rows = (int64_t)queries * beams;
+    z.size = rows * ((vocab + kLarge - 1) / kLarge) < kFewParts ? kSmall : kLarge;
+    z.parts = (vocab + z.size - 1) / z.size;
+    const int64_t groups = rows * z.parts;
     z.sum_at = groups * picks * (int64_t)sizeof(u64);
     z.top_at = z.sum_at + groups * (int64_t)sizeof(double);
     z.bytes = z.top_at + groups * (int64_t)sizeof(float);
     return z;
 }
 
-hipError_t launch_beam(const BeamArgs &a, int32_t type, hipStream_t s)
+hipError_t launch_beam(const BeamArgs &a, int32_t size, int32_t type, hipStream_t s)
 {
+    const bool small = size == kSmall;
     switch (type) {
-    case INFAAS_SEL_TYPE_FP32: return beam<float, 8>(a, s);
-    case INFAAS_SEL_TYPE_BF16: return beam<bf16_t, 4>(a, s);
-    default: return beam<fp16_t, 4>(a, s);
+    case INFAAS_SEL_TYPE_FP32: return small ? beam<float, 2>(a, s) : beam<float, 8>(a, s);
+    case INFAAS_SEL_TYPE_BF16: return small ? beam<bf16_t, 1>(a, s) : beam<bf16_t, 4>(a, s);
+    default: return small ? beam<fp16_t, 1>(a, s) : beam<fp16_t, 4>(a, s);
     }
 }
 

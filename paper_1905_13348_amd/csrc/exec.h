@@ -162,7 +162,7 @@ struct BeamArgs {
     double *sum;
     float *top;
 };
-struct BeamSizes { int64_t parts, sum_at, top_at, bytes; };
+struct BeamSizes { int64_t size, parts, sum_at, top_at, bytes; };      // size: logits of a part
 constexpr int kMostBeams = 64;       // beams, and picks
 
 constexpr int kMostSeqs = 4096;      // of a table
@@ -224,8 +224,8 @@ hipError_t launch_append_scaled(const AppendScaledArgs &a, int32_t type, hipStre
 hipError_t launch_read(const ReadArgs &a, int32_t type, hipStream_t s);
 hipError_t launch_advance(const AdvanceArgs &a, hipStream_t s);
 hipError_t launch_copy(const CopyArgs &a, hipStream_t s);
-BeamSizes beam_sizes(int32_t queries, int32_t beams, int32_t vocab, int32_t picks, int32_t type);
-hipError_t launch_beam(const BeamArgs &a, int32_t type, hipStream_t s);
+BeamSizes beam_sizes(int32_t queries, int32_t beams, int32_t vocab, int32_t picks);
+hipError_t launch_beam(const BeamArgs &a, int32_t size, int32_t type, hipStream_t s);
 hipError_t launch_sample(const SampleArgs &a, int32_t type, hipStream_t s);
 
 }  // namespace infaas

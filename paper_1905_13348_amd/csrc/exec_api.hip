@@ -473,12 +473,12 @@ int infaas_sel_exec_beam(infaas_sel_exec_t *x, int32_t queries, int32_t beams, i
     if ((uintptr_t)d_logits % (type == INFAAS_SEL_TYPE_FP32 ? 4 : 2)) return refuse("beam: logits are not aligned to their type");
     OnDevice on(x->device);
     if (on.err != hipSuccess) return hip_failed(on.err, "hipSetDevice");
-    const BeamSizes z = beam_sizes(queries, beams, vocab, picks, type);
+    const BeamSizes z = beam_sizes(queries, beams, vocab, picks);
     if (int rc = ensure(x, z.bytes, (hipStream_t)hip_stream, true, "infaas_sel_exec_reserve_beam")) return rc;
     char *const p = (char *)x->scratch;
     const BeamArgs a{d_logits, row_stride, queries, beams, vocab, picks, end_token, (int32_t)z.parts, d_scores, d_factor, d_ended,
                      d_out_parent, d_out_token, d_out_score, (unsigned long long *)p, (double *)(p + z.sum_at), (float *)(p + z.top_at)};
-    if (hipError_t e = launch_beam(a, type, (hipStream_t)hip_stream)) return hip_failed(e, "infaas_sel_exec_beam");
+    if (hipError_t e = launch_beam(a, (int32_t)z.size, type, (hipStream_t)hip_stream)) return hip_failed(e, "infaas_sel_exec_beam");
     return INFAAS_SEL_OK;
 }
 
@@ -488,7 +488,7 @@ int infaas_sel_exec_reserve_beam(infaas_sel_exec_t *x, int32_t queries, int32_t 
     if (int rc = check_beam(queries, beams, vocab, picks, type)) return rc;
     OnDevice on(x->device);
     if (on.err != hipSuccess) return hip_failed(on.err, "hipSetDevice");
-    return ensure(x, beam_sizes(queries, beams, vocab, picks, type).bytes, nullptr, false);
+    return ensure(x, beam_sizes(queries, beams, vocab, picks).bytes, nullptr, false);
 }
 
 }  // extern "C"

@@ -32,8 +32,9 @@ def reference(logits, scores, picks, ended=None, factor=None, end=-1):
             t = np.where(x == np.inf, 0.0, -np.inf) if top == np.inf else x - top
             weight = np.exp(t)
             lse = np.log(weight.sum())
-            # of a weight: two roundings and a constant's of its exponent in 32 bits, and an ulp of the power; then 2^-40 each
-            far = (weight * np.where(weight > 0, np.abs(t), 0) * 2.5 * 2.0 ** -24 + weight * 2.0 ** -22 + 2.0 ** -40).sum() / weight.sum()
+            # of a weight: two roundings and a constant's of its exponent in 32 bits, an ulp of the power (2^-23), and five
+            # roundings of the sums of up to 32 in 32 bits (2^-24 each)
+            far = (weight * np.where(weight > 0, np.abs(t), 0) * 2.5 * 2.0 ** -24 + weight * 7 * 2.0 ** -24).sum() / weight.sum()
             for i in np.argsort(-t, kind="stable")[:picks]:
                 if t[i] > -np.inf:
                     found.append((-(s + t[i] - lse) * f, w, int(i), s + t[i] - lse, far))
