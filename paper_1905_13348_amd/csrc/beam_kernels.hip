@@ -26,6 +26,47 @@ __device__ __forceinline__ u64 key_of(double x)
     return b >> 63 ? ~b : b | 1ull << 63;
 }
 
+// A neighbour's value in the steps of a reduction over a wave: 1, 2, 4 and 8 lanes down within rows of 16, then the last lane of a
+// row into the next one, and of the lower half into the upper; lanes without one get `none`.  The result is in lane 63.  (Six
+// operations; through LDS each step is a trip of a hundred cycles.)
+template <int CTRL, int ROWS> __device__ __forceinline__ int neighbour(int x, int none) { return __builtin_amdgcn_update_dpp(none, x, CTRL, ROWS, 0xf, false); }
+template <typename F> __device__ __forceinline__ void over_wave(F step)
+{
+    step(std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>());
+    step(std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>());
+    step(std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>());
+    step(std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>());
+    step(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());
+    step(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());
+}
+__device__ __forceinline__ float wave_max(float x)
+{
+    over_wave([&](auto ctrl, auto rows) { x = fmaxf(x, __int_as_float(neighbour<ctrl.value, rows.value>(__float_as_int(x), __float_as_int(-INFINITY)))); });
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+__device__ __forceinline__ double wave_sum(double x)
+{
+    over_wave([&](auto ctrl, auto rows) {
+        x += __hiloint2double(neighbour<ctrl.value, rows.value>(__double2hiint(x), 0), neighbour<ctrl.value, rows.value>(__double2loint(x), 0));
+    });
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(x), 63), __builtin_amdgcn_readlane(__double2loint(x), 63));
+}
+
+// log(x) of a normal positive number: 2^e m with m from 1/sqrt(2) to sqrt(2), log m = 2 artanh z, z = (m - 1) / (m + 1), |z| <= 0.172;
+// behind the term z^17 / 17 the series has 0.172^19 / 19 = 2e-16 left.  (A few lines of code: the library's takes longer to fetch
+// than to run, once a launch.)
+__device__ __forceinline__ double log_of(double x)
+{
+    int e = 0;
+    double m = frexp(x, &e);
+    if (m < 0.70710678118654752) { m *= 2; --e; }
+    const double z = (m - 1) / (m + 1), zz = z * z;
+    double p = 1.0 / 17;
+#pragma unroll
+    for (int n = 15; n >= 1; n -= 2) p = __builtin_fma(p, zz, 1.0 / n);
+    return __builtin_fma((double)e, 0.69314718055994531, 2 * z * p);
+}
+
 // What a beam has to continue with.  Dead ones (scores that are not finite, factors that are not positive) have nothing.
 __device__ __forceinline__ bool alive(const BeamArgs &a, int row)
 {
@@ -45,9 +86,11 @@ __device__ __forceinline__ uint32_t reached_by(uint32_t key, int n)
     return t;
 }
 
+constexpr int kWaveList = kList / kWaves;
+
 struct PartShared {
     u64 list[kList];
-    uint32_t listed, bound[kWaves];
+    uint32_t bound[kWaves];
     float top[kWaves];
     double sum[kWaves];
     int counts[kWaves];
@@ -97,42 +140,48 @@ __global__ __launch_bounds__(kThreads) void k_beam_parts(BeamArgs a)
             for (int e = 0; e < E; ++e) x[j * E + e] = (float)y[e];
         }
 
-        float top;
+        float top, most[PIECES];
         double total;
         uint32_t least;
         while (true) {
-            float most[P::COUNT];
+            float mine = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < P::COUNT; ++i) most[i] = x[i];
+            for (int j = 0; j < PIECES; ++j) {
+                most[j] = x[j * E];
 #pragma unroll
-            for (int n = P::COUNT / 2; n; n /= 2)
-#pragma unroll
-                for (int i = 0; i < n; ++i) most[i] = fmaxf(most[i], most[i + n]);
-            const float mine = most[0];
-            top = mine;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+                for (int e = 1; e < E; ++e) most[j] = fmaxf(most[j], x[j * E + e]);
+                mine = fmaxf(mine, most[j]);
+            }
+            top = wave_max(mine);
             // of a wave alone so many lanes have one at least as great: the part's best are not below any wave's bound
             const uint32_t bound = reached_by(mine > -INFINITY ? key_of(mine) : 0, a.picks);
             __syncthreads();
             if (lane == 0) { sh.top[wave] = top; sh.bound[wave] = bound; }
-            if (tid == 0) sh.listed = 0;
             __syncthreads();
             top = fmaxf(fmaxf(sh.top[0], sh.top[1]), fmaxf(sh.top[2], sh.top[3]));
             least = max(max(max(sh.bound[0], sh.bound[1]), max(sh.bound[2], sh.bound[3])), kNever + 1);
-            // Weights in 32 bits, a thread's added in a tree (five roundings at the most), the threads' sums in 64.
-            float w[P::COUNT];
+            // Weights in 32 bits, a thread's up to 32 added there by pieces (ten roundings at the most), the threads' in 64.
             const float off = top > -INFINITY ? top : 0.0f;
+            float sum = 0;
 #pragma unroll
-            for (int i = 0; i < P::COUNT; ++i)
-                w[i] = top < INFINITY ? __builtin_amdgcn_exp2f((x[i] - off) * 1.44269504088896f) : x[i] == top ? 1.0f : 0.0f;
+            for (int j = 0; j < PIECES; ++j) {
+                float w[E];
 #pragma unroll
-            for (int n = P::COUNT / 2; n; n /= 2)
+                for (int e = 0; e < E; ++e)
+                    w[e] = __builtin_amdgcn_exp2f((x[j * E + e] - off) * 1.44269504088896f);
 #pragma unroll
-                for (int i = 0; i < n; ++i) w[i] += w[i + n];
-            double sum = mine == mine ? w[0] : NAN;
-            for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-            if (lane == 0) sh.sum[wave] = sum;
+                for (int n = E / 2; n; n /= 2)
+#pragma unroll
+                    for (int e = 0; e < n; ++e) w[e] += w[e + n];
+                sum += w[0];
+            }
+            if (top == INFINITY) {      // (then the exponents were none)
+                sum = 0;
+#pragma unroll
+                for (int i = 0; i < P::COUNT; ++i) sum += x[i] == top ? 1.0f : 0.0f;
+            }
+            const double wave_total = wave_sum(mine == mine ? sum : NAN);
+            if (lane == 0) sh.sum[wave] = wave_total;
             __syncthreads();
             total = sh.sum[0] + sh.sum[1] + sh.sum[2] + sh.sum[3];
             if (total == total) break;
@@ -141,20 +190,25 @@ __global__ __launch_bounds__(kThreads) void k_beam_parts(BeamArgs a)
             for (int i = 0; i < P::COUNT; ++i) x[i] = x[i] > -INFINITY ? x[i] : -INFINITY;
         }
 
-        auto put = [&](float z, int i) {
-            const uint32_t at = atomicAdd(&sh.listed, 1u);
-            if (at < kList) sh.list[at] = (u64)key_of(z) << 32 | (uint32_t)~index(i);
-        };
+        // Each wave lists what reaches the bound.
         const float from = value_of(least);
-        uint32_t mask = 0;
+        int mine_listed = 0;
+        auto put = [&](bool is, float z, int i) {
+            const u64 who = __ballot(is);
+            if (!who) return;
+            const int at = mine_listed + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+            if (is && at < kWaveList) sh.list[wave * kWaveList + at] = (u64)key_of(z) << 32 | (uint32_t)~index(i);
+            mine_listed += (int)__popcll(who);
+        };
 #pragma unroll
-        for (int i = P::COUNT - 1; i >= 0; --i) mask = mask << 1 | (x[i] >= from);
-        for (; mask; mask &= mask - 1) {      // (read again: a register has no number)
-            const int i = __builtin_ctz(mask);
-            put((float)logits[index(i)], i);
+        for (int j = 0; j < PIECES; ++j) {
+            if (!__any(most[j] >= from)) continue;
+#pragma unroll
+            for (int e = 0; e < E; ++e) put(x[j * E + e] >= from, x[j * E + e], j * E + e);
         }
+        if (lane == 0) sh.counts[wave] = mine_listed;
         __syncthreads();
-        if (sh.listed > kList) {
+        if (max(max(sh.counts[0], sh.counts[1]), max(sh.counts[2], sh.counts[3])) > kWaveList) {
             // Too many reach the bound (equal ones, mostly): the value of the last that is wanted, bit by bit over all threads, and of
             // those with that value the ones with the lowest numbers.
             uint32_t t = 0;
@@ -166,10 +220,10 @@ __global__ __launch_bounds__(kThreads) void k_beam_parts(BeamArgs a)
                 for (int d = 1; d < 64; d <<= 1) n += __shfl_xor(n, d);
                 __syncthreads();
                 if (lane == 0) sh.counts[wave] = n;
-                if (tid == 0) sh.listed = 0;
                 __syncthreads();
                 if (sh.counts[0] + sh.counts[1] + sh.counts[2] + sh.counts[3] >= a.picks) t = next;
             }
+            mine_listed = 0;
             int taken = 0;      // of the pieces of one number, the threads in order
             for (int j = 0; j < PIECES; ++j) {
                 int mine_at = 0;
@@ -189,23 +243,31 @@ __global__ __launch_bounds__(kThreads) void k_beam_parts(BeamArgs a)
                     taken += sh.counts[w];
                 }
 #pragma unroll
-                for (int i = 0; i < P::COUNT; ++i) {
-                    if (i / E != j) continue;
-                    if (key_of(x[i]) > t) put(x[i], i);
-                    else if (key_of(x[i]) == t && at++ < a.picks) put(x[i], i);
-                }
+                for (int i = 0; i < P::COUNT; ++i)
+                    if (i / E == j) put(key_of(x[i]) > t || (key_of(x[i]) == t && at++ < a.picks), x[i], i);
             }
             __syncthreads();
+            if (lane == 0) sh.counts[wave] = mine_listed;
+            __syncthreads();
         }
-        const int n = (int)sh.listed;
-        u64 *const out = a.best + g * a.picks;
-        for (int i = tid; i < n; i += kThreads) {      // in order: an entry's place is the number of greater ones
-            const u64 entry = sh.list[i];
+        // In order: an entry's place is the number of greater ones.  (First all of a query's parts' firsts, then their seconds.)  Four threads to an entry, one for each wave's list.
+        const int ends[kWaves] = {sh.counts[0], sh.counts[0] + sh.counts[1], sh.counts[0] + sh.counts[1] + sh.counts[2],
+                                  sh.counts[0] + sh.counts[1] + sh.counts[2] + sh.counts[3]};
+        const int n = ends[kWaves - 1], lists = a.beams * a.parts;
+        u64 *const best = a.best + g / lists * lists * a.picks + g % lists;
+        for (int i0 = 0; i0 < n; i0 += kThreads / kWaves) {
+            const int i = i0 + tid / kWaves, l = tid % kWaves;
+            const int w = (i >= ends[0]) + (i >= ends[1]) + (i >= ends[2]);
+            const u64 entry = i < n ? sh.list[w * kWaveList + i - (w ? ends[w - 1] : 0)] : ~0ull;
             int before = 0;
-            for (int j = 0; j < n; ++j) before += sh.list[j] > entry;
-            if (before < a.picks) out[before] = entry;
+            const int to = sh.counts[l];
+#pragma unroll 4
+            for (int j = 0; j < to; ++j) before += sh.list[l * kWaveList + j] > entry;
+            before += __shfl_xor(before, 1);
+            before += __shfl_xor(before, 2);
+            if (i < n && l == 0 && before < a.picks) best[(int64_t)before * lists] = entry;
         }
-        for (int i = n + tid; i < a.picks; i += kThreads) out[i] = 0;
+        for (int i = n + tid; i < a.picks; i += kThreads) best[(int64_t)i * lists] = 0;
         if (tid == 0) {
             a.top[g] = top;
             a.sum[g] = total;
@@ -216,7 +278,6 @@ __global__ __launch_bounds__(kThreads) void k_beam_parts(BeamArgs a)
 // ---- queries ------------------------------------------------------------------------------------
 
 constexpr int kQueryThreads = 1024, kQueryWaves = kQueryThreads / 64;
-constexpr int kHeld = 4;             // entries that a thread holds
 
 struct QueryShared {
     double rank[kList];
@@ -229,49 +290,52 @@ struct QueryShared {
     u64 wave_rank[kQueryWaves], wave_number[kQueryWaves];
 };
 
-// A workgroup takes a query: the sums of its rows' parts, and of all parts' best the best.  A row to a wave, some entries to a
-// thread, which come while the sums are computed.  (With 256 threads, and entries looked up again in every pass, 24 queries of 8
+// A workgroup takes a query: the sums of its rows' parts, and of all parts' best the best.  A row to a wave, an entry to a
+// thread, which comes while the sums are computed.  (With 256 threads, and entries looked up again in every pass, 24 queries of 8
 // beams of 13 parts took 25 us.)
 __global__ __launch_bounds__(kQueryThreads) void k_beam_queries(BeamArgs a)
 {
     __shared__ QueryShared sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t per_row = (int64_t)a.parts * a.picks, listed = per_row * a.beams;
+    const int lists = a.beams * a.parts;
+    const int64_t listed = (int64_t)lists * a.picks;
     for (int q = blockIdx.x; q < a.queries; q += gridDim.x) {
         const u64 *const best = a.best + q * listed;
-        u64 held[kHeld];
-#pragma unroll
-        for (int u = 0; u < kHeld; ++u) held[u] = tid + u * kQueryThreads < listed ? best[tid + u * kQueryThreads] : 0;
+        const u64 held = tid < listed ? best[tid] : 0;
         __syncthreads();
         for (int w = wave; w < a.beams; w += kQueryWaves) {
             const int row = q * a.beams + w;
-            double shift = NAN, score = NAN, factor = 1.0;
-            float top = -INFINITY;
-            if (alive(a, row)) {
-                if (a.factor) factor = a.factor[row];
-                if (ended(a, row)) {
-                    score = a.scores[row];
-                } else {
-                    for (int p = lane; p < a.parts; p += 64) top = fmaxf(top, a.top[(int64_t)row * a.parts + p]);
-                    for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-                    double sum = 0;
-                    for (int p = lane; p < a.parts; p += 64) {
-                        const float t = a.top[(int64_t)row * a.parts + p];
-                        const double s = a.sum[(int64_t)row * a.parts + p];
-                        sum += t == top ? s : t > -INFINITY && top < INFINITY ? s * exp((double)t - (double)top) : 0.0;
-                    }
-                    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-                    if (top > -INFINITY) shift = (double)a.scores[row] - log(sum);
-                }
+            const float *const tops = a.top + (int64_t)row * a.parts;
+            const double *const sums = a.sum + (int64_t)row * a.parts;
+            // (everything that may be needed is under way at once)
+            const float t0 = lane < a.parts ? tops[lane] : -INFINITY;
+            const double s0 = lane < a.parts ? sums[lane] : 0.0;
+            const double own = a.scores[row], factor = a.factor ? a.factor[row] : 1.0;
+            const bool is_alive = alive(a, row), is_ended = ended(a, row);
+            double shift = NAN;
+            float top = t0;
+            for (int p = lane + 64; p < a.parts; p += 64) top = fmaxf(top, tops[p]);
+            top = wave_max(top);
+            auto weight = [&](float t) {
+                return t == top ? 1.0 : t > -INFINITY && top < INFINITY ? (double)__builtin_amdgcn_exp2f((t - top) * 1.44269504088896f) : 0.0;
+            };
+            double sum = weight(t0) * s0;
+            for (int p = lane + 64; p < a.parts; p += 64) sum += weight(tops[p]) * sums[p];
+            sum = wave_sum(sum);
+            if (is_alive && !is_ended && top > -INFINITY) shift = own - log_of(sum);
+            if (lane == 0) {
+                sh.shift[w] = shift;
+                sh.score[w] = is_alive && is_ended ? own : NAN;
+                sh.factor[w] = factor;
+                sh.top[w] = top;
             }
-            if (lane == 0) { sh.shift[w] = shift; sh.score[w] = score; sh.factor[w] = factor; sh.top[w] = top; }
         }
         if (tid == 0) sh.listed = 0;
         __syncthreads();
         // rank and number of an entry of the parts' lists, if it is a candidate
         auto from_list = [&](int64_t i, u64 e, double &rank, u64 &number) {
             if (e == 0) return false;
-            const int w = (int)(i / per_row);
+            const int w = (int)((uint32_t)(i % lists) / (uint32_t)a.parts);
             const double shift = sh.shift[w];
             const float x = value_of((uint32_t)(e >> 32)), top = sh.top[w];
             if (!(shift == shift) || (top == INFINITY && x < top)) return false;
@@ -283,11 +347,12 @@ __global__ __launch_bounds__(kQueryThreads) void k_beam_queries(BeamArgs a)
         auto each = [&](auto f) {
             double rank;
             u64 number;
-#pragma unroll
-            for (int u = 0; u < kHeld; ++u)
-                if (from_list(tid + u * kQueryThreads, held[u], rank, number)) f(rank, number);
-            for (int64_t i = tid + kHeld * kQueryThreads; i < listed; i += kQueryThreads)
-                if (from_list(i, best[i], rank, number)) f(rank, number);
+            u64 e = held;
+#pragma unroll 1
+            for (int64_t i = tid; i < listed; i += kQueryThreads) {
+                if (from_list(i, e, rank, number)) f(rank, number);
+                if (i + kQueryThreads < listed) e = best[i + kQueryThreads];
+            }
             if (tid < a.beams) {      // (the arrays are not looked at again: the result may be one of them)
                 const double score = sh.score[tid];
                 if (score == score) f(score * sh.factor[tid], (u64)tid << 32 | (uint32_t)a.end_token);
@@ -319,6 +384,7 @@ __global__ __launch_bounds__(kQueryThreads) void k_beam_queries(BeamArgs a)
                 const double rank = sh.rank[i];
                 const u64 number = sh.number[i];
                 int before = 0;
+#pragma unroll 4
                 for (int j = 0; j < found; ++j) before += sh.rank[j] > rank || (sh.rank[j] == rank && sh.number[j] < number);
                 if (before < a.picks) write(before, rank, number);
             }

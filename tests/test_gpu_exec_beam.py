@@ -32,9 +32,9 @@ def reference(logits, scores, picks, ended=None, factor=None, end=-1):
             t = np.where(x == np.inf, 0.0, -np.inf) if top == np.inf else x - top
             weight = np.exp(t)
             lse = np.log(weight.sum())
-            # of a weight: two roundings and a constant's of its exponent in 32 bits, an ulp of the power (2^-23), and five
-            # roundings of the sums of up to 32 in 32 bits (2^-24 each)
-            far = (weight * np.where(weight > 0, np.abs(t), 0) * 2.5 * 2.0 ** -24 + weight * 7 * 2.0 ** -24).sum() / weight.sum()
+            # of a weight: two roundings and a constant's of its exponent in 32 bits, which is in two parts (of the row's part, and
+            # of that to the row), an ulp of each power (2^-23), and ten roundings of the sums of up to 32 in 32 bits (2^-24 each)
+            far = (weight * np.where(weight > 0, np.abs(t), 0) * 2.5 * 2.0 ** -24 + weight * 14 * 2.0 ** -24).sum() / weight.sum()
             for i in np.argsort(-t, kind="stable")[:picks]:
                 if t[i] > -np.inf:
                     found.append((-(s + t[i] - lse) * f, w, int(i), s + t[i] - lse, far))
