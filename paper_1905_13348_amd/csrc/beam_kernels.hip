@@ -11,6 +11,9 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kList = 2048;          // candidates of a part or a query that are put in order in LDS
 constexpr uint32_t kNever = 0x007fffffu;     // order key of -infinity
+constexpr float kLog2e = 1.44269504088896f;
+// Beyond it a product with log2(e) is rounded by more than 2^-12: the difference is taken first, then.
+constexpr float kNear = 2048.0f;
 typedef unsigned long long u64;
 
 // Logits that are numbers as 32-bit keys in their order: equal logits (-0 and +0, too) have equal keys.
@@ -74,195 +77,225 @@ __device__ __forceinline__ bool alive(const BeamArgs &a, int row)
 }
 __device__ __forceinline__ bool ended(const BeamArgs &a, int row) { return a.ended && a.ended[row] != 0; }
 
-// The greatest value that at least n of a wave's lanes reach, with its lower 16 bits cut off (0: there are not so many).
-__device__ __forceinline__ uint32_t reached_by(uint32_t key, int n)
+// The greatest value that at least n of a wave's lanes reach, with its lower bits cut off (0: there are not so many).
+template <int LOWEST> __device__ __forceinline__ uint32_t reached_by(uint32_t key, int n)
 {
     uint32_t t = 0;
 #pragma unroll
-    for (int bit = 31; bit >= 16; --bit) {
+    for (int bit = 31; bit >= LOWEST; --bit) {
         const uint32_t next = t | 1u << bit;
         if ((int)__popcll(__ballot(key >= next)) >= n) t = next;
     }
     return t;
 }
 
-constexpr int kWaveList = kList / kWaves;
+// A wave's candidates: up to kKept, and those of a piece to each lane behind them.
+constexpr int kKept = 2 * kMostBeams, kWaveList = kKept + 64 * 8;
 
 struct PartShared {
-    u64 list[kList];
+    u64 list[kWaves][kWaveList];
     uint32_t bound[kWaves];
     float top[kWaves];
     double sum[kWaves];
     int counts[kWaves];
 };
 
+// The n entries of a wave's list become the `want` greatest (n is more), in any order; the least of them is returned.  (Rare, so
+// it takes few registers and not long code: 64 passes over the list.)
+__device__ __forceinline__ u64 keep_greatest(u64 *list, int n, int want)
+{
+    const int lane = threadIdx.x & 63;
+    u64 t = 0;
+#pragma unroll 1
+    for (int bit = 63; bit >= 0; --bit) {
+        const u64 next = t | 1ull << bit;
+        int count = 0;
+#pragma unroll 1
+        for (int i = 0; i < n; i += 64) count += (int)__popcll(__ballot(i + lane < n && list[i + lane] >= next));
+        if (count >= want) t = next;
+    }
+    int at = 0;
+#pragma unroll 1
+    for (int i = 0; i < n; i += 64) {
+        const u64 mine = i + lane < n ? list[i + lane] : 0;
+        const u64 who = __ballot(mine >= t);
+        if (mine >= t) list[at + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = mine;
+        at += (int)__popcll(who);
+    }
+    return t;
+}
+
 // ---- parts --------------------------------------------------------------------------------------
 
-// A workgroup takes a part of a row, whose logits stay in registers: one read of memory for the maximum, the sum of weights and
-// the best ones.  A thread's logits go by their numbers, not by addresses (its loads of 16 bytes are aligned to a logit only), so
-// rows with the same logits have the same sum wherever they begin.
-template <typename T, int PIECES> struct Part {
-    static constexpr int E = 16 / sizeof(T), COUNT = E * PIECES, SIZE = kThreads * COUNT;
-    static_assert(COUNT <= 32, "");
-};
+// A workgroup takes a part of a row, `chunks` times `PIECES` pieces of 16 bytes to a thread: one read of memory for the maximum,
+// the sum of weights and the best ones.  A thread's logits go by their numbers, not by addresses (its loads of 16 bytes are
+// aligned to a logit only), so rows with the same logits have the same sum wherever they begin.
 typedef vec<uint32_t, 4> Piece;
 typedef Piece PieceAt2 __attribute__((aligned(2)));
 typedef Piece PieceAt4 __attribute__((aligned(4)));
 
 template <typename T, int PIECES>
-__global__ __launch_bounds__(kThreads) void k_beam_parts(BeamArgs a)
+__global__ __launch_bounds__(kThreads, 4) void k_beam_parts(BeamArgs a)
 {
-    typedef Part<T, PIECES> P;
     typedef std::conditional_t<sizeof(T) == 2, PieceAt2, PieceAt4> Unaligned;
-    constexpr int E = P::E;
+    constexpr int E = 16 / sizeof(T), COUNT = E * PIECES, CHUNK = kThreads * COUNT;
     __shared__ PartShared sh;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t all = (int64_t)a.queries * a.beams * a.parts;
-    for (int64_t g = blockIdx.x; g < all; g += gridDim.x) {
-        const int row = (int)(g / a.parts), part = (int)(g % a.parts);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    u64 *const list = sh.list[wave];
+    const uint32_t all = (uint32_t)a.queries * a.beams * a.parts;
+    for (uint32_t g = blockIdx.x; g < all; g += gridDim.x) {
+        const int row = (int)(g / (uint32_t)a.parts), part = (int)(g % (uint32_t)a.parts);
         if (!alive(a, row) || ended(a, row)) continue;
         const T *const logits = (const T *)a.logits + row * a.row_stride;
-        const int first = part * P::SIZE;
-        auto index = [&](int i) { return first + (i / E * kThreads + tid) * E + i % E; };
-        float x[P::COUNT];
+        const int first = part * a.chunks * CHUNK, chunks = min(a.chunks, (a.vocab - first - 1) / CHUNK + 1);
+        Piece raw[PIECES];
+        // (a piece that goes beyond the row's end is read from so many logits earlier, and those are left out: see below)
+        auto number = [&](int i0) { return min(i0, max(a.vocab - E, 0)); };
+        auto load = [&](int c) {
 #pragma unroll
-        for (int j = 0; j < PIECES; ++j) {
+            for (int j = 0; j < PIECES; ++j) raw[j] = *(const Unaligned *)(logits + number(first + c * CHUNK + (j * kThreads + tid) * E));
+        };
+        auto load_first = [&] {
+            if (a.vocab >= E) return load(0);
             T y[E];
-            const int i0 = index(j * E);
-            if (i0 + E <= a.vocab) {
-                const Piece v = *(const Unaligned *)(logits + i0);
-                __builtin_memcpy(y, &v, 16);
-            } else {
 #pragma unroll
-                for (int e = 0; e < E; ++e) y[e] = i0 + e < a.vocab ? logits[i0 + e] : (T)-INFINITY;
-            }
+            for (int e = 0; e < E; ++e) y[e] = e < a.vocab ? logits[e] : (T)-INFINITY;
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[j * E + e] = (float)y[e];
-        }
-
-        float top, most[PIECES];
+            for (int j = 0; j < PIECES; ++j) __builtin_memcpy(&raw[j], y, 16);
+        };
+        float top;
         double total;
-        uint32_t least;
-        while (true) {
-            float mine = -INFINITY;
+        int listed;
+        // What kind of numbers there are shows in the sum: kind 0 takes the logits as they come, 1 takes out what is no number, 2
+        // counts those of +infinity (the weights of the others are 0).
+        for (int kind = 0;; ++kind) {
+            // A lane's greatest, and the wave's, which weights are taken against: its product with log2(e), rounded, and what the
+            // rounding makes of a weight, to the first power.  (One operation for each exponent, and no error but its own rounding.)
+            float mine = -INFINITY, ref = 0, halvings = 0;
+            double correction = 1;
+            double sum = 0;
+            uint32_t least = 0;
+            float from = 0;
+            listed = 0;
+            load_first();
+            for (int c = 0; c < chunks; ++c) {
+                float x[COUNT], most[PIECES];
 #pragma unroll
-            for (int j = 0; j < PIECES; ++j) {
-                most[j] = x[j * E];
+                for (int j = 0; j < PIECES; ++j) {
+                    T y[E];
+                    __builtin_memcpy(y, &raw[j], 16);
 #pragma unroll
-                for (int e = 1; e < E; ++e) most[j] = fmaxf(most[j], x[j * E + e]);
-                mine = fmaxf(mine, most[j]);
+                    for (int e = 0; e < E; ++e) x[j * E + e] = (float)y[e];
+                    const int i0 = first + c * CHUNK + (j * kThreads + tid) * E;
+                    if (i0 + E > a.vocab) {
+#pragma unroll
+                        for (int e = 0; e < E; ++e) x[j * E + e] = number(i0) + e >= i0 ? x[j * E + e] : -INFINITY;
+                    }
+                }
+                if (c + 1 < chunks) load(c + 1);
+                if (kind)
+#pragma unroll
+                    for (int i = 0; i < COUNT; ++i) x[i] = x[i] > -INFINITY ? x[i] : -INFINITY;
+#pragma unroll
+                for (int j = 0; j < PIECES; ++j) {
+                    most[j] = x[j * E];
+#pragma unroll
+                    for (int e = 1; e < E; ++e) most[j] = fmaxf(most[j], x[j * E + e]);
+                    mine = fmaxf(mine, most[j]);
+                }
+                // of a wave alone so many lanes have one at least as great: the part's best are not below any wave's bound
+                least = max(least, reached_by<16>(mine > -INFINITY ? key_of(mine) : 0, a.picks));
+                if (c == 0) {
+                    __syncthreads();
+                    if (lane == 0) sh.bound[wave] = least;
+                    __syncthreads();
+                    least = max(max(max(sh.bound[0], sh.bound[1]), max(sh.bound[2], sh.bound[3])), kNever + 1);
+                }
+                from = value_of(least);
+                top = wave_max(mine);
+                const float now = top > -INFINITY ? top : 0.0f;
+                if (kind < 2 && now != ref) {
+                    // (nothing as yet stays nothing: the first reference can be far below 0)
+                    sum = sum > 0 ? sum * (double)__builtin_amdgcn_exp2f((ref - now) * 1.44269504088896f) : sum;
+                    ref = now;
+                    halvings = ref * kLog2e;
+                    correction = 1 + ((double)halvings - (double)ref * (double)kLog2e) * 0.69314718055994531;
+                }
+                // Weights in 32 bits, a chunk's up to 32 added there by pieces (ten roundings at the most), all others in 64.
+                auto add_up = [&](auto weight) {
+                    float all_pieces = 0;
+#pragma unroll
+                    for (int j = 0; j < PIECES; ++j) {
+                        float w[E];
+#pragma unroll
+                        for (int e = 0; e < E; ++e) w[e] = weight(x[j * E + e]);
+#pragma unroll
+                        for (int n = E / 2; n; n /= 2)
+#pragma unroll
+                            for (int e = 0; e < n; ++e) w[e] += w[e + n];
+                        all_pieces += w[0];
+                    }
+                    return all_pieces;
+                };
+                if (kind < 2 && fabsf(ref) < kNear) {
+                    const float part_sum = add_up([&](float z) { return __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, -halvings)); });
+                    sum = __builtin_fma((double)part_sum, correction, sum);
+                } else if (kind < 2) {
+                    sum += (double)add_up([&](float z) { return __builtin_amdgcn_exp2f((z - ref) * kLog2e); });
+                } else {
+                    sum += (double)add_up([&](float z) { return z == INFINITY ? 1.0f : 0.0f; });
+                }
+                // Each wave lists what reaches the bound, group by group in the logits' order.
+#pragma unroll
+                for (int j = 0; j < PIECES; ++j) {
+                    if (!__any(most[j] >= from)) continue;
+                    if (listed > kKept) {      // then only what is greater than all but the kept ones counts: equal ones come later
+                        least = max(least, (uint32_t)(keep_greatest(list, listed, a.picks) >> 32) + 1);
+                        from = value_of(least);
+                        listed = a.picks;
+                    }
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const bool is = x[j * E + e] >= from;
+                        const u64 who = __ballot(is);
+                        if (!who) continue;
+                        const int at = listed + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+                        if (is) list[at] = (u64)key_of(x[j * E + e]) << 32 | (uint32_t)~(number(first + c * CHUNK + (j * kThreads + tid) * E) + e);
+                        listed += (int)__popcll(who);
+                    }
+                }
             }
-            top = wave_max(mine);
-            // of a wave alone so many lanes have one at least as great: the part's best are not below any wave's bound
-            const uint32_t bound = reached_by(mine > -INFINITY ? key_of(mine) : 0, a.picks);
-            __syncthreads();
-            if (lane == 0) { sh.top[wave] = top; sh.bound[wave] = bound; }
-            __syncthreads();
-            top = fmaxf(fmaxf(sh.top[0], sh.top[1]), fmaxf(sh.top[2], sh.top[3]));
-            least = max(max(max(sh.bound[0], sh.bound[1]), max(sh.bound[2], sh.bound[3])), kNever + 1);
-            // Weights in 32 bits, a thread's up to 32 added there by pieces (ten roundings at the most), the threads' in 64.
-            const float off = top > -INFINITY ? top : 0.0f;
-            float sum = 0;
-#pragma unroll
-            for (int j = 0; j < PIECES; ++j) {
-                float w[E];
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    w[e] = __builtin_amdgcn_exp2f((x[j * E + e] - off) * 1.44269504088896f);
-#pragma unroll
-                for (int n = E / 2; n; n /= 2)
-#pragma unroll
-                    for (int e = 0; e < n; ++e) w[e] += w[e + n];
-                sum += w[0];
-            }
-            if (top == INFINITY) {      // (then the exponents were none)
-                sum = 0;
-#pragma unroll
-                for (int i = 0; i < P::COUNT; ++i) sum += x[i] == top ? 1.0f : 0.0f;
+            if (listed > kKept) {
+                keep_greatest(list, listed, a.picks);
+                listed = a.picks;
             }
             const double wave_total = wave_sum(mine == mine ? sum : NAN);
-            if (lane == 0) sh.sum[wave] = wave_total;
-            __syncthreads();
-            total = sh.sum[0] + sh.sum[1] + sh.sum[2] + sh.sum[3];
-            if (total == total) break;
-            // There are logits that are no numbers: they are taken out, once.
-#pragma unroll
-            for (int i = 0; i < P::COUNT; ++i) x[i] = x[i] > -INFINITY ? x[i] : -INFINITY;
-        }
-
-        // Each wave lists what reaches the bound.
-        const float from = value_of(least);
-        int mine_listed = 0;
-        auto put = [&](bool is, float z, int i) {
-            const u64 who = __ballot(is);
-            if (!who) return;
-            const int at = mine_listed + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
-            if (is && at < kWaveList) sh.list[wave * kWaveList + at] = (u64)key_of(z) << 32 | (uint32_t)~index(i);
-            mine_listed += (int)__popcll(who);
-        };
-#pragma unroll
-        for (int j = 0; j < PIECES; ++j) {
-            if (!__any(most[j] >= from)) continue;
-#pragma unroll
-            for (int e = 0; e < E; ++e) put(x[j * E + e] >= from, x[j * E + e], j * E + e);
-        }
-        if (lane == 0) sh.counts[wave] = mine_listed;
-        __syncthreads();
-        if (max(max(sh.counts[0], sh.counts[1]), max(sh.counts[2], sh.counts[3])) > kWaveList) {
-            // Too many reach the bound (equal ones, mostly): the value of the last that is wanted, bit by bit over all threads, and of
-            // those with that value the ones with the lowest numbers.
-            uint32_t t = 0;
-            for (int bit = 31; bit >= 0; --bit) {
-                const uint32_t next = t | 1u << bit;
-                int n = 0;
-#pragma unroll
-                for (int i = 0; i < P::COUNT; ++i) n += key_of(x[i]) >= next;
-                for (int d = 1; d < 64; d <<= 1) n += __shfl_xor(n, d);
-                __syncthreads();
-                if (lane == 0) sh.counts[wave] = n;
-                __syncthreads();
-                if (sh.counts[0] + sh.counts[1] + sh.counts[2] + sh.counts[3] >= a.picks) t = next;
-            }
-            mine_listed = 0;
-            int taken = 0;      // of the pieces of one number, the threads in order
-            for (int j = 0; j < PIECES; ++j) {
-                int mine_at = 0;
-#pragma unroll
-                for (int i = 0; i < P::COUNT; ++i) mine_at += i / E == j && key_of(x[i]) == t;
-                int inc = mine_at;
-                for (int d = 1; d < 64; d <<= 1) {
-                    const int o = __shfl_up(inc, d);
-                    if (lane >= d) inc += o;
-                }
-                __syncthreads();
-                if (lane == 63) sh.counts[wave] = inc;
-                __syncthreads();
-                int at = taken + inc - mine_at;
-                for (int w = 0; w < kWaves; ++w) {
-                    if (w < wave) at += sh.counts[w];
-                    taken += sh.counts[w];
-                }
-#pragma unroll
-                for (int i = 0; i < P::COUNT; ++i)
-                    if (i / E == j) put(key_of(x[i]) > t || (key_of(x[i]) == t && at++ < a.picks), x[i], i);
+            if (lane == 0) {
+                sh.top[wave] = top;
+                sh.sum[wave] = wave_total;
+                sh.counts[wave] = listed;
             }
             __syncthreads();
-            if (lane == 0) sh.counts[wave] = mine_listed;
-            __syncthreads();
+            top = fmaxf(fmaxf(sh.top[0], sh.top[1]), fmaxf(sh.top[2], sh.top[3]));
+            total = 0;
+            for (int w = 0; w < kWaves; ++w)
+                total += kind == 2 || sh.top[w] == top ? sh.sum[w] : sh.sum[w] * (double)__builtin_amdgcn_exp2f((sh.top[w] - top) * 1.44269504088896f);
+            if (kind == 2 || fabs(total) < INFINITY) break;
         }
-        // In order: an entry's place is the number of greater ones.  (First all of a query's parts' firsts, then their seconds.)  Four threads to an entry, one for each wave's list.
+        // In order: an entry's place is the number of greater ones.  (First all of a query's parts' firsts, then their seconds.)  Four
+        // threads to an entry, one for each wave's list.
         const int ends[kWaves] = {sh.counts[0], sh.counts[0] + sh.counts[1], sh.counts[0] + sh.counts[1] + sh.counts[2],
                                   sh.counts[0] + sh.counts[1] + sh.counts[2] + sh.counts[3]};
         const int n = ends[kWaves - 1], lists = a.beams * a.parts;
-        u64 *const best = a.best + g / lists * lists * a.picks + g % lists;
+        u64 *const best = a.best + (int64_t)(g / (uint32_t)lists) * lists * a.picks + g % (uint32_t)lists;
         for (int i0 = 0; i0 < n; i0 += kThreads / kWaves) {
             const int i = i0 + tid / kWaves, l = tid % kWaves;
             const int w = (i >= ends[0]) + (i >= ends[1]) + (i >= ends[2]);
-            const u64 entry = i < n ? sh.list[w * kWaveList + i - (w ? ends[w - 1] : 0)] : ~0ull;
+            const u64 entry = i < n ? sh.list[w][i - (w ? ends[w - 1] : 0)] : ~0ull;
             int before = 0;
             const int to = sh.counts[l];
 #pragma unroll 4
-            for (int j = 0; j < to; ++j) before += sh.list[l * kWaveList + j] > entry;
+            for (int j = 0; j < to; ++j) before += sh.list[l][j] > entry;
             before += __shfl_xor(before, 1);
             before += __shfl_xor(before, 2);
             if (i < n && l == 0 && before < a.picks) best[(int64_t)before * lists] = entry;
@@ -297,11 +330,10 @@ __global__ __launch_bounds__(kQueryThreads) void k_beam_queries(BeamArgs a)
 {
     __shared__ QueryShared sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int lists = a.beams * a.parts;
-    const int64_t listed = (int64_t)lists * a.picks;
+    const uint32_t lists = a.beams * a.parts, listed = lists * a.picks;      // (2^21 at the most)
     for (int q = blockIdx.x; q < a.queries; q += gridDim.x) {
-        const u64 *const best = a.best + q * listed;
-        const u64 held = tid < listed ? best[tid] : 0;
+        const u64 *const best = a.best + (int64_t)q * listed;
+        const u64 held = (uint32_t)tid < listed ? best[tid] : 0;
         __syncthreads();
         for (int w = wave; w < a.beams; w += kQueryWaves) {
             const int row = q * a.beams + w;
@@ -333,9 +365,9 @@ __global__ __launch_bounds__(kQueryThreads) void k_beam_queries(BeamArgs a)
         if (tid == 0) sh.listed = 0;
         __syncthreads();
         // rank and number of an entry of the parts' lists, if it is a candidate
-        auto from_list = [&](int64_t i, u64 e, double &rank, u64 &number) {
+        auto from_list = [&](uint32_t i, u64 e, double &rank, u64 &number) {
             if (e == 0) return false;
-            const int w = (int)((uint32_t)(i % lists) / (uint32_t)a.parts);
+            const int w = (int)(i % lists / (uint32_t)a.parts);
             const double shift = sh.shift[w];
             const float x = value_of((uint32_t)(e >> 32)), top = sh.top[w];
             if (!(shift == shift) || (top == INFINITY && x < top)) return false;
@@ -349,7 +381,7 @@ __global__ __launch_bounds__(kQueryThreads) void k_beam_queries(BeamArgs a)
             u64 number;
             u64 e = held;
 #pragma unroll 1
-            for (int64_t i = tid; i < listed; i += kQueryThreads) {
+            for (uint32_t i = tid; i < listed; i += kQueryThreads) {
                 if (from_list(i, e, rank, number)) f(rank, number);
                 if (i + kQueryThreads < listed) e = best[i + kQueryThreads];
             }
@@ -360,7 +392,7 @@ __global__ __launch_bounds__(kQueryThreads) void k_beam_queries(BeamArgs a)
         };
         uint32_t mine = 0;
         each([&](double rank, u64) { mine = max(mine, (uint32_t)(key_of(rank) >> 32)); });
-        const uint32_t bound = reached_by(mine, a.picks);
+        const uint32_t bound = reached_by<8>(mine, a.picks);      // (to 12 bits behind the first: of 11 bits the exponent's)
         if (lane == 0) sh.bound[wave] = bound;
         __syncthreads();
         uint32_t least = 0;
@@ -431,8 +463,9 @@ template <typename T, int PIECES> hipError_t beam(const BeamArgs &a, hipStream_t
     return hipGetLastError();
 }
 
-// Logits of a part: 8192, or 2048 where those would make too few workgroups.
-constexpr int kLarge = 8192, kSmall = 2048, kFewParts = 512;
+// Logits of a chunk: 8192, or 2048 where those would make too few workgroups; a part has several chunks where there are many
+// rows, since what a part costs besides is that of about 8192 logits.
+constexpr int kLarge = 8192, kSmall = 2048, kFewParts = 512, kManyParts = 2048, kMostChunks = 4;
 
 }  // namespace
 
@@ -440,8 +473,10 @@ BeamSizes beam_sizes(int32_t queries, int32_t beams, int32_t vocab, int32_t pick
 {
     BeamSizes z{};
     const int64_t rows = (int64_t)queries * beams;
-    z.size = rows * ((vocab + kLarge - 1) / kLarge) < kFewParts ? kSmall : kLarge;
-    z.parts = (vocab + z.size - 1) / z.size;
+    const int64_t large = rows * ((vocab + kLarge - 1) / kLarge);
+    z.chunk = large < kFewParts ? kSmall : kLarge;
+    z.chunks = std::max<int64_t>(1, std::min<int64_t>(kMostChunks, large / kManyParts));
+    z.parts = (vocab + z.chunk * z.chunks - 1) / (z.chunk * z.chunks);
     const int64_t groups = rows * z.parts;
     z.sum_at = groups * picks * (int64_t)sizeof(u64);
     z.top_at = z.sum_at + groups * (int64_t)sizeof(double);
@@ -449,9 +484,9 @@ BeamSizes beam_sizes(int32_t queries, int32_t beams, int32_t vocab, int32_t pick
     return z;
 }
 
-hipError_t launch_beam(const BeamArgs &a, int32_t size, int32_t type, hipStream_t s)
+hipError_t launch_beam(const BeamArgs &a, const BeamSizes &z, int32_t type, hipStream_t s)
 {
-    const bool small = size == kSmall;
+    const bool small = z.chunk == kSmall;
     switch (type) {
     case INFAAS_SEL_TYPE_FP32: return small ? beam<float, 2>(a, s) : beam<float, 8>(a, s);
     case INFAAS_SEL_TYPE_BF16: return small ? beam<bf16_t, 1>(a, s) : beam<bf16_t, 4>(a, s);

@@ -152,7 +152,7 @@ struct CopyArgs {
 struct BeamArgs {
     const void *logits;
     int64_t row_stride;
-    int32_t queries, beams, vocab, picks, end_token, parts;
+    int32_t queries, beams, vocab, picks, end_token, chunks, parts;
     const float *scores, *factor;
     const int32_t *ended;
     int32_t *out_parent, *out_token;
@@ -162,7 +162,7 @@ struct BeamArgs {
     double *sum;
     float *top;
 };
-struct BeamSizes { int64_t size, parts, sum_at, top_at, bytes; };      // size: logits of a part
+struct BeamSizes { int64_t chunk, chunks, parts, sum_at, top_at, bytes; };      // a chunk's logits, a part's chunks, a row's parts
 constexpr int kMostBeams = 64;       // beams, and picks
 
 constexpr int kMostSeqs = 4096;      // of a table
@@ -225,7 +225,7 @@ hipError_t launch_read(const ReadArgs &a, int32_t type, hipStream_t s);
 hipError_t launch_advance(const AdvanceArgs &a, hipStream_t s);
 hipError_t launch_copy(const CopyArgs &a, hipStream_t s);
 BeamSizes beam_sizes(int32_t queries, int32_t beams, int32_t vocab, int32_t picks);
-hipError_t launch_beam(const BeamArgs &a, int32_t size, int32_t type, hipStream_t s);
+hipError_t launch_beam(const BeamArgs &a, const BeamSizes &z, int32_t type, hipStream_t s);
 hipError_t launch_sample(const SampleArgs &a, int32_t type, hipStream_t s);
 
 }  // namespace infaas

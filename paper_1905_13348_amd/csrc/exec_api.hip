@@ -206,7 +206,8 @@ int check_beam(int32_t queries, int32_t beams, int32_t vocab, int32_t picks, int
         return refuse("beam: %d beams and %d picks (1 .. %d)", beams, picks, kMostBeams);
     if (vocab < 1 || vocab > 1 << 20) return refuse("beam: a vocabulary of %d (1 .. 1048576)", vocab);
     if (type != INFAAS_SEL_TYPE_FP32 && type != INFAAS_SEL_TYPE_BF16 && type != INFAAS_SEL_TYPE_FP16) return refuse("beam: type %d", type);
-    if ((int64_t)queries * beams > INT32_MAX) return refuse("beam: %d queries of %d beams", queries, beams);
+    // (a part of a row has 2048 logits at least)
+    if ((int64_t)queries * beams * (vocab / 2048 + 1) > INT32_MAX) return refuse("beam: %d queries of %d beams", queries, beams);
     return INFAAS_SEL_OK;
 }
 
@@ -476,9 +477,9 @@ int infaas_sel_exec_beam(infaas_sel_exec_t *x, int32_t queries, int32_t beams, i
     const BeamSizes z = beam_sizes(queries, beams, vocab, picks);
     if (int rc = ensure(x, z.bytes, (hipStream_t)hip_stream, true, "infaas_sel_exec_reserve_beam")) return rc;
     char *const p = (char *)x->scratch;
-    const BeamArgs a{d_logits, row_stride, queries, beams, vocab, picks, end_token, (int32_t)z.parts, d_scores, d_factor, d_ended,
+    const BeamArgs a{d_logits, row_stride, queries, beams, vocab, picks, end_token, (int32_t)z.chunks, (int32_t)z.parts, d_scores, d_factor, d_ended,
                      d_out_parent, d_out_token, d_out_score, (unsigned long long *)p, (double *)(p + z.sum_at), (float *)(p + z.top_at)};
-    if (hipError_t e = launch_beam(a, (int32_t)z.size, type, (hipStream_t)hip_stream)) return hip_failed(e, "infaas_sel_exec_beam");
+    if (hipError_t e = launch_beam(a, z, type, (hipStream_t)hip_stream)) return hip_failed(e, "infaas_sel_exec_beam");
     return INFAAS_SEL_OK;
 }
 

@@ -113,6 +113,22 @@ def test_logits_alike(vocab, picks):
     check(np.where(rng.random((6, vocab)) < 0.5, 0.0, -0.0), np.zeros((2, 3)), picks, "bf16")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [1, 150, 600])
+def test_parts_of_several_chunks(rows, dtype):
+    """Many rows make parts of several chunks: rising and falling logits, equal ones, masks at either end, numbers that are none."""
+    rng = np.random.default_rng(rows)
+    V = 70_001
+    x = np.repeat(made(rng, 3, V), -(-rows // 3), axis=0)[:rows]
+    up = np.arange(V) / V * 20
+    for r, row in enumerate((up, -up, np.zeros(V), np.where(np.arange(V) < 69_990, -np.inf, 1.0), np.where(np.arange(V) % 9000, -60_000.0, up))):
+        x[r % rows] = row
+    if rows > 10:
+        x[6, 40_000], x[7, 69_999], x[8, [3, 50_000]] = np.nan, np.inf, np.inf
+        x[8, 100] = np.nan
+    check(x, -rng.random((rows, 1)) * 3, 12, dtype)
+
+
 def test_many_ties_between_many_beams():
     """More equal continuations than a query's list holds."""
     check(np.zeros((64, 20_000)), np.zeros((1, 64)), 64, "fp32")
