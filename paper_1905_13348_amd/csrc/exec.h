@@ -124,7 +124,8 @@ struct AppendArgs {
 struct AppendScaledArgs {
     AppendArgs append;
     const int32_t *seq_start;
-    int32_t q_groups, chunk;         // workgroups for the queries; tokens that one of the others looks through
+    int32_t q_groups, q_tokens;      // workgroups for the queries, and their tokens
+    int32_t chunk, shares, rows;     // tokens that one of the others looks through; how many share its columns; rows side by side
 };
 
 struct ReadArgs {

@@ -253,7 +253,7 @@ int append(infaas_sel_exec *x, const infaas_sel_cache *cache, const infaas_sel_s
     AppendArgs a{*args, cache_args(cache, batch, scales), batch->d_token_seq, batch->d_token_pos, batch->num_tokens, batch->num_seqs,
                  batch->heads, cache->kv_heads, cache->head_dim};
     if (coded) {
-        const AppendScaledArgs sa{a, batch->d_seq_start, 0, 0};
+        const AppendScaledArgs sa{a, batch->d_seq_start, 0, 0, 0, 0, 0};
         if (hipError_t e = launch_append_scaled(sa, cache->type, (hipStream_t)hip_stream)) return hip_failed(e, "infaas_sel_exec_append_scaled");
         return INFAAS_SEL_OK;
     }
