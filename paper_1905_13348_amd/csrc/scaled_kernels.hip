@@ -249,32 +249,33 @@ template <typename T> __device__ __forceinline__ void append_blocks(const Append
     }
 }
 
-// The workgroups in front take the queries of some tokens each.  The others take `chunk` tokens: of those they look for the ones with
-// which a block begins for this step, and take these blocks one after the other.  The tokens of a block are known from the
-// sequence's first one (their positions rise by one), so nothing is passed between workgroups and no order of atomics decides.
+// The workgroups in front take `chunk` tokens: of those they look for the ones with which a block begins for this step, and take
+// these blocks one after the other.  The tokens of a block are known from the sequence's first one (their positions rise by
+// one), so nothing is passed between workgroups and no order of atomics decides.  The others take the queries of some tokens each.
 template <typename T>
 __global__ __launch_bounds__(256) void k_append_scaled(AppendScaledArgs p)
 {
     __shared__ float2 turns[kTurns];
-    if ((int)blockIdx.x < p.q_groups) {
-        for (int64_t t = (int64_t)blockIdx.x * p.q_tokens; t < p.append.num_tokens; t += (int64_t)p.q_groups * p.q_tokens)
+    const int blocks = gridDim.x - p.q_groups;
+    if ((int)blockIdx.x >= blocks) {
+        for (int64_t t = (int64_t)(blockIdx.x - blocks) * p.q_tokens; t < p.append.num_tokens; t += (int64_t)p.q_groups * p.q_tokens)
             append_queries<T>(p, (int)t, turns);
         return;
     }
     const int64_t all = ((int64_t)p.append.num_tokens + p.chunk - 1) / p.chunk * p.shares;
-    for (int64_t g = blockIdx.x - p.q_groups; g < all; g += gridDim.x - p.q_groups) append_blocks<T>(p, g / p.shares, (int)(g % p.shares), turns);
+    for (int64_t g = blockIdx.x; g < all; g += blocks) append_blocks<T>(p, g / p.shares, (int)(g % p.shares), turns);
 }
 
 // ---- read -------------------------------------------------------------------------------------
 
-// A thread takes sixteen bytes of the result, eight dimensions of a token's key or value, of four tokens or parts of a token at a
-// time: where they are is looked up for all four before their loads, since each look-up is three trips to memory in a row.
+// A thread takes sixteen dimensions of a token's key or value, of four tokens or parts of a token at a time: where they are is
+// looked up for all four before their loads, since each look-up is three trips to memory in a row.
 template <typename T, bool CODED>
 __global__ __launch_bounds__(256) void k_read(ReadArgs p)
 {
     constexpr int DEEP = 4;
     const CacheArgs &c = p.cache;
-    const uint32_t parts = p.head_dim / 8, each = 2 * p.kv_heads * parts;
+    const uint32_t parts = p.head_dim / 16, each = 2 * p.kv_heads * parts;
     const int64_t all = (int64_t)each * p.num_tokens;
     for (int64_t i0 = (int64_t)blockIdx.x * 256 * DEEP; i0 < all; i0 += (int64_t)gridDim.x * 256 * DEEP) {
         const int64_t first = i0 / each;                                // (the same for the workgroup)
@@ -293,21 +294,22 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs p)
         }
 #pragma unroll
         for (int d = 0; d < DEEP; ++d) page[d] = page_of(c, seq[d], p.num_seqs, pos[d]);
-        vec<T, 8> y[DEEP];
-        vec<uint32_t, 2> codes[DEEP];
+        vec<uint32_t, 4> raw[DEEP][2];
         uint32_t e[DEEP];
 #pragma unroll
         for (int d = 0; d < DEEP; ++d) {
             const bool keys = part[d] < p.kv_heads * parts;
             const int head = (int)(part[d] / parts % p.kv_heads), slot = pos[d] & ((1 << c.page_shift) - 1);
             const int64_t there = max(page[d], (int64_t)0);
-            const int64_t at = page[d] < 0 ? 0 : there * c.page_stride + slot * c.slot_stride + head * c.head_stride + part[d] % parts * 8;
+            const int64_t at = page[d] < 0 ? 0 : there * c.page_stride + slot * c.slot_stride + head * c.head_stride + part[d] % parts * 16;
+            const void *pool = keys ? c.k : c.v;
             if (CODED) {
                 e[d] = (keys ? c.k_scale : c.v_scale)[page[d] < 0 ? 0 : there * c.scale_page_stride +
                                                                           (slot >> c.block_shift) * c.scale_block_stride + head * c.scale_head_stride];
-                codes[d] = *(const vec<uint32_t, 2> *)((const uint8_t *)(keys ? c.k : c.v) + at);
+                raw[d][0] = *(const vec<uint32_t, 4> *)((const uint8_t *)pool + at);
             } else {
-                y[d] = *(const vec<T, 8> *)((const T *)(keys ? c.k : c.v) + at);
+                raw[d][0] = *(const vec<uint32_t, 4> *)((const T *)pool + at);
+                raw[d][1] = *(const vec<uint32_t, 4> *)((const T *)pool + at + 8);
             }
         }
 #pragma unroll
@@ -315,10 +317,16 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs p)
             if (token[d] >= p.num_tokens) continue;
             const bool keys = part[d] < p.kv_heads * parts;
             const int head = (int)(part[d] / parts % p.kv_heads);
-            if (CODED) y[d] = decode8<T>(codes[d], e[d]);
-            if (page[d] < 0) y[d] = vec<T, 8>{};
             T *to = keys ? (T *)p.k + token[d] * p.k_token_stride + head * p.k_head_stride : (T *)p.v + token[d] * p.v_token_stride + head * p.v_head_stride;
-            *(vec<T, 8> *)(to + part[d] % parts * 8) = y[d];
+            to += part[d] % parts * 16;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                union { vec<T, 8> v; vec<uint32_t, 4> w; } u;
+                if (CODED) u.v = decode8<T>(vec<uint32_t, 2>{raw[d][0][2 * h], raw[d][0][2 * h + 1]}, e[d]);
+                else u.w = raw[d][h];
+                if (page[d] < 0) u.w = vec<uint32_t, 4>{};
+                *(vec<uint32_t, 4> *)(to + 8 * h) = u.w;
+            }
         }
     }
 }
@@ -326,7 +334,7 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs p)
 template <typename T>
 hipError_t read(const ReadArgs &a, hipStream_t s)
 {
-    const int64_t all = (int64_t)2 * a.kv_heads * (a.head_dim / 8) * a.num_tokens;
+    const int64_t all = (int64_t)2 * a.kv_heads * (a.head_dim / 16) * a.num_tokens;
     const dim3 grid((unsigned)std::min<int64_t>(kMostGroups, (all + 1023) / 1024));
     if (a.cache.k_scale) k_read<T, true><<<grid, 256, 0, s>>>(a);
     else k_read<T, false><<<grid, 256, 0, s>>>(a);
