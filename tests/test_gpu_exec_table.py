@@ -41,13 +41,14 @@ class Both:
 @pytest.mark.parametrize("S, width, page, pages, most", [
     (1, 1, 1, 1, 1), (1, 3, 4, 5, 20), (5, 4, 16, 30, 100), (64, 8, 4, 300, 400), (70, 5, 2, 200, 300), (300, 7, 8, 2000, 5000), (1025, 3, 16, 2500, 3000),
     (4096, 2, 8, 6000, 9000), (3, 700, 1, 1500, 1000), (16, 40, 64, 40_000, 20_000)])
-def test_a_life(S, width, page, pages, most):
-    """Steps of all kinds: sequences that grow, are cut, begin anew, go on from others, and pages that run out."""
-    rng = np.random.default_rng(S + width)
+@pytest.mark.parametrize("seed", [0, 1, 2])
+def test_a_life(S, width, page, pages, most, seed):
+    """Steps of all kinds: sequences that grow, are cut, begin anew, go on from others, and pages and tokens that run out."""
+    rng = np.random.default_rng(S + width + seed * 10_000)
     b = Both(S, width, page, pages, most)
     b.hold((rng.random(pages) < 0.2) * rng.integers(1, 3, pages))
     room = width * page
-    for t in range(14):
+    for t in range(21):
         kind = t % 7
         new, parent = rng.integers(0, max(2, room // 4), S), None
         if kind == 1:
