@@ -319,30 +319,37 @@ __device__ __forceinline__ void join(RowPart &a, float m1, float l1, vec<float, 
     a.m = m2;
 }
 
-constexpr int kNarrow = 16;      // rows of an item that its waves go through side by side
+// Rows of an item that its waves go through side by side.  (32 rows of 256 dimensions are more than a wave's registers.)
+template <int D> constexpr int kNarrow = D == 256 ? 16 : 32;
 
-// Up to sixteen rows: what bounds them is the cache's bytes, and a wave that computes while three stand by is too slow for
+// Up to thirty-two rows, GROUPS times sixteen: what bounds them is the cache's bytes, and a wave that computes while three stand by is too slow for
 // these.  So each wave has keys of its own, 32 at a time, nothing waits for another wave until the end, and the waves' parts are
 // joined through LDS.  Lane (key, c) loads the quarter c of a key's and of a value's codes, in one piece; with the dimensions
 // numbered that way for both operands the codes go from memory to the first product through registers alone.  Values are
 // written to the wave's part of LDS as numbers, to be read transposed.
-template <typename T, int D>
+template <typename T, int D, int GROUPS>
 __device__ __forceinline__ void narrow_item(const AttendArgs &a, const PlanItem &it, uint4 *lds0, uint4 *lds1, uint4 *lds2, uint4 *lds3,
-                                            float2 (*ml)[kNarrow])
+                                            float2 (*ml)[16])
 {
     constexpr int KEYS = 32, ROW = D * 2, PIECES = D / 64, CH = D / 8;      // PIECES: of 16 codes, of a lane's quarter
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, c = lane >> 4;
     const int G = a.batch.heads / a.batch.kv_heads, rows = it.nt * G;
-    const bool valid = col < rows;
-    const int rt = valid ? col / G : 0, token = it.t0 + rt, head = it.head * G + col - rt * G;
-    const int lim = valid ? min(a.plan.tokens[token].limit, it.k1) : 0;
-    vec<T, 8> q[D / 32];
+    int lim[GROUPS], end = 0, lo = 0x7fffffff;      // how far the rows see: each, one of them, all that see anything
+    vec<T, 8> q[GROUPS][D / 32];
 #pragma unroll
-    for (int kk = 0; kk < D / 32; ++kk) {
-        q[kk] = vec<T, 8>{};
-        if (valid) q[kk] = *(const vec<T, 8> *)((const T *)a.q + token * a.q_token_stride + head * a.q_head_stride + c * (D / 4) + kk * 8);
+    for (int g = 0; g < GROUPS; ++g) {
+        const int r = g * 16 + col;
+        const bool valid = r < rows;
+        const int rt = valid ? r / G : 0, token = it.t0 + rt, head = it.head * G + (valid ? r - rt * G : 0);
+        lim[g] = valid ? min(a.plan.tokens[token].limit, it.k1) : 0;
+#pragma unroll
+        for (int kk = 0; kk < D / 32; ++kk) {
+            q[g][kk] = vec<T, 8>{};
+            if (valid) q[g][kk] = *(const vec<T, 8> *)((const T *)a.q + token * a.q_token_stride + head * a.q_head_stride + c * (D / 4) + kk * 8);
+        }
+        end = max(end, lim[g]);
+        if (lim[g] > it.k0) lo = min(lo, lim[g]);
     }
-    int end = lim, lo = lim > it.k0 ? lim : 0x7fffffff;      // how far the rows see: one of them, all that see anything
     for (int d = 1; d < 16; d <<= 1) { end = max(end, __shfl_xor(end, d)); lo = min(lo, __shfl_xor(lo, d)); }
     end = __builtin_amdgcn_readfirstlane(end);
     lo = __builtin_amdgcn_readfirstlane(lo);
@@ -353,10 +360,15 @@ __device__ __forceinline__ void narrow_item(const AttendArgs &a, const PlanItem 
     const int page_mask = (1 << a.cache.page_shift) - 1;
     const int32_t *const table = a.cache.table + (int64_t)it.seq * a.cache.table_width;
 
-    vec<float, 4> o[D / 16];
+    vec<float, 4> o[GROUPS][D / 16];
+    float m[GROUPS], l[GROUPS];
 #pragma unroll
-    for (int dt = 0; dt < D / 16; ++dt) o[dt] = vec<float, 4>{};
-    float m = -INFINITY, l = 0;
+    for (int g = 0; g < GROUPS; ++g) {
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) o[g][dt] = vec<float, 4>{};
+        m[g] = -INFINITY;
+        l[g] = 0;
+    }
     bool far = false, odd = false;
     int first_there = 0x7fffffff;
 
@@ -421,13 +433,17 @@ __device__ __forceinline__ void narrow_item(const AttendArgs &a, const PlanItem 
                     const int row = h * 16 + col;
                     *(vec<T, 8> *)(lv + row * ROW + (((c * PIECES + x) * 2 + y) ^ turn(row)) * 16) = u.v;
                 }
-        vec<float, 4> s[2];
+        vec<float, 4> s[GROUPS][2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            s[h] = vec<float, 4>{};
 #pragma unroll
-            for (int kk = 0; kk < D / 32; ++kk)
-                s[h] = Mfma<T>::run(decode8<T>(vec<uint32_t, 2>{kc[h][kk / 2][kk % 2 * 2], kc[h][kk / 2][kk % 2 * 2 + 1]}, ke[h]), q[kk], s[h]);
+            for (int g = 0; g < GROUPS; ++g) s[g][h] = vec<float, 4>{};
+#pragma unroll
+            for (int kk = 0; kk < D / 32; ++kk) {
+                const vec<T, 8> k = decode8<T>(vec<uint32_t, 2>{kc[h][kk / 2][kk % 2 * 2], kc[h][kk / 2][kk % 2 * 2 + 1]}, ke[h]);
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g) s[g][h] = Mfma<T>::run(k, q[g][kk], s[g][h]);
+            }
         }
         if (kt + 4 * KEYS < end) {      // the next tile is under way while this one's weights and products are computed
             locate(kt + 4 * KEYS);
@@ -435,49 +451,66 @@ __device__ __forceinline__ void narrow_item(const AttendArgs &a, const PlanItem 
             load(vc, a.cache.v);
             look_up(kt + 8 * KEYS);
         }
-        if (part || bits != ~0u) {
+        float top[GROUPS];
+        bool moves = far;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+        for (int g = 0; g < GROUPS; ++g) {
+            if (part || bits != ~0u) {
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const int i = h * 16 + c * 4 + x;
-                    s[h][x] = kt + i < lim && (bits >> i & 1) ? s[h][x] : -INFINITY;
-                }
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int i = h * 16 + c * 4 + x;
+                        s[g][h][x] = kt + i < lim[g] && (bits >> i & 1) ? s[g][h][x] : -INFINITY;
+                    }
+            }
+            top[g] = s[g][0][0];
+#pragma unroll
+            for (int x = 1; x < 8; ++x) top[g] = fmaxf(top[g], s[g][x / 4][x % 4]);
+            moves |= apart(top[g], a.scale_log2, m[g]) > kSlack + kRaise<T>;
         }
-        float top = s[0][0];
-#pragma unroll
-        for (int x = 1; x < 8; ++x) top = fmaxf(top, s[x / 4][x % 4]);
         // the weights' reference, as where tiles are full; a row's four lanes agree on it whenever it moves
-        float scale = a.scale_log2;
-        float ref = m == -INFINITY ? 0.0f : m;
-        if (__any(apart(top, scale, m) > kSlack + kRaise<T>) || far) {
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float m2 = fmaxf(m, apart(top, scale, kRaise<T>));
-            const float f = m2 == -INFINITY ? 1.0f : exp2_fast(m - m2);
-            m = m2;
-            l *= f;
+        float scale = a.scale_log2, ref[GROUPS];
 #pragma unroll
-            for (int dt = 0; dt < D / 16; ++dt) o[dt] *= f;
-            ref = m == -INFINITY ? 0.0f : m;
-            far = __any(fabsf(m) > kFused && m > -INFINITY);
+        for (int g = 0; g < GROUPS; ++g) ref[g] = m[g] == -INFINITY ? 0.0f : m[g];
+        if (__any(moves)) {
+            bool beyond = false;
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                top[g] = fmaxf(top[g], __shfl_xor(top[g], 16));
+                top[g] = fmaxf(top[g], __shfl_xor(top[g], 32));
+                const float m2 = fmaxf(m[g], apart(top[g], scale, kRaise<T>));
+                const float f = m2 == -INFINITY ? 1.0f : exp2_fast(m[g] - m2);
+                m[g] = m2;
+                l[g] *= f;
+#pragma unroll
+                for (int dt = 0; dt < D / 16; ++dt) o[g][dt] *= f;
+                ref[g] = m2 == -INFINITY ? 0.0f : m2;
+                beyond |= fabsf(m2) > kFused && m2 > -INFINITY;
+            }
+            far = __any(beyond);
             if (far) {
 #pragma unroll
-                for (int x = 0; x < 8; ++x) s[x / 4][x % 4] = apart(s[x / 4][x % 4], scale, ref);
+                for (int g = 0; g < GROUPS; ++g) {
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) s[g][x / 4][x % 4] = apart(s[g][x / 4][x % 4], scale, ref[g]);
+                    ref[g] = 0.0f;
+                }
                 scale = 1.0f;
-                ref = 0.0f;
             }
         }
-        vec<T, 8> pt;
+        vec<T, 8> pt[GROUPS];
 #pragma unroll
-        for (int x = 0; x < 8; x += 2) {
-            const vec<float, 2> e = {exp2_fast(s[x / 4][x % 4] * scale - ref), exp2_fast(s[x / 4][x % 4 + 1] * scale - ref)};
-            l += e[0];
-            l += e[1];
-            const vec<T, 2> y = __builtin_convertvector(e, vec<T, 2>);      // (the rounding of full tiles)
-            pt[x] = y[0];
-            pt[x + 1] = y[1];
-        }
+        for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+            for (int x = 0; x < 8; x += 2) {
+                const vec<float, 2> e = {exp2_fast(s[g][x / 4][x % 4] * scale - ref[g]), exp2_fast(s[g][x / 4][x % 4 + 1] * scale - ref[g])};
+                l[g] += e[0];
+                l[g] += e[1];
+                const vec<T, 2> y = __builtin_convertvector(e, vec<T, 2>);      // (the rounding of full tiles)
+                pt[g][x] = y[0];
+                pt[g][x + 1] = y[1];
+            }
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) {
             union { vec<short, 4> h[2]; vec<T, 8> v; } vf;
@@ -487,13 +520,14 @@ __device__ __forceinline__ void narrow_item(const AttendArgs &a, const PlanItem 
                 vf.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                     (lds_short4 *)(lv + row * ROW + ((dt * 2 + (col & 3) / 2) ^ turn(row)) * 16 + (col & 1) * 8));
             }
-            o[dt] = Mfma<T>::run(vf.v, pt, o[dt]);
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) o[g][dt] = Mfma<T>::run(vf.v, pt[g], o[g][dt]);
         }
     }
     if (__any(odd)) {      // the values that were taken out, of the tiles that they were taken out of
         for (int t = it.k0 + wave * KEYS; t < end; t += 4 * KEYS) {
             if (t + KEYS <= lo) continue;
-            for (int key = t; key < min(t + KEYS, lim); ++key) {
+            for (int key = t; key < min(t + KEYS, end); ++key) {
                 const int64_t page = table[key >> a.cache.page_shift];
                 if (page < 0 || page >= a.cache.num_pages) continue;
                 const int slot = key & page_mask;
@@ -505,44 +539,49 @@ __device__ __forceinline__ void narrow_item(const AttendArgs &a, const PlanItem 
                 for (int dt = 0; dt < D / 16; ++dt) {
                     const vec<T, 4> y = decode4<T>(*(const uint32_t *)(v + dt * 16), e8);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (!(fabsf((float)y[e]) < INFINITY)) o[dt][e] += (float)y[e];
+                    for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (key < lim[g] && !(fabsf((float)y[e]) < INFINITY)) o[g][dt][e] += (float)y[e];
                 }
             }
         }
     }
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if (lim <= it.k0) {
-        m = -INFINITY;
-        l = 0;
+    // the waves' parts, sixteen rows at a time
 #pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) o[dt] = vec<float, 4>{};
-    }
-    if (l == 0 && lim > first_there) m = kNothing;
-
-    // the waves' parts
-    __syncthreads();
-    if (c == 0) ml[wave][col] = float2{m, l};
+    for (int g = 0; g < GROUPS; ++g) {
+        l[g] += __shfl_xor(l[g], 16);
+        l[g] += __shfl_xor(l[g], 32);
+        if (lim[g] <= it.k0) {
+            m[g] = -INFINITY;
+            l[g] = 0;
 #pragma unroll
-    for (int dt = 0; dt < D / 16; ++dt) ((vec<float, 4> *)lv)[col * (D / 4) + ((dt * 4 + c) ^ col)] = o[dt];
-    __syncthreads();
-    for (int i = tid; i < rows * (D / 4); i += 256) {
-        const int r = i / (D / 4), d = i % (D / 4), t = r / G;
-        RowPart sum{-INFINITY, 0, vec<float, 4>{}};
-        const int at = r * (D / 4) + (d ^ r);
-        join(sum, ml[0][r].x, ml[0][r].y, ((const vec<float, 4> *)lds0)[at]);
-        join(sum, ml[1][r].x, ml[1][r].y, ((const vec<float, 4> *)lds1)[at]);
-        join(sum, ml[2][r].x, ml[2][r].y, ((const vec<float, 4> *)lds2)[at]);
-        join(sum, ml[3][r].x, ml[3][r].y, ((const vec<float, 4> *)lds3)[at]);
-        if (it.base < 0) {
-            const float f = one_by(sum.m, sum.l);
-            T *out = (T *)a.out + (it.t0 + t) * a.out_token_stride + (it.head * G + r - t * G) * a.out_head_stride + d * 4;
-            *(vec<T, 4> *)out = vec<T, 4>{(T)(sum.o[0] * f), (T)(sum.o[1] * f), (T)(sum.o[2] * f), (T)(sum.o[3] * f)};
-        } else {
-            const int64_t row = (int64_t)it.base + r;
-            if (d == 0) a.part_ml[row] = float2{sum.m, sum.l};
-            *(vec<float, 4> *)(a.part_o + row * D + d * 4) = sum.o;
+            for (int dt = 0; dt < D / 16; ++dt) o[g][dt] = vec<float, 4>{};
+        }
+        if (l[g] == 0 && lim[g] > first_there) m[g] = kNothing;
+        __syncthreads();
+        if (c == 0) ml[wave][col] = float2{m[g], l[g]};
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) ((vec<float, 4> *)lv)[col * (D / 4) + ((dt * 4 + c) ^ col)] = o[g][dt];
+        __syncthreads();
+        const int these = min(rows - g * 16, 16);
+        for (int i = tid; i < these * (D / 4); i += 256) {
+            const int r = i / (D / 4), d = i % (D / 4), row = g * 16 + r, t = row / G;
+            RowPart sum{-INFINITY, 0, vec<float, 4>{}};
+            const int at = r * (D / 4) + (d ^ r);
+            join(sum, ml[0][r].x, ml[0][r].y, ((const vec<float, 4> *)lds0)[at]);
+            join(sum, ml[1][r].x, ml[1][r].y, ((const vec<float, 4> *)lds1)[at]);
+            join(sum, ml[2][r].x, ml[2][r].y, ((const vec<float, 4> *)lds2)[at]);
+            join(sum, ml[3][r].x, ml[3][r].y, ((const vec<float, 4> *)lds3)[at]);
+            if (it.base < 0) {
+                const float f = one_by(sum.m, sum.l);
+                T *out = (T *)a.out + (it.t0 + t) * a.out_token_stride + (it.head * G + row - t * G) * a.out_head_stride + d * 4;
+                *(vec<T, 4> *)out = vec<T, 4>{(T)(sum.o[0] * f), (T)(sum.o[1] * f), (T)(sum.o[2] * f), (T)(sum.o[3] * f)};
+            } else {
+                const int64_t to = (int64_t)it.base + row;
+                if (d == 0) a.part_ml[to] = float2{sum.m, sum.l};
+                *(vec<float, 4> *)(a.part_o + to * D + d * 4) = sum.o;
+            }
         }
     }
     __syncthreads();
@@ -571,7 +610,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
     constexpr int KB = D == 256 ? 32 : 64, CH = D / 8, LOADS = KB * CH / 256, ROW = D * 2;
     constexpr int PIECE = CODED ? 16 : 8, CODE_LOADS = LOADS / 2 < 1 ? 1 : LOADS / 2;      // elements of 16 bytes in the cache
     __shared__ uint4 lk0[KB * CH], lv0[KB * CH], lk1[KB * CH], lv1[KB * CH];
-    __shared__ float2 narrow_ml[CODED ? 4 : 1][kNarrow];
+    __shared__ float2 narrow_ml[CODED ? 4 : 1][16];
     __shared__ int64_t where[4][KB];      // of the next tiles' rows, in pieces (of what is not there: any that is)
     __shared__ int64_t scale_at[CODED ? 4 : 1][CODED ? KB : 1];      // and of their scales
     constexpr int MINE = KB / 4;          // rows of a tile that each wave looks up
@@ -601,13 +640,14 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
     if constexpr (CODED) {      // (a loop of its own: within the other one both kinds' registers are too many)
         for (int i = blockIdx.x / kDies; i < n; i += step) {
             const PlanItem it = a.plan.items[i < n0 ? first0 + i : first1 + i - n0];
-            if (it.nt * G <= kNarrow) narrow_item<T, D>(a, it, lk0, lv0, lk1, lv1, narrow_ml);
+            if (it.nt * G <= 16) narrow_item<T, D, 1>(a, it, lk0, lv0, lk1, lv1, narrow_ml);
+            else if (it.nt * G <= kNarrow<D>) narrow_item<T, D, kNarrow<D> / 16>(a, it, lk0, lv0, lk1, lv1, narrow_ml);
         }
     }
     for (int i = blockIdx.x / kDies; i < n; i += step) {
         const PlanItem it = a.plan.items[i < n0 ? first0 + i : first1 + i - n0];
         const int rows = it.nt * G;
-        if (CODED && rows <= kNarrow) continue;
+        if (CODED && rows <= kNarrow<D>) continue;
         const int r = wave * 32 + col;
         const bool valid = r < rows;
         const int rt = (int)((uint32_t)r * inv_g >> 16), token = it.t0 + rt, head = it.head * G + r - rt * G;
