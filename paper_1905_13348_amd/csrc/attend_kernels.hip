@@ -629,6 +629,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
     const int vrow = half * 4 + (lane & 15) / 4;
     const int value_at = vrow * ROW + (((((lane >> 4) & 1) * 2 + (lane & 3) / 2) ^ value_turn<CH>(vrow)) << 4) + (lane & 1) * 8;
 
+    // where a thread writes the numbers that it makes of codes: of a row's pieces two side by side
+    const int store_row = tid / (CH / 2), store_piece = tid % (CH / 2) * 2;
+    const int k_store = store_row * ROW + ((store_piece ^ key_turn<CH>(store_row)) << 4);
+    const int v_store = store_row * ROW + ((store_piece ^ value_turn<CH>(store_row)) << 4);
+
     // Workgroups go to the dies in turn; each die takes a stretch of the groups' items, and behind them one of the
     // sequences', so that neighbouring items (the tiles that read the same keys) meet in one L2 and are there at the same
     // time.  Stretches are of equal cost as the plan counts it.  Of 256 sequences behind 32k prefixes: one stretch of both kinds to a die 458 us
@@ -713,16 +718,18 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_items(AttendAr
             }
         };
         auto store_codes = [&](auto buf) {
-            vec<T, 8> *const lk = (vec<T, 8> *)(buf.value ? lk1 : lk0), *const lv = (vec<T, 8> *)(buf.value ? lv1 : lv0);
+            constexpr int STEP = 256 / (CH / 2);      // rows of a round, which turn alike
+            static_assert(CODE_LOADS == 1 || (key_turn<CH>(STEP) == key_turn<CH>(0) && value_turn<CH>(STEP) == value_turn<CH>(0)), "");
+            char *const lk = (char *)(buf.value ? lk1 : lk0), *const lv = (char *)(buf.value ? lv1 : lv0);
+            int k_to = k_store, v_to = v_store;
+            asm volatile("" : "+v"(k_to), "+v"(v_to));      // (a few exclusive-ors a tile instead of fourteen registers)
 #pragma unroll
-            for (int x = 0; x < CODE_LOADS; ++x) {
-                const int row = (x * 256 + tid) / (CH / 2), c = tid % (CH / 2) * 2;
+            for (int x = 0; x < CODE_LOADS; ++x)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    lk[row * CH + ((c + h) ^ key_turn<CH>(row))] = decode8<T>(vec<uint32_t, 2>{ck[x][2 * h], ck[x][2 * h + 1]}, ek[x]);
-                    lv[row * CH + ((c + h) ^ value_turn<CH>(row))] = decode8<T>(vec<uint32_t, 2>{cv[x][2 * h], cv[x][2 * h + 1]}, ev[x]);
+                    *(vec<T, 8> *)(lk + (k_to ^ h << 4) + x * STEP * ROW) = decode8<T>(vec<uint32_t, 2>{ck[x][2 * h], ck[x][2 * h + 1]}, ek[x]);
+                    *(vec<T, 8> *)(lv + (v_to ^ h << 4) + x * STEP * ROW) = decode8<T>(vec<uint32_t, 2>{cv[x][2 * h], cv[x][2 * h + 1]}, ev[x]);
                 }
-            }
         };
         auto load = [&](auto buf, int slot) {
             uint4 *const lk = buf.value ? lk1 : lk0, *const lv = buf.value ? lv1 : lv0;
