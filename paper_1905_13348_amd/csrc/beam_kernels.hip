@@ -89,6 +89,25 @@ template <int LOWEST> __device__ __forceinline__ uint32_t reached_by(uint32_t ke
     return t;
 }
 
+// The same of a workgroup's threads, wave by wave through `counts`.  Where many are picked: a wave alone has too few lanes then for
+// a bound that is of use.  (64 of 8 x 128,000 fp32, with the waves' bounds 730 us.)
+constexpr int kManyPicks = 16;
+template <int LOWEST, int WAVES> __device__ __forceinline__ uint32_t reached_by_all(uint32_t key, int n, int (*counts)[WAVES])
+{
+    uint32_t t = 0;
+#pragma unroll 1
+    for (int bit = 31; bit >= LOWEST; --bit) {
+        const uint32_t next = t | 1u << bit;
+        const int mine = (int)__popcll(__ballot(key >= next));
+        if ((threadIdx.x & 63) == 0) counts[bit & 1][threadIdx.x >> 6] = mine;
+        __syncthreads();
+        int all = 0;
+        for (int w = 0; w < WAVES; ++w) all += counts[bit & 1][w];
+        if (all >= n) t = next;
+    }
+    return t;
+}
+
 // A wave's candidates: up to kKept, and those of a piece to each lane behind them.
 constexpr int kKept = 2 * kMostBeams, kWaveList = kKept + 64 * 8;
 
@@ -97,22 +116,43 @@ struct PartShared {
     uint32_t bound[kWaves];
     float top[kWaves];
     double sum[kWaves];
-    int counts[kWaves];
+    int counts[kWaves], reached[2][kWaves];
 };
 
-// The n entries of a wave's list become the `want` greatest (n is more), in any order; the least of them is returned.  (Rare, so
-// it takes few registers and not long code: 64 passes over the list.)
+// What all lanes' bits have in common (OF_ALL) or any lane's.
+template <bool OF_ALL> __device__ __forceinline__ uint32_t bits_of_wave(uint32_t x)
+{
+    over_wave([&](auto ctrl, auto rows) {
+        const uint32_t y = (uint32_t)neighbour<ctrl.value, rows.value>((int)x, OF_ALL ? -1 : 0);
+        x = OF_ALL ? x & y : x | y;
+    });
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+
+// The n entries of a wave's list become the `want` greatest (n is more), in any order; the least of them is returned.  Bit by bit
+// from the first in which entries differ, until just so many are left.  (Few registers and not long code: it stands in every
+// piece's way.  With all 64 bits, a list's rows one after the other: 64 of 8 x 128,000 fp32 774 us.)
 __device__ __forceinline__ u64 keep_greatest(u64 *list, int n, int want)
 {
     const int lane = threadIdx.x & 63;
-    u64 t = 0;
+    u64 both = ~0ull, any = 0;
+#pragma unroll 2
+    for (int i = 0; i < n; i += 64) {
+        const u64 x = list[min(i + lane, n - 1)];
+        both &= x;
+        any |= x;
+    }
+    both = (u64)bits_of_wave<true>((uint32_t)(both >> 32)) << 32 | bits_of_wave<true>((uint32_t)both);
+    any = (u64)bits_of_wave<false>((uint32_t)(any >> 32)) << 32 | bits_of_wave<false>((uint32_t)any);
+    int bit = 63 - __builtin_clzll(both ^ any);      // (entries differ: each has a number of its own)
+    u64 t = both & ~((2ull << bit) - 1);
 #pragma unroll 1
-    for (int bit = 63; bit >= 0; --bit) {
+    for (; bit >= 0; --bit) {
         const u64 next = t | 1ull << bit;
         int count = 0;
-#pragma unroll 1
-        for (int i = 0; i < n; i += 64) count += (int)__popcll(__ballot(i + lane < n && list[i + lane] >= next));
+        for (int i = 0; i < n; i += 64) count += (int)__popcll(__ballot(i + lane < n && list[min(i + lane, n - 1)] >= next));
         if (count >= want) t = next;
+        if (count == want) break;
     }
     int at = 0;
 #pragma unroll 1
@@ -204,8 +244,11 @@ __global__ __launch_bounds__(kThreads, 4) void k_beam_parts(BeamArgs a)
                     mine = fmaxf(mine, most[j]);
                 }
                 // of a wave alone so many lanes have one at least as great: the part's best are not below any wave's bound
-                least = max(least, reached_by<16>(mine > -INFINITY ? key_of(mine) : 0, a.picks));
-                if (c == 0) {
+                const uint32_t key = mine > -INFINITY ? key_of(mine) : 0;
+                if (a.picks <= kManyPicks || c) least = max(least, reached_by<16>(key, a.picks));
+                if (c == 0 && a.picks > kManyPicks) {
+                    least = max(reached_by_all<16, kWaves>(key, a.picks, sh.reached), kNever + 1);
+                } else if (c == 0) {
                     __syncthreads();
                     if (lane == 0) sh.bound[wave] = least;
                     __syncthreads();
@@ -320,6 +363,7 @@ struct QueryShared {
     double shift[kMostBeams], score[kMostBeams], factor[kMostBeams];
     float top[kMostBeams];
     uint32_t listed, bound[kQueryWaves];
+    int reached[2][kQueryWaves];
     u64 wave_rank[kQueryWaves], wave_number[kQueryWaves];
 };
 
@@ -392,11 +436,15 @@ __global__ __launch_bounds__(kQueryThreads) void k_beam_queries(BeamArgs a)
         };
         uint32_t mine = 0;
         each([&](double rank, u64) { mine = max(mine, (uint32_t)(key_of(rank) >> 32)); });
-        const uint32_t bound = reached_by<8>(mine, a.picks);      // (to 12 bits behind the first: of 11 bits the exponent's)
-        if (lane == 0) sh.bound[wave] = bound;
-        __syncthreads();
-        uint32_t least = 0;
-        for (int w = 0; w < kQueryWaves; ++w) least = max(least, sh.bound[w]);
+        uint32_t least = 0;      // (to 12 bits behind the first: 11 are the exponent's)
+        if (a.picks <= kManyPicks) {
+            const uint32_t bound = reached_by<8>(mine, a.picks);
+            if (lane == 0) sh.bound[wave] = bound;
+            __syncthreads();
+            for (int w = 0; w < kQueryWaves; ++w) least = max(least, sh.bound[w]);
+        } else {
+            least = reached_by_all<8, kQueryWaves>(mine, a.picks, sh.reached);
+        }
         each([&](double rank, u64 number) {
             if ((uint32_t)(key_of(rank) >> 32) < least) return;
             const uint32_t at = atomicAdd(&sh.listed, 1u);
