@@ -24,7 +24,7 @@ __device__ __forceinline__ int parent_of(const AdvanceArgs &a, int s)
 // ---- rows that go on from others ----------------------------------------------------------------
 
 // A workgroup takes some columns of the table, of all rows: what the rows are to be is read before any is written.  Counts
-// change by atomics, whose order does not matter.
+// change by atomics, whose order does not matter.  (4 us: a launch and four trips to memory in a row.)
 constexpr int kCells = 8192;
 __global__ __launch_bounds__(kThreads) void k_reparent(AdvanceArgs a, int columns)
 {
@@ -128,7 +128,8 @@ constexpr int kFewTokens = 4096;
 
 // One workgroup; thread t has sequences t, t + 1024, ...  What bounds it is the chain of its steps, each a trip to memory or a
 // barrier, and the first fetch of its instructions: so few sequences have a shorter code, sums are taken two at a time and only
-// where they may differ from what is known, and the counts of pages are under way from the start.
+// where they may differ from what is known, and the counts of pages are under way from the start.  (256 sequences that drop drafts or
+// take some 8 to 10 us, before that 17; 300 prompts 13, before that 20; 4096 sequences, four to a thread, 33.)
 template <int ROWS>
 __global__ __launch_bounds__(kThreads) void k_advance(AdvanceArgs a)
 {
@@ -328,7 +329,8 @@ __global__ __launch_bounds__(256) void k_tokens(AdvanceArgs a)
 
 // ---- copies of pages ----------------------------------------------------------------------------
 
-// Workgroups (sequence, keys or values, part): a thread takes 16 bytes at a time.
+// Workgroups (sequence, keys or values, part): a thread takes 16 bytes at a time.  (Bound by the launch: 192 pages of up to 16 keys
+// of 4 heads of 128 in bf16 4.4 us.)
 __global__ __launch_bounds__(256) void k_copy(CopyArgs a)
 {
     const int s = blockIdx.x, parts = gridDim.z;

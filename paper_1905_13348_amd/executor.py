@@ -8,6 +8,14 @@
     ex.attend(cache, batch, q_out, out, scale)
     ex.sample(logits, draws, token, prob, top_p=...)     # behind the last layer
 
+A cache may be of 8 bits (``ex.cache(..., k_scale=, v_scale=)``), and a batch's arrays may be kept on the device:
+
+    table = ex.table(seqs, width, page_size, pages, max_tokens)
+    batch = ex.batch(cache, heads, **table.arrays())
+    ex.advance(table, new, parent)                       # once a step: lengths, pages, the batch's arrays
+    ex.copy(cache, table)                                # each layer, before its append
+    ex.beam(logits, scores, parent, token, score)        # instead of sample: the next step's parents
+
 Argument marshalling only, like ``Selector``: shapes and types are checked here, values in the library.  A cache and a
 batch keep references to their tensors; the tensors' contents may change from step to step.  There is no backward pass:
 inputs that require a gradient are refused where gradients are recorded.
