@@ -129,7 +129,7 @@ constexpr int kFewTokens = 4096;
 // One workgroup; thread t has sequences t, t + 1024, ...  What bounds it is the chain of its steps, each a trip to memory or a
 // barrier, and the first fetch of its instructions: so few sequences have a shorter code, sums are taken two at a time and only
 // where they may differ from what is known, and the counts of pages are under way from the start.  (256 sequences that drop drafts or
-// take some 8 to 10 us, before that 17; 300 prompts 13, before that 20; 4096 sequences, four to a thread, 33.)
+// take some 8 to 10 us, before that 17; 300 prompts 10.4, before that 20; 4096 sequences, four to a thread, 33.)
 template <int ROWS>
 __global__ __launch_bounds__(kThreads) void k_advance(AdvanceArgs a)
 {
@@ -235,7 +235,11 @@ __global__ __launch_bounds__(kThreads) void k_advance(AdvanceArgs a)
         if (refused || tokens <= (uint32_t)a.t.max_tokens) break;
         refused = true;      // once more: what those need that are turned away does not count
     }
-    __syncthreads();
+    bool copies = false;
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+        if (r * kThreads < S) copies |= last[r] >= 0;
+    copies = __syncthreads_or(copies);
 
     // free pages, in order, to who needs them
     uint32_t found = 0;
@@ -262,10 +266,10 @@ __global__ __launch_bounds__(kThreads) void k_advance(AdvanceArgs a)
             refs[page] = 1;
         }
     }
-    if (pages) {
-        __threadfence();
-        __syncthreads();
-    }
+    // What was handed out is read again where pages ran out, or for a copy: only then it has to be in memory first.  (300 prompts, a
+    // fence in any case: 13.4 us, so 10.4.)
+    if (pages && (copies || found < pages)) __threadfence();
+    __syncthreads();
 
     // who got it
     uint32_t total = 0;
