@@ -129,18 +129,38 @@ template <bool OF_ALL> __device__ __forceinline__ uint32_t bits_of_wave(uint32_t
     return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
 }
 
+__device__ __forceinline__ uint32_t min_of_wave(uint32_t x)
+{
+    over_wave([&](auto ctrl, auto rows) { x = min(x, (uint32_t)neighbour<ctrl.value, rows.value>((int)x, -1)); });
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+
 // The n entries of a wave's list become the `want` greatest (n is more), in any order; the least of them is returned.  Bit by bit
-// from the first in which entries differ, until just so many are left.  (Few registers and not long code: it stands in every
-// piece's way.  With all 64 bits, a list's rows one after the other: 64 of 8 x 128,000 fp32 774 us.)
+// from the first in which entries differ, until just so many are left; where those with the least logit (a mask's) are among
+// them, from the first bit in which these differ.  (Few registers and not long code: it stands in every
+// piece's way.  With all 64 bits, a list's rows one after the other: 64 of 8 x 128,000 fp32 774 us.  Rows whose
+// logits are -60,000 but for 129, 512 rows of 128,000 bf16: from the first bit in which any differ 150 us, so 57.)
 __device__ __forceinline__ u64 keep_greatest(u64 *list, int n, int want)
 {
     const int lane = threadIdx.x & 63;
     u64 both = ~0ull, any = 0;
+    uint32_t lowest = ~0u;
 #pragma unroll 2
     for (int i = 0; i < n; i += 64) {
         const u64 x = list[min(i + lane, n - 1)];
         both &= x;
         any |= x;
+        lowest = min(lowest, (uint32_t)(x >> 32));
+    }
+    lowest = min_of_wave(lowest);
+    int above = 0;
+    for (int i = 0; i < n; i += 64) above += (int)__popcll(__ballot(i + lane < n && (uint32_t)(list[min(i + lane, n - 1)] >> 32) > lowest));
+    if (above < want) {
+        both = ~0ull, any = 0;
+        for (int i = 0; i < n; i += 64) {
+            const u64 x = list[min(i + lane, n - 1)];
+            if ((uint32_t)(x >> 32) == lowest) { both &= x; any |= x; }
+        }
     }
     both = (u64)bits_of_wave<true>((uint32_t)(both >> 32)) << 32 | bits_of_wave<true>((uint32_t)both);
     any = (u64)bits_of_wave<false>((uint32_t)(any >> 32)) << 32 | bits_of_wave<false>((uint32_t)any);

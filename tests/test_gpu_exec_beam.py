@@ -156,6 +156,21 @@ def test_masks(dtype):
         check(x[:1], np.zeros((1, 1)), picks, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("vocab", [700, 20_011, 100_003])
+@pytest.mark.parametrize("picks", [1, 8, 33])
+def test_finite_masks(dtype, vocab, picks):
+    """All of a row but a few logits are one low number, which is picked where there are not enough others; lists fill with it."""
+    rng = np.random.default_rng(picks + vocab)
+    left = [0, 1, picks - 1, picks, picks + 1, 129]
+    x = np.full((len(left), vocab), -60000.0)
+    for row, k in zip(x, left):
+        at = rng.choice(vocab, k, replace=False)
+        row[at] = rng.integers(-20, 20, k) / 4        # (ties among these, too)
+    check(x, np.zeros((len(left), 1)), picks, dtype)
+    check(x, -rng.random((2, 3)), picks, dtype)
+
+
 @pytest.mark.parametrize("picks", [2, 4, 12])
 def test_beams_that_ended(picks):
     rng = np.random.default_rng(4)
