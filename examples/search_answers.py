@@ -5,7 +5,7 @@
 Every query has some beams, each a sequence of the worker's table.  A step picks the best continuations of all beams of a query,
 lets the sequences go on from the beams that they continue (pages are shared, a page that is not full is copied), and appends and
 attends over a cache of 8 or 16 bits.  Lengths, pages and the batch's arrays stay on the device; a beam that has ended takes no
-more tokens and keeps its score.
+more tokens and keeps its score, and one for which a query has no continuation left is empty until the query has enough again.
 """
 import argparse
 import os
@@ -29,8 +29,8 @@ def make_cache(ex, variant, pages, page, bits, block):
 
 
 def search(variant, queries, tokens, beams=4, end_token=1, bits=8, alpha=0.7, page=16, block=8):
-    """queries: token numbers of each (one at least).  Returns the beams' tokens [queries, beams, tokens], their scores, and of
-    every step what was picked from what."""
+    """queries: token numbers of each (one at least).  Returns the beams' tokens [queries, beams, tokens] (-1 and a score of minus
+    infinity where there were fewer answers than beams), their scores, and of every step what was picked from what."""
     v, Q, W = variant, len(queries), beams
     S, longest, all_new = Q * W, max(len(q) for q in queries) + tokens, sum(len(q) for q in queries)
     i32 = lambda a: torch.as_tensor(a, dtype=torch.int32).cuda()
@@ -76,22 +76,29 @@ def search(variant, queries, tokens, beams=4, end_token=1, bits=8, alpha=0.7, pa
     length = torch.ones((Q, W), device="cuda")
     history = torch.zeros((S, 0), dtype=torch.int32, device="cuda")
     batch, picked = batch_of(S), []
+    refused = torch.zeros((), dtype=torch.int64, device="cuda")
     for t in range(tokens):
         parent, token = (torch.empty((Q, W), dtype=torch.int32, device="cuda") for _ in range(2))
         best = torch.empty((Q, W), device="cuda")
         factor = length ** -alpha
         ex.beam(logits, scores, parent, token, best, ended=ended, factor=factor, end_token=end_token)
-        go = parent.view(-1).long()
         picked.append(dict(logits=logits, scores=scores, ended=ended, factor=factor, parent=parent, token=token, best=best, history=history))
+        # (a pick of -1: the query had fewer continuations than beams; its score of minus infinity keeps it from going on)
+        none = parent.view(-1) < 0
+        go = parent.view(-1).clamp_min(0).long()
         was = ended.view(-1)[go].view(Q, W)
         length = length.view(-1)[go].view(Q, W) + (1 - was)
-        ended, scores = (token == end_token).int(), best
-        history = torch.cat([history[go], token.view(-1, 1)], dim=1)
+        ended, scores = ((token == end_token) | (token < 0)).int(), best
+        history = torch.cat([history[go], token.view(-1, 1)], dim=1).masked_fill(none[:, None], -1)
         if t + 1 < tokens:
-            ex.advance(table, (1 - ended).view(-1), parent.view(-1))
-            x = v.embed[token.view(-1)[table.token_seq[:S].clamp_min(0).long()].long()]
+            new = (1 - ended).view(-1)
+            ex.advance(table, new, parent.view(-1))
+            refused += (table.taken != new).sum()
+            x = v.embed[token.view(-1)[table.token_seq[:S].clamp_min(0).long()].clamp_min(0).long()]
             logits = step(x, batch)[table.seq_start[:-1].clamp_max(S - 1).long()]
     torch.cuda.synchronize()
+    if refused:      # (whose logits would be another beam's)
+        raise RuntimeError(f"{int(refused)} steps of beams for which no pages were left")
     ex.destroy()
     return history.view(Q, W, tokens), scores, picked
 
