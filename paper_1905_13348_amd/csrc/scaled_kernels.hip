@@ -9,14 +9,24 @@ namespace {
 
 // ---- append -----------------------------------------------------------------------------------
 
-// Sine and cosine of a position's turn.  In turns, of which quarters are taken off in 64 bits: what is left is an eighth at most,
-// and keeps its bits in 32.  (With whole turns taken off alone an angle near a half or a whole one is off by 2e-7: five times as
-// many codes fall on the other side of a border.)
+// Sine and cosine of a position's turn, to 0.76 and 0.59 of a last place of 32 bits, 0.29 rms (half of one at most, and 0.29 rms, is the
+// rounding itself).  In turns, of which quarters are taken off in 64 bits; what is left is an angle x of an eighth of a turn at most, as
+// a number of 32 bits and what that leaves out.  sin x = x - x^3 / 6 + .., cos x = 1 - x^2 / 2 + ..: the leading terms are added with what
+// their roundings leave out, the others (up to 0.08 and 0.02) in 32 bits; behind the last ones 1e-4 and 2e-3 of a place are left.
+// (The series in 64 bits altogether: eleven registers more, and two waves to a SIMD instead of three.)
 __device__ __forceinline__ float2 turned(int pos, double freq)
 {
-    const double turns = (double)pos * freq * 0.15915494309189535, q = rint(4 * turns);
-    float s, c;
-    sincospif(2.0f * (float)(turns - 0.25 * q), &s, &c);
+    const double turns = (double)pos * freq * 0.15915494309189535, q = rint(4 * turns), angle = (turns - 0.25 * q) * 6.283185307179586;
+    const float x = (float)angle, rest = (float)(angle - (double)x), z = x * x;
+    const float z_rest = __builtin_fmaf(x, x, -z) + 2 * x * rest;
+    float p = 1.0f / 362880, c4 = -1.0f / 3628800;
+    p = __builtin_fmaf(__builtin_fmaf(-1.0f / 39916800, z, p), z, -1.0f / 5040);
+    p = __builtin_fmaf(__builtin_fmaf(p, z, 1.0f / 120), z, -1.0f / 6);
+    c4 = __builtin_fmaf(__builtin_fmaf(c4, z, 1.0f / 40320), z, -1.0f / 720);
+    c4 = __builtin_fmaf(c4, z, 1.0f / 24);
+    const float s = x + __builtin_fmaf(x * z, p, rest * __builtin_fmaf(z, -0.5f, 1.0f));
+    const float half = 0.5f * z, most = 1 - half;
+    const float c = most + ((1 - most) - half + __builtin_fmaf(z * z, c4, -0.5f * z_rest));
     const int quarter = (int)(int64_t)q;
     const float sn = quarter & 1 ? c : s, cs = quarter & 1 ? s : c;
     return float2{quarter & 2 ? -sn : sn, (quarter + 1) & 2 ? -cs : cs};
