@@ -319,6 +319,9 @@ __device__ __forceinline__ void join(RowPart &a, float m1, float l1, vec<float, 
     a.m = m2;
 }
 
+// The least scale with which a code may be infinite as a number of T: 448 times 2^(e - 127) is 1.75 times 2^(e - 119).
+template <typename T> constexpr uint32_t kInfinite = std::is_same<T, fp16_t>::value ? 135 : 247;
+
 // Rows of an item that its waves go through side by side.  (32 rows of 256 dimensions are more than a wave's registers.)
 template <int D> constexpr int kNarrow = D == 256 ? 16 : 32;
 
@@ -326,10 +329,11 @@ template <int D> constexpr int kNarrow = D == 256 ? 16 : 32;
 // these.  So each wave has keys of its own, 32 at a time, nothing waits for another wave until the end, and the waves' parts are
 // joined through LDS.  Lane (key, c) loads the quarter c of a key's and of a value's codes, in one piece; with the dimensions
 // numbered that way for both operands the codes go from memory to the first product through registers alone.  Values are
-// written to the wave's part of LDS as numbers, to be read transposed.  (bf16, 32 query heads on 8 KV heads of 128 dimensions: one
-// token behind 200,003 keys 105 us with the tiles of the other items, so 81, 5.1 TB/s where a large copy reaches 5.2; 192 sequences of
-// up to 16,000 keys behind 8000 shared ones 1206 us, so 823, 4.8 TB/s.  64 dimensions, 64 bytes
-// to a key and head: 58 us, 3.5 TB/s.  With four tokens to each of 64 sequences and 64 heads, 32 rows: 242 us, so 198.)
+// written to the wave's part of LDS as numbers, to be read transposed.  (bf16, 32 query heads on 8 KV heads of 128 dimensions; pages
+// with heads in front: one token behind 200,003 keys 105 us with the tiles of the other items, so 82, 5.0 TB/s where a large copy reaches
+// 5.2; with tokens in front, where a head's keys are 128 bytes each a line apart, 109.  192 sequences of up to 16,000 keys
+// behind 8000 shared ones 1206 us, so 829, 4.8 TB/s.  64 dimensions, heads in front 50 us, 4.1 TB/s, tokens in front 59.  With four
+// tokens to each of 64 sequences and 64 heads, 32 rows: 242 us, so 204.)
 template <typename T, int D, int GROUPS>
 __device__ __forceinline__ void narrow_item(const AttendArgs &a, const PlanItem &it, uint4 *lds0, uint4 *lds1, uint4 *lds2, uint4 *lds3,
                                             float2 (*ml)[16])
@@ -372,7 +376,7 @@ __device__ __forceinline__ void narrow_item(const AttendArgs &a, const PlanItem 
         m[g] = -INFINITY;
         l[g] = 0;
     }
-    bool far = false, odd = false;
+    bool far = false, odd = false, infinite = false;
     int first_there = 0x7fffffff;
 
     int page[2];                                     // of the next tile's keys; -1: not there
@@ -417,10 +421,13 @@ __device__ __forceinline__ void narrow_item(const AttendArgs &a, const PlanItem 
     for (; kt < end; kt += 4 * KEYS) {
         const unsigned long long ballots[2] = {__ballot(there[0]), __ballot(there[1])};
         const uint32_t bits = (uint32_t)(ballots[0] & 0xffff) | (uint32_t)(ballots[1] & 0xffff) << 16;
-        const bool part = kt + KEYS > lo;      // some rows see keys that others do not
+        // (an infinite value beside a second weight, which may be 0 or negative, would make NaN)
+        const bool high = __any((there[0] && ve[0] >= kInfinite<T>) || (there[1] && ve[1] >= kInfinite<T>));
+        infinite |= high;
+        const bool part = kt + KEYS > lo || high;      // (the first: some rows see keys that others do not)
         if (bits && first_there == 0x7fffffff) first_there = kt + __builtin_ctz(bits);
-        // values, as numbers: zeros where nothing is there; where rows differ in what they see, what is no number is taken out
-        // here and added at the end where it is seen (a weight of zero would make NaN of it)
+        // values, as numbers: zeros where nothing is there; where rows differ in what they see, or values may be infinite, what is no
+        // number is taken out here and added at the end where it is seen (a weight of zero would make NaN of it)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -502,7 +509,11 @@ __device__ __forceinline__ void narrow_item(const AttendArgs &a, const PlanItem 
                 scale = 1.0f;
             }
         }
-        vec<T, 8> pt[GROUPS];
+        // Weights go to the product in two numbers each, of which the second is what the first one's rounding leaves out: half a step of
+        // half a step of a weight is lost, 2^-16 in bf16 and 2^-22 in fp16.  (With one number results are off by up to 2.2e-3 of
+        // their norm in bf16, for 1.7e-3 of the result's own rounding.  The loads hide most of the second products: the times above
+        // were 81, 820, 48 and 197 us without.)
+        vec<T, 8> pt[GROUPS], rest[GROUPS];
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
@@ -510,9 +521,12 @@ __device__ __forceinline__ void narrow_item(const AttendArgs &a, const PlanItem 
                 const vec<float, 2> e = {exp2_fast(s[g][x / 4][x % 4] * scale - ref[g]), exp2_fast(s[g][x / 4][x % 4 + 1] * scale - ref[g])};
                 l[g] += e[0];
                 l[g] += e[1];
-                const vec<T, 2> y = __builtin_convertvector(e, vec<T, 2>);      // (the rounding of full tiles)
+                const vec<T, 2> y = __builtin_convertvector(e, vec<T, 2>);
+                const vec<T, 2> z = __builtin_convertvector(e - __builtin_convertvector(y, vec<float, 2>), vec<T, 2>);
                 pt[g][x] = y[0];
                 pt[g][x + 1] = y[1];
+                rest[g][x] = z[0];
+                rest[g][x + 1] = z[1];
             }
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) {
@@ -525,11 +539,13 @@ __device__ __forceinline__ void narrow_item(const AttendArgs &a, const PlanItem 
             }
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g) o[g][dt] = Mfma<T>::run(vf.v, pt[g], o[g][dt]);
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) o[g][dt] = Mfma<T>::run(vf.v, rest[g], o[g][dt]);
         }
     }
     if (__any(odd)) {      // the values that were taken out, of the tiles that they were taken out of
         for (int t = it.k0 + wave * KEYS; t < end; t += 4 * KEYS) {
-            if (t + KEYS <= lo) continue;
+            if (t + KEYS <= lo && !infinite) continue;
             for (int key = t; key < min(t + KEYS, end); ++key) {
                 const int64_t page = table[key >> a.cache.page_shift];
                 if (page < 0 || page >= a.cache.num_pages) continue;
