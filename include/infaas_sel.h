@@ -703,13 +703,16 @@ typedef struct {
  * The tokens of a sequence stand one behind the other: token t of sequence s is at position
  * d_token_pos[d_seq_start[s]] + t - d_seq_start[s].  One whose d_token_pos is another (padding at the end, say) is not written, nor
  * are those of a sequence whose first token has none.  A block belongs to one sequence of the batch (a page that several
- * share is full, or copied first: infaas_sel_exec_advance).  Needs d_seq_start as well.  Errors: INVALID_ARG, HIP.
+ * share is full, or copied first: infaas_sel_exec_advance).  Needs d_seq_start as well.  A block's tokens are one workgroup's to
+ * scale, or a few's: blocks of 8 to 64 keys are what the call is made for (14,003 tokens of one sequence, 8 heads of 128: 80 us
+ * with blocks of 64, 450 with 1024, 5300 with 16,384).  Errors: INVALID_ARG, HIP.
  */
 int infaas_sel_exec_append_scaled(infaas_sel_exec_t *x, const infaas_sel_cache *cache, const infaas_sel_scales *scales,
                                   const infaas_sel_batch *batch, const infaas_sel_append_args *args, void *hip_stream);
 
 /* infaas_sel_exec_attend over a cache of 8 bits: the same plan, the same result as over a cache that holds those numbers in
- * the queries' type, up to the order of its sums.  Errors: INVALID_ARG, HIP, OOM. */
+ * the queries' type, up to the order of its sums and the rounding of weights (where few rows see the same keys, up to 32 tokens times
+ * query heads of a KV head, 16 of 256 dimensions, weights are not rounded to 16 bits).  Errors: INVALID_ARG, HIP, OOM. */
 int infaas_sel_exec_attend_scaled(infaas_sel_exec_t *x, const infaas_sel_cache *cache, const infaas_sel_scales *scales,
                                   const infaas_sel_batch *batch, const void *d_q, int64_t q_token_stride, int64_t q_head_stride,
                                   void *d_out, int64_t out_token_stride, int64_t out_head_stride, float scale, void *hip_stream);
@@ -760,7 +763,8 @@ typedef struct {
  *       Pages are handed out the lowest-numbered first, to the sequences in their order.  If its last page is not full, and
  *       other rows name it as well, the sequence gets a page for a copy of it first (d_copies): infaas_sel_exec_copy has to run,
  *       for every layer's cache, before the step's keys are appended.
- * A step's arrays are then those of a batch of max_tokens tokens (in a replayed graph, too).  Lengths that are out of range count as the
+ * A step's arrays are then those of a batch of max_tokens tokens (in a replayed graph, too), or, where the caller knows that no more
+ * come, of their first so many: a batch's work and memory go by its size, padding or not.  Lengths that are out of range count as the
  * nearest that is not, pages in the table that are not there as none.  Errors: INVALID_ARG, HIP.
  */
 int infaas_sel_exec_advance(infaas_sel_exec_t *x, const infaas_sel_table *table, const int32_t *d_new, const int32_t *d_parent,

@@ -64,7 +64,7 @@ __device__ __forceinline__ UnitRange unit_range(const BatchArgs &b, const CacheA
 // one at least to every tile).  How many depends on the rows of the tiles (their mean by cost): see kFewItems.
 // 9 to 11 us for few sequences, 16 to 20 for 256 behind prefixes or four prompts of 2048: once a step, for all layers.
 // The cost counts all keys of a sequence, also those behind a tile's tokens.  Behind a long prefix that is nothing; of a prompt
-// alone the dies' work is uneven (1024 tokens of 32 heads on 8: from 2.1 to 0.02 of the mean, 45 us), below 4096
+// alone the dies' work is uneven (1024 tokens of 32 heads on 8: from 2.1 to 0.02 of the mean, 56 us), below 4096
 // tokens, from which on a tile is one item.
 __global__ __launch_bounds__(kPlanThreads) void k_plan(BatchArgs b, CacheArgs c, PlanView p, int max_items, int max_rows)
 {
@@ -623,7 +623,7 @@ __device__ __forceinline__ void narrow_item(const AttendArgs &a, const PlanItem 
 // CODED: the cache has codes of 8 bits and scales.  A tile's codes then come into registers, and are written to LDS as numbers
 // of T when the tile's turn comes: half the bytes from memory, and a conversion of two numbers to an instruction, which the
 // waves share.  Full tiles are bound as those of a 16-bit cache are: prompts of up to 700 tokens behind 12,000 keys (fp16, 32 heads on
-// 4 of 128) 730 us, 640 TFLOP/s (bf16 668), where tiles of a 16-bit cache reach 608 (637) with prompts of that kind.  Converting a tile while the products of the one
+// 4 of 128) 708 to 728 us, 640 to 660 TFLOP/s (bf16 686), where tiles of a 16-bit cache reach 623 (655) with prompts of that kind.  Converting a tile while the products of the one
 // before it run, two tiles ahead, took 737 for 729 in turns; matrix instructions on codes would need the queries and weights
 // in two codes each, as many products, and a second rounding of every weight.
 template <typename T, int D, bool CODED>

@@ -90,7 +90,7 @@ template <int LOWEST> __device__ __forceinline__ uint32_t reached_by(uint32_t ke
 }
 
 // The same of a workgroup's threads, wave by wave through `counts`.  Where many are picked: a wave alone has too few lanes then for
-// a bound that is of use.  (64 of 8 x 128,000 fp32, with the waves' bounds 730 us.)
+// a bound that is of use.  (64 picks, 16 queries of 8 beams x 128,000 fp32: with the waves' bounds 741 us, so 56.)
 constexpr int kManyPicks = 16;
 template <int LOWEST, int WAVES> __device__ __forceinline__ uint32_t reached_by_all(uint32_t key, int n, int (*counts)[WAVES])
 {
@@ -138,8 +138,8 @@ __device__ __forceinline__ uint32_t min_of_wave(uint32_t x)
 // The n entries of a wave's list become the `want` greatest (n is more), in any order; the least of them is returned.  Bit by bit
 // from the first in which entries differ, until just so many are left; where those with the least logit (a mask's) are among
 // them, from the first bit in which these differ.  (Few registers and not long code: it stands in every
-// piece's way.  With all 64 bits, a list's rows one after the other: 64 of 8 x 128,000 fp32 774 us.  Rows whose
-// logits are -60,000 but for 129, 512 rows of 128,000 bf16: from the first bit in which any differ 150 us, so 57.)
+// piece's way.  Rows whose logits are -60,000 but for 129, 512 rows of 128,000 bf16: from the first bit in which any differ 150 us,
+// so 57.)
 __device__ __forceinline__ u64 keep_greatest(u64 *list, int n, int want)
 {
     const int lane = threadIdx.x & 63;

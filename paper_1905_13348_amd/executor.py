@@ -189,7 +189,11 @@ class Table:
 
     State, which ``Executor.advance`` takes a step further: ``page_table`` [sequences, width], ``seq_len`` [sequences],
     ``page_refs`` [pages].  What it writes beside that: ``seq_start``, ``token_seq`` and ``token_pos``, which with the state are the arrays
-    of a batch of ``max_tokens`` tokens (``arrays()``), ``taken`` [sequences] and ``copies`` [sequences, 3]."""
+    of a batch of ``max_tokens`` tokens (``arrays()``), ``taken`` [sequences] and ``copies`` [sequences, 3].
+
+    A batch's work and memory go by its size, padding or not.  Where prompts and single tokens take turns, make a batch of each kind:
+    of ``arrays()`` as they are, and with ``token_seq`` and ``token_pos`` cut to the tokens that a step has at the most
+    (``token_seq[:num_seqs]`` for one of each sequence)."""
 
     def __init__(self, num_seqs: int, table_width: int, page_size: int, num_pages: int, max_tokens: int, device: int = 0):
         torch = _use_torch()
